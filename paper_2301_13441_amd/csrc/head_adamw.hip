@@ -1,0 +1,303 @@
+// One AdamW step over many tensors, on gfx950 (the formulas and the 8-bit states: head.h).
+//
+// Bound by memory: 28 bytes a value with float32 gradients and states, 14 with bfloat16 gradients and states in 8 bits.
+// A launch takes up to TENSORS tensors, whose addresses go by value with its arguments: there is no table on the
+// device to keep, and a captured launch carries its own.  A workgroup finds its tensor by the number of its first block of
+// VALUES values and takes one block.  A lane takes 8 adjacent values, so that 16 lanes hold the HEAD_BLOCK = 128 values
+// of an 8-bit scale and their largest magnitude is four exchanges away.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "head_device.hpp"
+
+namespace head_impl {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int EACH = 8;                   // values of a lane
+constexpr int VALUES = THREADS * EACH;    // values of a workgroup
+constexpr int TENSORS = 40;               // tensors of a launch
+constexpr int64_t MAX_GRID = 1 << 22;     // workgroups of a launch: 2^30 threads
+static_assert(HEAD_BLOCK == 16 * EACH, "a scale's values are those of 16 lanes");
+
+struct Tensor {
+    float *param;
+    const void *grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    bf16 *copy;
+    int64_t n;
+    uint32_t key;      // of the random numbers
+    int32_t wide;      // all addresses are whole in pieces of EACH values, or 16 bytes
+};
+struct Batch {
+    Tensor tensor[TENSORS];
+    int64_t first[TENSORS + 1];  // first block of a tensor; the last entry: the number of blocks
+    int32_t count;
+};
+struct Numbers {
+    float beta1, rest1, beta2, rest2, keep, rate, root, eps;  // rest: 1 - beta; keep: 1 - rate decay; rate, root: with the corrections
+};
+
+__host__ __device__ inline uint32_t hash(uint32_t x)  // a multiply and xor-shift finaliser: every bit depends on every other
+{
+    x = (x ^ (x >> 16)) * 0x7FEB352Du;
+    x = (x ^ (x >> 15)) * 0x846CA68Bu;
+    return x ^ (x >> 16);
+}
+
+// What an e4m3 code stands for, times 2^(s - 134).
+__device__ __forceinline__ float decode(uint32_t code, int s)
+{
+    const int exponent = (code >> 3) & 15, digits = code & 7;
+    if ((code & 127) == 127) return __builtin_nanf("");
+    const float y = ldexpf(static_cast<float>(digits + (exponent ? 8 : 0)), (exponent ? exponent : 1) - 144 + s);
+    return code & 128 ? -y : y;
+}
+
+// Scale byte of a block whose largest finite magnitude is `most`: its exponent + 127, at least 1; 0 for a block of zeros.
+__device__ __forceinline__ int scale_of(float most)
+{
+    if (!(most > 0)) return 0;
+    return max(1, static_cast<int>(__float_as_uint(most) >> 23));
+}
+
+// 2^(134 - s), by which a block of scale s is multiplied before it is coded.  By powf, which misses some powers by one rounding
+// (2^16 among them): that is how torch.ldexp takes them here, and a step written in torch then gives the same codes as
+// this kernel, where ldexpf would give about one of a million another one.  powf is long: a workgroup makes a table of them.
+__device__ __forceinline__ float factor_of(int s) { return powf(2.0f, static_cast<float>(134 - s)); }
+
+// The code of x in a block of scale s, rounded up where the rest plus `random` (16 bits, as a fraction) reaches one.
+__device__ __forceinline__ uint32_t encode(float x, int s, float factor, uint32_t random, bool keep)
+{
+    if (!(fabsf(x) < INFINITY)) return 127;
+    if (s == 0) return 0;
+    const float y = fabsf(x) * factor;                                            // below 256
+    const int exponent = max(-6, static_cast<int>(__float_as_uint(y) >> 23) - 127);
+    // in steps of the code, below 16: the sum has room for the 16 bits of the random number
+    float whole = floorf(ldexpf(y, 3 - exponent) + static_cast<float>(random) * (1.0f / 65536));
+    if (keep && x > 0 && whole == 0) whole = 1;
+    const uint32_t code = static_cast<uint32_t>(8 * (exponent + 6) + static_cast<int>(whole));
+    return code | (x < 0 ? 128u : 0u);
+}
+
+template <class T>
+struct Values {
+    T v[EACH];
+};
+
+// 8 adjacent values, `some` of which exist; `wide`: all do, and their address is whole in 16 bytes or their own length.
+template <class T>
+__device__ __forceinline__ void take(Values<T> &to, const T *from, int some, bool wide)
+{
+    constexpr int P = sizeof(T) * EACH > 16 ? 16 / sizeof(T) : EACH;
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < EACH; i += P) *reinterpret_cast<Pack<T, P> *>(to.v + i) = *reinterpret_cast<const Pack<T, P> *>(from + i);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) to.v[i] = i < some ? from[i] : T(0);
+}
+template <class T>
+__device__ __forceinline__ void put(T *to, const Values<T> &from, int some, bool wide)
+{
+    constexpr int P = sizeof(T) * EACH > 16 ? 16 / sizeof(T) : EACH;
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < EACH; i += P) *reinterpret_cast<Pack<T, P> *>(to + i) = *reinterpret_cast<const Pack<T, P> *>(from.v + i);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (i < some) to[i] = from.v[i];
+}
+
+// Largest finite magnitude of the 16 lanes of a block.
+__device__ __forceinline__ float block_most(const float (&x)[EACH])
+{
+    float most = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.0f);
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d, 16));
+    return most;
+}
+
+// The tensor of a block, and the block's first value in it.
+__device__ __forceinline__ int find(const Batch &b, int64_t block, int64_t &at)
+{
+    int t = 0, end = b.count;  // the last tensor that begins at the block or before
+    while (end - t > 1) {
+        const int mid = (t + end) / 2;
+        if (b.first[mid] <= block) t = mid;
+        else end = mid;
+    }
+    at = (block - b.first[t]) * VALUES + static_cast<int64_t>(threadIdx.x) * EACH;
+    return t;
+}
+
+template <class G, bool EIGHT>
+__global__ __launch_bounds__(THREADS) void adamw_kernel(const Batch b, const Numbers c)
+{
+    __shared__ float factor[256];
+    if constexpr (EIGHT) {
+        factor[threadIdx.x] = factor_of(threadIdx.x);
+        __syncthreads();
+    }
+    const int64_t blocks = b.first[b.count];
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        int64_t at;
+        const Tensor &t = b.tensor[find(b, block, at)];
+        const int some = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(EACH, t.n - at)));
+        const bool wide = some == EACH && t.wide;
+        if (!EIGHT && some == 0) continue;
+        Values<float> p, m, v;
+        Values<G> g;
+        Values<uint8_t> mc, vc;
+        take(p, t.param + at, some, wide);
+        take(g, static_cast<const G *>(t.grad) + at, some, wide);
+        if constexpr (EIGHT) {
+            take(mc, static_cast<const uint8_t *>(t.m) + at, some, wide);
+            take(vc, static_cast<const uint8_t *>(t.v) + at, some, wide);
+            const int ms = some ? t.m_scale[at / HEAD_BLOCK] : 0, vs = some ? t.v_scale[at / HEAD_BLOCK] : 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                m.v[i] = decode(mc.v[i], ms);
+                v.v[i] = decode(vc.v[i], vs);
+                v.v[i] *= v.v[i];
+            }
+        } else {
+            take(m, static_cast<const float *>(t.m) + at, some, wide);
+            take(v, static_cast<const float *>(t.v) + at, some, wide);
+        }
+        Values<bf16> copy;
+        float root[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const float x = widen(g.v[i]);
+            // products and sums rounded one by one, as the formula has them: 8-bit states then round the same way wherever the
+            // step is computed in float32
+            m.v[i] = c.beta1 * m.v[i] + c.rest1 * x;
+            v.v[i] = c.beta2 * v.v[i] + c.rest2 * x * x;
+            root[i] = sqrtf(v.v[i]);
+            p.v[i] = p.v[i] * c.keep - c.rate * m.v[i] / (root[i] * c.root + c.eps);
+            copy.v[i] = narrow<bf16>(p.v[i]);
+        }
+        put(t.param + at, p, some, wide);
+        if (t.copy) put(t.copy + at, copy, some, wide);
+        if constexpr (EIGHT) {
+            const int ms = scale_of(block_most(m.v)), vs = scale_of(block_most(root));
+            const float mf = factor[ms], vf = factor[vs];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const uint64_t place = static_cast<uint64_t>(at) + i;
+                const uint32_t random = hash(static_cast<uint32_t>(place) + t.key + static_cast<uint32_t>(place >> 32) * 0x9E3779B9u);
+                mc.v[i] = static_cast<uint8_t>(encode(m.v[i], ms, mf, random & 0xFFFF, false));
+                vc.v[i] = static_cast<uint8_t>(encode(root[i], vs, vf, random >> 16, true));
+            }
+            put(static_cast<uint8_t *>(t.m) + at, mc, some, wide);
+            put(static_cast<uint8_t *>(t.v) + at, vc, some, wide);
+            if (some && threadIdx.x % 16 == 0) {
+                t.m_scale[at / HEAD_BLOCK] = static_cast<uint8_t>(ms);
+                t.v_scale[at / HEAD_BLOCK] = static_cast<uint8_t>(vs);
+            }
+        } else {
+            put(static_cast<float *>(t.m) + at, m, some, wide);
+            put(static_cast<float *>(t.v) + at, v, some, wide);
+        }
+    }
+}
+
+// `param` and `copy` are where m and v go.
+__global__ __launch_bounds__(THREADS) void adamw_values_kernel(const Batch b)
+{
+    const int64_t blocks = b.first[b.count];
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        int64_t at;
+        const Tensor &t = b.tensor[find(b, block, at)];
+        const int some = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(EACH, t.n - at)));
+        const bool wide = some == EACH && t.wide;
+        if (some == 0) continue;
+        Values<uint8_t> mc, vc;
+        take(mc, static_cast<const uint8_t *>(t.m) + at, some, wide);
+        take(vc, static_cast<const uint8_t *>(t.v) + at, some, wide);
+        const int ms = t.m_scale[at / HEAD_BLOCK], vs = t.v_scale[at / HEAD_BLOCK];
+        Values<bf16> m, v;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            m.v[i] = narrow<bf16>(decode(mc.v[i], ms));
+            const float root = decode(vc.v[i], vs);
+            v.v[i] = narrow<bf16>(root * root);
+        }
+        put(reinterpret_cast<bf16 *>(t.param) + at, m, some, wide);
+        put(t.copy + at, v, some, wide);
+    }
+}
+
+// Launches `kernel` for all tensors that have values, TENSORS at a time.
+template <class Fill, class Launch>
+hipError_t in_batches(int32_t n_tensors, Fill fill, Launch launch)
+{
+    Batch b{};
+    for (int32_t i = 0; i <= n_tensors; ++i) {
+        if (b.count == TENSORS || (i == n_tensors && b.count > 0)) {
+            const int64_t grid = std::min(b.first[b.count], MAX_GRID);
+            launch(b, dim3(static_cast<uint32_t>(grid)));
+            if (const hipError_t e = hipGetLastError()) return e;
+            b.count = 0;
+        }
+        if (i == n_tensors) break;
+        Tensor &t = b.tensor[b.count];
+        fill(i, t);
+        if (t.n == 0) continue;
+        b.first[b.count + 1] = b.first[b.count] + ceil_div(t.n, VALUES);
+        ++b.count;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const head_adamw_rule &rule, const head_adamw_tensor *tensors, int32_t n_tensors, hipStream_t stream)
+{
+    const double step = static_cast<double>(rule.step);
+    const Numbers c{static_cast<float>(rule.beta1), static_cast<float>(1 - rule.beta1), static_cast<float>(rule.beta2),
+                    static_cast<float>(1 - rule.beta2), static_cast<float>(1 - rule.rate * rule.decay),
+                    static_cast<float>(rule.rate / (1 - std::pow(rule.beta1, step))),
+                    static_cast<float>(1 / std::sqrt(1 - std::pow(rule.beta2, step))), static_cast<float>(rule.eps)};
+    const uint32_t key = hash(rule.seed + 0x9E3779B9u * static_cast<uint32_t>(rule.step));
+    return in_batches(
+        n_tensors,
+        [&](int32_t i, Tensor &t) {
+            const head_adamw_tensor &s = tensors[i];
+            t = Tensor{s.param, s.grad, s.m, s.v, s.m_scale, s.v_scale, static_cast<bf16 *>(s.copy), s.n,
+                       hash(key + static_cast<uint32_t>(i)), 0};
+            const uint64_t states = address(s.m) | address(s.v);
+            t.wide = (address(s.param) | address(s.grad) | address(s.copy)) % 16 == 0 && states % (rule.bits == 8 ? EACH : 16) == 0;
+        },
+        [&](const Batch &b, dim3 grid) {
+            const bool narrow_grad = rule.grad_dtype == HEAD_BF16;
+            auto *kernel = rule.bits == 8 ? (narrow_grad ? adamw_kernel<bf16, true> : adamw_kernel<float, true>)
+                                          : (narrow_grad ? adamw_kernel<bf16, false> : adamw_kernel<float, false>);
+            hipLaunchKernelGGL(kernel, grid, dim3(THREADS), 0, stream, b, c);
+        });
+}
+
+hipError_t launch_adamw_values(const head_adamw_tensor *tensors, void *const *out_m, void *const *out_v, int32_t n_tensors,
+                               hipStream_t stream)
+{
+    return in_batches(
+        n_tensors,
+        [&](int32_t i, Tensor &t) {
+            const head_adamw_tensor &s = tensors[i];
+            t = Tensor{static_cast<float *>(out_m[i]), nullptr, s.m, s.v, s.m_scale, s.v_scale, static_cast<bf16 *>(out_v[i]), s.n, 0, 0};
+            t.wide = (address(s.m) | address(s.v)) % EACH == 0 && (address(out_m[i]) | address(out_v[i])) % 16 == 0;
+        },
+        [&](const Batch &b, dim3 grid) { hipLaunchKernelGGL(adamw_values_kernel, grid, dim3(THREADS), 0, stream, b); });
+}
+
+}  // namespace head_impl

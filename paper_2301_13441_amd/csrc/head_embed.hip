@@ -1,0 +1,481 @@
+// Sums of embedding vectors over a row's ids, and their gradient by sorted ids, on gfx950.
+//
+//     out[r] = scale * sum_t table[id(r, t) + offset[t]]
+//     grad_table[v] = scale * sum of grad[r] over all (r, t) whose vector is v
+//
+// Forward: a vector of `dim` values is read by a group of lanes, a piece of up to 16 bytes each; groups that share a row
+// (a wavefront's, or a workgroup's where rows are few) take its ids in turn and add up their sums at the end.
+//
+// Backward: (vector, row) pairs, one for each id, are sorted by vector with a stable radix sort, 8 bits a pass: counts of
+// each digit by tile, sums over the tiles, then each tile moves its pairs to their places.  The sorted list is cut into
+// chunks of equal length whatever vectors they hold, so that a vector that every row has costs no more than others; a group
+// of lanes adds up a chunk, run after run of equal vectors.  A run inside a chunk is a vector's gradient.  Of runs that cross
+// chunks the parts go to the workspace, and a second kernel adds up the parts of each.  No atomics on values: the order
+// of every sum is fixed by the ids alone.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "head_device.hpp"
+
+namespace head_impl {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int64_t MAX_GRID = 1 << 22;  // workgroups of a launch: 2^30 threads, a grid's axis has room for 2^32
+
+struct Ids {
+    const int32_t *id;
+    const int64_t *offset;
+    int64_t stride, n_vectors;
+    int64_t n_ids;
+};
+
+// The vector that id t of a row stands for; -1: none.
+__device__ __forceinline__ int64_t vector_of(const Ids &s, const int32_t *row, int64_t t)
+{
+    const int32_t id = row[t];
+    const int64_t v = id + (s.offset ? s.offset[t] : 0);
+    return id >= 0 && v >= 0 && v < s.n_vectors ? v : -1;
+}
+
+// `lanes` lanes of a group read a vector; `team` groups share a row.
+template <class T, int V>
+__global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Ids s, const T *table, int64_t table_stride, float scale,
+                                                     T *out, int lanes, int team)
+{
+    extern __shared__ float sums[];  // [groups][lanes * V], where a row's groups are in several wavefronts
+    const int group = threadIdx.x / lanes, lane = threadIdx.x % lanes, groups = blockDim.x / lanes;
+    const int rows = groups / team, member = group % team;
+    const int c = (blockIdx.y * lanes + lane) * V;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * rows; first < n_rows; first += static_cast<int64_t>(gridDim.x) * rows) {
+        const int64_t row = first + group / team;
+        float a[V] = {};
+        if (row < n_rows && c < dim) {
+            const int32_t *ids = s.id + row * s.stride;
+#pragma unroll 8
+            for (int64_t t = member; t < s.n_ids; t += team) {
+                const int64_t v = vector_of(s, ids, t);
+                if (v >= 0) {
+                    const Pack<T, V> p = *reinterpret_cast<const Pack<T, V> *>(table + v * table_stride + c);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) a[k] += widen(p.v[k]);
+                }
+            }
+        }
+        if (team > 1) {
+            const int in_wave = std::min(team, 64 / lanes);
+            for (int d = lanes; d < lanes * in_wave; d *= 2)
+#pragma unroll
+                for (int k = 0; k < V; ++k) a[k] += __shfl_xor(a[k], d, 64);
+            if (team > in_wave) {
+                __syncthreads();  // who still reads the last row's
+                if (threadIdx.x % 64 < lanes)
+#pragma unroll
+                    for (int k = 0; k < V; ++k) sums[(threadIdx.x / 64 * lanes + lane) * V + k] = a[k];
+                __syncthreads();
+                const int waves = team / in_wave, from = threadIdx.x / 64 / waves * waves;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    a[k] = 0;
+                    for (int w = 0; w < waves; ++w) a[k] += sums[((from + w) * lanes + lane) * V + k];
+                }
+            }
+        }
+        if (member == 0 && row < n_rows && c < dim) {
+            Pack<T, V> p;
+#pragma unroll
+            for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[k]);
+            *reinterpret_cast<Pack<T, V> *>(out + row * dim + c) = p;
+        }
+    }
+}
+
+// ---- the sort
+
+constexpr int DIGIT = 8, DIGITS = 1 << DIGIT;
+constexpr int ITEMS = 16;                // pairs of a lane
+constexpr int TILE = THREADS * ITEMS;    // pairs of a workgroup
+constexpr int WAVES = THREADS / 64;
+
+// Where pairs come from: the ids of the batch on the first pass, the last pass's output on the others.
+struct Pairs {
+    Ids s;
+    const uint32_t *key, *row;   // null on the first pass
+    uint32_t n;
+    uint32_t n_ids, magic, shift;  // division by n_ids of a number below 2^31
+};
+
+__device__ __forceinline__ uint32_t row_of(const Pairs &p, uint32_t i)
+{
+    return p.n_ids == 1 ? i : __umulhi(i, p.magic) >> p.shift;
+}
+// An id that stands for no vector sorts behind all that do.
+__device__ __forceinline__ uint32_t key_of(const Pairs &p, uint32_t i, uint32_t row)
+{
+    if (p.key) return p.key[i];
+    const int64_t v = vector_of(p.s, p.s.id + row * p.s.stride, i - row * p.n_ids);
+    return static_cast<uint32_t>(v < 0 ? p.s.n_vectors : v);
+}
+
+__global__ __launch_bounds__(THREADS) void count_kernel(Pairs p, int bit, uint32_t n_tiles, uint32_t *counts)
+{
+    __shared__ uint32_t count[DIGITS];
+    count[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t first = blockIdx.x * TILE + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const uint32_t i = first + k * THREADS;
+        if (i < p.n) atomicAdd(&count[key_of(p, i, p.key ? 0 : row_of(p, i)) >> bit & (DIGITS - 1)], 1u);
+    }
+    __syncthreads();
+    counts[threadIdx.x * n_tiles + blockIdx.x] = count[threadIdx.x];
+}
+
+// Sum of v over the lanes before this one of the workgroup; `all`: over the whole workgroup.
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t &all, uint32_t *lds)
+{
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = __shfl_up(s, d, 64);
+        if (static_cast<int>(threadIdx.x % 64) >= d) s += o;
+    }
+    __syncthreads();
+    if (threadIdx.x % 64 == 63) lds[threadIdx.x / 64] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < static_cast<int>(threadIdx.x / 64)) before += lds[w];
+        all += lds[w];
+    }
+    return before + s - v;
+}
+
+// A workgroup for each digit: its counts become sums over the tiles before, and the digit's total goes behind them.
+__global__ __launch_bounds__(THREADS) void tiles_kernel(uint32_t n_tiles, uint32_t *counts, uint32_t *totals)
+{
+    __shared__ uint32_t lds[WAVES];
+    uint32_t *row = counts + static_cast<int64_t>(blockIdx.x) * n_tiles, sum = 0;
+    for (uint32_t first = 0; first < n_tiles; first += THREADS) {
+        const uint32_t i = first + threadIdx.x;
+        uint32_t all;
+        const uint32_t before = sum_before(i < n_tiles ? row[i] : 0, all, lds);
+        if (i < n_tiles) row[i] = sum + before;
+        sum += all;
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = sum;
+}
+
+// A wavefront's LDS accesses before are made before its accesses after, its lanes' of each other's words too.
+__device__ __forceinline__ void in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__global__ __launch_bounds__(THREADS) void move_kernel(Pairs p, int bit, uint32_t n_tiles, const uint32_t *counts, const uint32_t *totals,
+                                                       uint32_t *key_out, uint32_t *row_out)
+{
+    __shared__ uint32_t place[WAVES][DIGITS];  // where a wavefront's next pair of a digit goes
+    __shared__ uint32_t lds[WAVES];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) place[w][threadIdx.x] = 0;
+    __syncthreads();
+    // A wavefront has ITEMS * 64 adjacent pairs, 64 at a time.
+    const uint32_t first = blockIdx.x * TILE + wave * (ITEMS * 64) + lane;
+    uint32_t key[ITEMS], row[ITEMS];
+    uint16_t before[ITEMS];  // pairs of the same digit that the wavefront had before
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const uint32_t i = first + k * 64;
+        const bool here = i < p.n;
+        row[k] = here ? (p.key ? p.row[i] : row_of(p, i)) : 0;
+        key[k] = here ? key_of(p, i, row[k]) : 0;
+        const uint32_t digit = key[k] >> bit & (DIGITS - 1);
+        uint64_t same = __ballot(here);
+#pragma unroll
+        for (int j = 0; j < DIGIT; ++j) {
+            const uint64_t set = __ballot(digit >> j & 1);
+            same &= digit >> j & 1 ? set : ~set;
+        }
+        const int ahead = __popcll(same & ((1ull << lane) - 1));
+        uint32_t had = 0;
+        if (here) had = place[wave][digit];
+        in_order();  // all have read before the first lane of each digit writes
+        if (here && ahead == 0) place[wave][digit] = had + __popcll(same);
+        in_order();
+        before[k] = static_cast<uint16_t>(had + ahead);
+    }
+    __syncthreads();
+    {   // lane = digit: the places of the wavefronts one after the other, from the digit's and the tile's
+        uint32_t all;
+        uint32_t at = sum_before(totals[threadIdx.x], all, lds) + counts[threadIdx.x * n_tiles + blockIdx.x];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const uint32_t had = place[w][threadIdx.x];
+            place[w][threadIdx.x] = at;
+            at += had;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+        if (first + k * 64 < p.n) {
+            const uint32_t to = place[wave][key[k] >> bit & (DIGITS - 1)] + before[k];
+            key_out[to] = key[k];
+            row_out[to] = row[k];
+        }
+}
+
+// ---- the sums
+
+template <class T>
+__global__ __launch_bounds__(THREADS) void zero_kernel(T *to, int64_t n)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int64_t lanes = static_cast<int64_t>(gridDim.x) * THREADS, lane = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x;
+    const int64_t head = std::min<int64_t>(n, (16 - reinterpret_cast<uintptr_t>(to) % 16) % 16 / sizeof(T));
+    const int64_t whole = (n - head) / V;
+    for (int64_t i = lane; i < whole; i += lanes) reinterpret_cast<Pack<T, V> *>(to + head)[i] = Pack<T, V>{};
+    if (lane < head) to[lane] = T(0);
+    if (lane < n - head - whole * V) to[head + whole * V + lane] = T(0);
+}
+
+struct Sorted {
+    const uint32_t *key, *row;
+    uint32_t n, n_vectors;  // pairs whose key is n_vectors stand for nothing
+    uint32_t chunk, n_chunks;
+};
+
+// A group of `lanes` lanes adds up a chunk.  parts: [2 * chunk's number][dim], the part of the run that it begins in the
+// midst of, then the part of the run that it ends in the midst of.
+template <class T, int V>
+__global__ __launch_bounds__(THREADS) void sum_kernel(Sorted s, int dim, const T *grad, int64_t grad_stride, float scale, T *out,
+                                                      float *parts, int lanes)
+{
+    const uint32_t group = (blockIdx.x * THREADS + threadIdx.x) / lanes;
+    const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * V;
+    if (group >= s.n_chunks || c >= dim) return;
+    const uint32_t first = group * s.chunk, end = std::min(s.n, first + s.chunk);
+    uint32_t key = s.key[first];
+    if (key >= s.n_vectors) return;
+    bool begun = first > 0 && s.key[first - 1] == key;  // before this chunk
+    float a[V] = {};
+    auto store = [&](bool ends) {
+        if (begun || !ends) {
+            float *to = parts + (2 * static_cast<int64_t>(group) + (begun ? 0 : 1)) * dim + c;
+            Pack<float, V> p;
+#pragma unroll
+            for (int k = 0; k < V; ++k) p.v[k] = a[k];
+#pragma unroll
+            for (int k = 0; k < V; ++k) to[k] = p.v[k];
+        } else {
+            Pack<T, V> p;
+#pragma unroll
+            for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[k]);
+            *reinterpret_cast<Pack<T, V> *>(out + static_cast<int64_t>(key) * dim + c) = p;
+        }
+    };
+    constexpr int AHEAD = 8;
+    for (uint32_t i = first; i < end; i += AHEAD) {
+        uint32_t keys[AHEAD];
+        Pack<T, V> p[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) keys[j] = i + j < end ? s.key[i + j] : s.n_vectors;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const uint32_t row = keys[j] < s.n_vectors ? s.row[i + j] : 0;
+            p[j] = *reinterpret_cast<const Pack<T, V> *>(grad + row * grad_stride + c);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (keys[j] >= s.n_vectors) break;
+            if (keys[j] != key) {
+                store(true);
+                key = keys[j];
+                begun = false;
+#pragma unroll
+                for (int k = 0; k < V; ++k) a[k] = 0;
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) a[k] += widen(p[j].v[k]);
+        }
+    }
+    store(end == s.n || s.key[end] != key);
+}
+
+// A group of lanes for each chunk: if a run begins in the chunk and goes on, all its parts.
+template <class T, int V>
+__global__ __launch_bounds__(THREADS) void join_kernel(Sorted s, int dim, const float *parts, float scale, T *out, int lanes)
+{
+    const uint32_t group = (blockIdx.x * THREADS + threadIdx.x) / lanes;
+    const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * V;
+    if (group + 1 >= s.n_chunks || c >= dim) return;  // no run goes on from the last chunk
+    const uint32_t first = group * s.chunk, end = first + s.chunk;
+    const uint32_t key = s.key[end - 1];
+    if (key >= s.n_vectors || s.key[end] != key) return;
+    if (s.key[first] == key && first > 0 && s.key[first - 1] == key) return;
+    float a[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) a[k] = parts[(2 * static_cast<int64_t>(group) + 1) * dim + c + k];
+    for (uint32_t g = group + 1; g < s.n_chunks && s.key[g * s.chunk] == key; ++g)
+#pragma unroll
+        for (int k = 0; k < V; ++k) a[k] += parts[2 * static_cast<int64_t>(g) * dim + c + k];
+    Pack<T, V> p;
+#pragma unroll
+    for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[k]);
+    *reinterpret_cast<Pack<T, V> *>(out + static_cast<int64_t>(key) * dim + c) = p;
+}
+
+// ---- what a call launches
+
+template <class T, class F>
+hipError_t by_piece(int wide, F f)
+{
+    switch (wide) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 4: return f(std::integral_constant<int, 4>());
+        default:
+            if constexpr (sizeof(T) == 2) return f(std::integral_constant<int, 8>());
+            return hipErrorInvalidValue;
+    }
+}
+
+int power_at_least(int64_t n, int most)
+{
+    int p = 1;
+    while (p < n && p < most) p *= 2;
+    return p;
+}
+
+template <class T>
+hipError_t embed(const head_ids &ids, int64_t dim, const T *table, int64_t table_stride, float scale, T *out, hipStream_t stream)
+{
+    const uint64_t bits = address(table) | address(out) | static_cast<uint64_t>(table_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));
+    const Ids s{ids.ids, ids.offset, ids.ids_stride, ids.n_vectors, ids.n_ids};
+    return by_piece<T>(piece(bits, sizeof(T)), [&](auto V) {
+        const int lanes = power_at_least(ceil_div(dim, V()), 64), in_wave = 64 / lanes;
+        // a group for each row, a wavefront's groups, or a workgroup's
+        const bool few = ids.n_rows <= 1024 && ids.n_ids >= 4 * in_wave;
+        const int threads = few ? 1024 : THREADS;
+        const int team = few ? threads / lanes : ids.n_ids >= 4 * in_wave ? in_wave : 1;
+        const int64_t rows = threads / lanes / team;
+        const size_t bytes = team > in_wave ? static_cast<size_t>(threads / 64) * lanes * V() * sizeof(float) : 0;
+        const dim3 grid(static_cast<uint32_t>(std::min(ceil_div(ids.n_rows, rows), MAX_GRID / (threads / THREADS))),
+                        static_cast<uint32_t>(ceil_div(dim, static_cast<int64_t>(lanes) * V())));
+        hipLaunchKernelGGL((embed_kernel<T, V()>), grid, dim3(threads), bytes, stream, ids.n_rows, static_cast<int>(dim), s, table,
+                           table_stride, scale, out, lanes, team);
+        return hipGetLastError();
+    });
+}
+
+// The parts of the workspace of the backward pass, in bytes from its start.
+struct GradPlan {
+    uint32_t n, n_tiles, chunk, n_chunks;
+    int passes;
+    int64_t key[2], row[2], counts, totals, parts, bytes;
+};
+
+GradPlan plan_grad(const head_ids &ids, int64_t dim)
+{
+    GradPlan p{};
+    p.n = static_cast<uint32_t>(ids.n_rows * ids.n_ids);
+    p.n_tiles = static_cast<uint32_t>(ceil_div(p.n, TILE));
+    p.passes = 1;
+    while (ids.n_vectors >> (DIGIT * p.passes)) ++p.passes;
+    p.chunk = 64;
+    p.n_chunks = static_cast<uint32_t>(ceil_div(p.n, p.chunk));
+    int64_t at = 0;
+    auto part = [&](int64_t bytes) {
+        const int64_t from = at;
+        at += round_up(bytes, 256);
+        return from;
+    };
+    for (int k = 0; k < 2; ++k) {
+        p.key[k] = part(int64_t{4} * p.n);
+        p.row[k] = part(int64_t{4} * p.n);
+    }
+    p.counts = part(int64_t{4} * DIGITS * p.n_tiles);
+    p.totals = part(4 * DIGITS);
+    p.parts = part(int64_t{8} * p.n_chunks * dim);
+    p.bytes = p.n ? at : 0;
+    return p;
+}
+
+template <class T>
+hipError_t embed_grad(const head_ids &ids, int64_t dim, const T *grad, int64_t grad_stride, float scale, T *out, char *workspace,
+                      hipStream_t stream)
+{
+    const int64_t values = ids.n_vectors * dim;
+    hipLaunchKernelGGL((zero_kernel<T>), dim3(static_cast<uint32_t>(std::min<int64_t>(ceil_div(values, THREADS * 16), 8192))), dim3(THREADS), 0,
+                       stream, out, values);
+    if (const hipError_t e = hipGetLastError()) return e;
+    const GradPlan plan = plan_grad(ids, dim);
+    if (plan.n == 0) return hipSuccess;
+    auto words = [&](int64_t at) { return reinterpret_cast<uint32_t *>(workspace + at); };
+    Pairs p{};
+    p.s = Ids{ids.ids, ids.offset, ids.ids_stride, ids.n_vectors, ids.n_ids};
+    p.n = plan.n;
+    p.n_ids = static_cast<uint32_t>(ids.n_ids);
+    if (p.n_ids > 1) {  // 2^(31 + k) / n_ids, rounded up, is exact for numbers below 2^31 where 2^k >= n_ids
+        int k = 0;
+        while ((uint64_t{1} << k) < p.n_ids) ++k;
+        p.magic = static_cast<uint32_t>((uint64_t{1} << (31 + k)) / p.n_ids + 1);
+        p.shift = static_cast<uint32_t>(k - 1);
+    }
+    for (int pass = 0; pass < plan.passes; ++pass) {
+        if (pass > 0) {
+            p.key = words(plan.key[(pass - 1) % 2]);
+            p.row = words(plan.row[(pass - 1) % 2]);
+        }
+        hipLaunchKernelGGL(count_kernel, dim3(plan.n_tiles), dim3(THREADS), 0, stream, p, pass * DIGIT, plan.n_tiles, words(plan.counts));
+        hipLaunchKernelGGL(tiles_kernel, dim3(DIGITS), dim3(THREADS), 0, stream, plan.n_tiles, words(plan.counts), words(plan.totals));
+        hipLaunchKernelGGL(move_kernel, dim3(plan.n_tiles), dim3(THREADS), 0, stream, p, pass * DIGIT, plan.n_tiles, words(plan.counts),
+                           words(plan.totals), words(plan.key[pass % 2]), words(plan.row[pass % 2]));
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    const int last = (plan.passes - 1) % 2;
+    const Sorted s{words(plan.key[last]), words(plan.row[last]), plan.n, static_cast<uint32_t>(ids.n_vectors), plan.chunk, plan.n_chunks};
+    float *parts = reinterpret_cast<float *>(workspace + plan.parts);
+    const uint64_t bits = address(grad) | address(out) | static_cast<uint64_t>(grad_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));
+    return by_piece<T>(piece(bits, sizeof(T)), [&](auto V) {
+        const int lanes = power_at_least(ceil_div(dim, V()), 64);
+        const dim3 grid(static_cast<uint32_t>(ceil_div(static_cast<int64_t>(plan.n_chunks) * lanes, THREADS)),
+                        static_cast<uint32_t>(ceil_div(dim, static_cast<int64_t>(lanes) * V())));
+        hipLaunchKernelGGL((sum_kernel<T, V()>), grid, dim3(THREADS), 0, stream, s, static_cast<int>(dim), grad, grad_stride, scale, out,
+                           parts, lanes);
+        hipLaunchKernelGGL((join_kernel<T, V()>), grid, dim3(THREADS), 0, stream, s, static_cast<int>(dim), parts, scale, out, lanes);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+hipError_t launch_embed(const head_ids &ids, int32_t dtype, int64_t dim, const void *table, int64_t table_stride, float scale,
+                        void *out, hipStream_t stream)
+{
+    if (dtype == HEAD_BF16)
+        return embed(ids, dim, static_cast<const bf16 *>(table), table_stride, scale, static_cast<bf16 *>(out), stream);
+    return embed(ids, dim, static_cast<const float *>(table), table_stride, scale, static_cast<float *>(out), stream);
+}
+
+int64_t embed_grad_bytes(const head_ids &ids, int32_t, int64_t dim) { return plan_grad(ids, dim).bytes; }
+
+hipError_t launch_embed_grad(const head_ids &ids, int32_t dtype, int64_t dim, const void *grad, int64_t grad_stride, float scale,
+                             void *grad_table, void *workspace, hipStream_t stream)
+{
+    if (dtype == HEAD_BF16)
+        return embed_grad(ids, dim, static_cast<const bf16 *>(grad), grad_stride, scale, static_cast<bf16 *>(grad_table),
+                          static_cast<char *>(workspace), stream);
+    return embed_grad(ids, dim, static_cast<const float *>(grad), grad_stride, scale, static_cast<float *>(grad_table),
+                      static_cast<char *>(workspace), stream);
+}
+
+}  // namespace head_impl
