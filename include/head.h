@@ -44,6 +44,7 @@ enum {
 #define HEAD_MAX_VECTORS 1000000000  /* n_vectors, n_classes */
 #define HEAD_MAX_IDS 2147483647      /* n_ids */
 #define HEAD_MAX_TOKENS 2147483647   /* n_rows * n_ids, of head_embed_grad */
+#define HEAD_MAX_LOGITS (INT64_C(1) << 44) /* n_rows * n_classes */
 #define HEAD_MAX_TENSORS 1000000     /* tensors of one head_adamw call */
 #define HEAD_BLOCK 128               /* values that share a scale byte in the 8-bit states */
 

@@ -57,7 +57,8 @@ int check_classes(const head_classes *c)
 {
     if (!c || c->n_classes < 1) return HEAD_EINVAL;
     if (int rc = check_shape(c->dtype, c->n_rows, c->dim)) return rc;
-    return c->n_classes > HEAD_MAX_VECTORS ? HEAD_ELIMIT : HEAD_OK;
+    if (c->n_classes > HEAD_MAX_VECTORS || (c->n_rows > 0 && c->n_classes > HEAD_MAX_LOGITS / c->n_rows)) return HEAD_ELIMIT;
+    return HEAD_OK;
 }
 
 int check_class_pointers(const head_classes &c)

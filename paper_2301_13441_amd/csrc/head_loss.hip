@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "head_device.hpp"
@@ -23,7 +24,6 @@
 namespace head_impl {
 namespace {
 
-constexpr int64_t MAX_GRID = 1 << 22;
 constexpr int STEP = 128;                       // bytes of the sum's axis in a tile
 constexpr int64_t PIECE_BYTES = int64_t{1} << 30;  // of p in the workspace, where rows are not too many for that
 
@@ -35,11 +35,8 @@ __device__ const Chunk g_zeros[1] = {};
 
 using GlobalChunk = const __attribute__((address_space(1))) void *;
 using LdsChunk = __attribute__((address_space(3))) void *;
-
-__device__ __forceinline__ void to_lds(const void *from, char *to)  // 16 bytes a lane, the wavefront's 1024 adjacent
-{
-    __builtin_amdgcn_global_load_lds((GlobalChunk)(from), (LdsChunk)(to), 16, 0, 0);
-}
+using Half = short __attribute__((ext_vector_type(4)));  // of a chunk
+using LdsHalf = __attribute__((address_space(3))) Half *;
 
 // An operand: `rows` along the result's axis, `depth` along the sum's.
 template <class T>
@@ -49,47 +46,90 @@ struct Operand {
     int64_t rows, depth;
 };
 
-// Tiles of ROWS x 128 bytes of an operand.  ALONG: the sum's axis lies along memory; row r's chunk c of 16 bytes is in slot
-// c ^ (r / SPREAD % 8), so that the 8 lanes that read the same chunk of 8 rows SPREAD apart meet 8 different bank groups.
-// Otherwise a row of the tile holds the ROWS values of one index of the sum.
-template <class T, bool ALONG, int ROWS, int THREADS, int SPREAD>
+// Tiles of ROWS x 128 bytes of an operand, brought to LDS by THREADS lanes, 16 bytes each at a time.
+// ALONG: the sum's axis lies along memory.  Row r of the tile is STEP bytes, its chunk c of 16 bytes in slot c ^ key(r): the
+// 16 lanes that are served at once read the same chunk of 16 rows, which so lie in 16 different groups of four banks.  Rows are
+// those of memory in another order where a lane of a matrix instruction is to have NT adjacent ones: row nt * 32 + l of every
+// NT * 32 is the one NT * l + nt in memory.
+// Otherwise a row of the tile holds the ROWS values of one index of the sum, its chunk c in slot c ^ key(index): bfloat16 values
+// are read by the instruction that transposes 4 x 16 of them, 16 lanes 32 bytes of each of 4 rows, and 32 lanes are served at
+// once; float32 ones one by one, 32 adjacent ones of each of two rows.
+template <class T, bool ALONG, int ROWS, int THREADS, int NT>
 struct Tile {
     static constexpr int VALUES = 16 / sizeof(T), DEPTH = STEP / sizeof(T), BYTES = ROWS * STEP;
-    static constexpr int LOADS = BYTES / (THREADS * 16);
+    static constexpr int LOADS = BYTES / (THREADS * 16), WAVES = THREADS / 64;
+    static constexpr int CHUNKS = ROWS / VALUES;  // of a row of the tile that lies across
+    static constexpr int SLOTS = STEP / 16;       // of a row of one that lies along
 
-    static __device__ __forceinline__ void load(const Operand<T> &o, int64_t row0, int64_t depth0, char *lds)
+    static __device__ __forceinline__ int key(int r)
     {
-        const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        if constexpr (ALONG) return r / (256 / STEP) % SLOTS;
+        return sizeof(T) == 2 ? r % 4 * 4 : r / 4 % 2 * 8;
+    }
+
+    const T *from[LOADS];  // this lane's chunks at depth 0; rows past the end are the last one again, of whose results nobody reads
+    int at[LOADS];         // their indexes of the sum, in the tile
+
+    __device__ __forceinline__ void aim(const Operand<T> &o, int64_t row0)
+    {
+        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int part = j * (THREADS / 64) + wave;  // 1024 bytes of the tile
-            const void *from = g_zeros;
+            const int part = j * WAVES + wave;  // 1024 bytes of the tile
             if constexpr (ALONG) {
-                const int r = part * 8 + lane / 8;
-                const int chunk = (lane % 8) ^ (r / SPREAD % 8);
-                const int64_t row = std::min(row0 + r, o.rows - 1), k = depth0 + chunk * VALUES;
-                if (k < o.depth) from = o.at + row * o.stride + k;
+                const int r = part * (64 / SLOTS) + lane / SLOTS, in = r % (NT * 32);
+                const int64_t row = row0 + r - in + in % 32 * NT + in / 32;
+                at[j] = ((lane % SLOTS) ^ key(r)) * VALUES;
+                from[j] = o.at + std::min(row, o.rows - 1) * o.stride + at[j];
             } else {
-                constexpr int CHUNKS = ROWS / VALUES;  // of a row of the tile
-                const int64_t k = depth0 + (part * 64 + lane) / CHUNKS, row = row0 + (part * 64 + lane) % CHUNKS * VALUES;
-                if (k < o.depth && row < o.rows) from = o.at + k * o.stride + row;
+                at[j] = (part * 64 + lane) / CHUNKS;
+                const int64_t row = row0 + ((part * 64 + lane) % CHUNKS ^ key(at[j])) * VALUES;
+                from[j] = o.at + at[j] * o.stride + std::min(row, (o.rows - 1) / VALUES * VALUES);
             }
-            to_lds(from, lds + part * 1024);
         }
     }
 
-    // What lane `lane` holds of 32 rows in a matrix instruction: of row r (its own, lane % 32's), the values of chunk
+    __device__ __forceinline__ void load(const Operand<T> &o, int64_t depth, char *lds) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const int64_t ahead = ALONG ? depth : depth * o.stride;
+        auto chunk = [&](int j, const void *p) {
+            __builtin_amdgcn_global_load_lds((GlobalChunk)(p), (LdsChunk)(lds + (j * WAVES + wave) * 1024), 16, 0, 0);
+        };
+        if (depth + DEPTH <= o.depth) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) chunk(j, from[j] + ahead);
+        } else {  // the last one: zeros past the end of the sum
+            const int left = static_cast<int>(o.depth - depth);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) chunk(j, at[j] < left ? static_cast<const void *>(from[j] + ahead) : g_zeros);
+        }
+    }
+
+    // What a lane holds of 32 rows in a matrix instruction: of row r (the first of them + lane % 32) the values of chunk
     // 2 * kk + lane / 32.
     static __device__ __forceinline__ Chunk read(const char *lds, int r, int kk)
     {
         const int chunk = 2 * kk + threadIdx.x % 64 / 32;
         if constexpr (ALONG) {
-            return *reinterpret_cast<const Chunk *>(lds + r * STEP + ((chunk ^ (r / SPREAD % 8)) * 16));
+            return *reinterpret_cast<const Chunk *>(lds + r * STEP + ((chunk ^ key(r)) * 16));
+        } else if constexpr (sizeof(T) == 2) {
+            // lane i of 16 reads 4 values of row i / 4 and gets those of column i, of 4 rows
+            const int i = threadIdx.x % 16, depth = chunk * VALUES + i / 4;
+            const int in = r / 32 * 32 + threadIdx.x % 32 / 16 * 16 + i % 4 * 4;
+            const char *at = lds + depth * (ROWS * 2) + (in / VALUES ^ key(depth)) * 16 + in % VALUES * 2;
+            Half h[2];
+            h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalf)(at));
+            h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalf)(at + 4 * ROWS * 2));
+            return *reinterpret_cast<Chunk *>(h);
         } else {
-            Pack<T, VALUES> p;
+            Chunk p;
 #pragma unroll
-            for (int j = 0; j < VALUES; ++j) p.v[j] = reinterpret_cast<const T *>(lds)[(chunk * VALUES + j) * ROWS + r];
-            return *reinterpret_cast<Chunk *>(&p);
+            for (int j = 0; j < VALUES; ++j) {
+                const int depth = chunk * VALUES + j;
+                p[j] = reinterpret_cast<const float *>(lds)[depth * ROWS + (r / VALUES ^ key(depth)) * VALUES + r % VALUES];
+            }
+            return p;
         }
     }
 };
@@ -125,55 +165,109 @@ struct Shape {
     }
 };
 
-// c = A[row0.., depth0..depth1) B[.., column0..): A and B of 2 * (S::M + S::N) * STEP bytes of LDS.
+// The products of a workgroup's tiles, one after the other: tile of C = A[row0.., depth0..depth1) B[.., column0..).  While the
+// matrix core works on one step's tiles of A and B the next step's are on their way to the other half of LDS, the next
+// tile's first ones while it works on a tile's last ones and while that tile is finished.
 template <class T, class S, bool A_ALONG, bool B_ALONG>
-__device__ __forceinline__ void product(const Operand<T> &a, const Operand<T> &b, int64_t row0, int64_t column0, int64_t depth0,
-                                        int64_t depth1, char *lds, Acc (&c)[S::MT][S::NT])
-{
+struct Products {
     using A = Tile<T, A_ALONG, S::M, S::THREADS, 1>;
     using B = Tile<T, B_ALONG, S::N, S::THREADS, S::NEXT ? S::NT : 1>;
-    constexpr int BYTES = A::BYTES + B::BYTES;
+    static_assert(B_ALONG || !S::NEXT, "rows of a tile that lies across stay in order");
+    static constexpr int BYTES = A::BYTES + B::BYTES;  // of a step; LDS holds two
+
+    const Operand<T> &a, &b;
+    char *lds;
+    A ta;
+    B tb;
+    int64_t depth0;
+    int steps = 0, step = 0, half = 0;
+
+    __device__ __forceinline__ Products(const Operand<T> &a_, const Operand<T> &b_, char *lds_) : a(a_), b(b_), lds(lds_) {}
+
+    __device__ __forceinline__ void load() const
+    {
+        const int64_t depth = depth0 + step * int64_t{A::DEPTH};
+        ta.load(a, depth, lds + half * BYTES);
+        tb.load(b, depth, lds + half * BYTES + A::BYTES);
+    }
+
+    // Begins a tile.  Tiles begin at different steps (turn), so that workgroups side by side, whose rows may lie a power of
+    // two apart, do not ask for the same few of the memory's channels at the same time.
+    __device__ __forceinline__ void aim(int64_t row0, int64_t column0, int64_t from, int64_t to, uint32_t turn)
+    {
+        ta.aim(a, row0);
+        tb.aim(b, column0);
+        depth0 = from;
+        steps = from < to ? static_cast<int>((to - from + A::DEPTH - 1) / A::DEPTH) : 0;
+        step = steps ? static_cast<int>(turn % static_cast<uint32_t>(steps)) : 0;
+        if (steps) load();
+    }
+
+    // The product that aim() began; next() is called once, to begin the one after it.
+    template <class Next>
+    __device__ __forceinline__ void run(Acc (&c)[S::MT][S::NT], Next next)
+    {
 #pragma unroll
-    for (int mt = 0; mt < S::MT; ++mt)
+        for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < S::NT; ++nt) c[mt][nt] = Acc{};
-    auto load = [&](int64_t depth, int which) {
-        A::load(a, row0, depth, lds + which * BYTES);
-        B::load(b, column0, depth, lds + which * BYTES + A::BYTES);
-    };
-    __syncthreads();  // who still reads what LDS held before
-    if (depth0 < depth1) load(depth0, 0);
-    int which = 0;
-    for (int64_t depth = depth0; depth < depth1; depth += A::DEPTH, which ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();  // this step's tiles are there, and nobody reads the other ones any more
-        if (depth + A::DEPTH < depth1) load(depth + A::DEPTH, which ^ 1);
-        const char *la = lds + which * BYTES, *lb = la + A::BYTES;
+            for (int nt = 0; nt < S::NT; ++nt) c[mt][nt] = Acc{};
+        if (steps == 0) return next();
+        const int count = steps;
+        for (int done = 1; done <= count; ++done) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();  // this step's tiles are there, and nobody reads the other half any more
+            const char *la = lds + half * BYTES, *lb = la + A::BYTES;
+            half ^= 1;
+            if (done < count) {
+                step = step + 1 < count ? step + 1 : 0;
+                load();
+            } else next();
+            // the next 32 bytes of the sum's axis are read while the matrix core has the last ones; more would fill the registers
+            Chunk x[2][S::MT], y[2][S::NT];
+            auto read = [&](int kk) {
 #pragma unroll
-        for (int kk = 0; kk < STEP / 32; ++kk) {
-            Chunk x[S::MT], y[S::NT];
+                for (int mt = 0; mt < S::MT; ++mt) x[kk % 2][mt] = A::read(la, S::wave_m() * (S::MT * 32) + mt * 32 + threadIdx.x % 32, kk);
 #pragma unroll
-            for (int mt = 0; mt < S::MT; ++mt) x[mt] = A::read(la, S::wave_m() * (S::MT * 32) + mt * 32 + threadIdx.x % 32, kk);
+                for (int nt = 0; nt < S::NT; ++nt) y[kk % 2][nt] = B::read(lb, S::wave_n() * (S::NT * 32) + nt * 32 + threadIdx.x % 32, kk);
+            };
+            read(0);
 #pragma unroll
-            for (int nt = 0; nt < S::NT; ++nt) y[nt] = B::read(lb, S::column(nt), kk);
+            for (int kk = 0; kk < STEP / 32; ++kk) {
+                if (kk + 1 < STEP / 32) read(kk + 1);
 #pragma unroll
-            for (int mt = 0; mt < S::MT; ++mt)
+                for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
-                for (int nt = 0; nt < S::NT; ++nt) multiply(x[mt], y[nt], c[mt][nt], T());
+                    for (int nt = 0; nt < S::NT; ++nt) multiply(x[kk % 2][mt], y[kk % 2][nt], c[mt][nt], T());
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
-    __syncthreads();  // LDS is free
-}
+};
 
-// exp(x) for x <= 0 or little above, to a rounding or two: the product with log2(e) is taken in two parts, for the rounding
-// of one would be multiplied by x.
-__device__ __forceinline__ float exp_of(float x)
+// exp(x - from), finite or not: the difference first, which no finite x and from >= x take out of range.  The product with
+// log2(e) is rounded, by x - from times 2^-24 of the result.  Where results are float32 it is taken in two parts, to a rounding or
+// two of the result; the exponentials are then still nothing next to the float32 matrix instructions.
+template <class T>
+__device__ __forceinline__ float exp_from(float x, float from)
 {
     constexpr float LOG2E = 1.44269502162933349609375f, REST = 1.925963033500011079e-08f;
-    const float t = x * LOG2E;
-    const float e = __builtin_amdgcn_exp2f(t);
-    const float rest = fmaf(x, LOG2E, -t) + x * REST;
-    return fabsf(rest) < 1 ? fmaf(e, rest * 0.693147180559945f, e) : e;  // x infinite: no rest
+    const float d = x - from, t = d * LOG2E, e = __builtin_amdgcn_exp2f(t);
+    if constexpr (sizeof(T) == 2) return e;
+    const float rest = fmaf(d, LOG2E, -t) + d * REST;
+    return fabsf(rest) < 1 ? fmaf(e, rest * 0.693147180559945f, e) : e;  // d infinite: no rest
+}
+
+// Workgroup `id` of `rows` x `columns` tiles: workgroups go to the 8 XCDs in turn, so each XCD gets a range of the tiles, in
+// which GROUP rows of tiles go together, column after column: what an XCD works on at a time is a block of tiles of some 8 x 8,
+// whose operands its L2 holds.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t rows, uint32_t columns, uint32_t &row, uint32_t &column)
+{
+    constexpr uint32_t XCDS = 8, GROUP = 8;
+    const uint32_t tiles = rows * columns, each = tiles / XCDS, more = tiles % XCDS, xcd = id % XCDS;
+    const uint32_t i = xcd * each + std::min(xcd, more) + id / XCDS;
+    const uint32_t first = i / (GROUP * columns) * GROUP, in = std::min(GROUP, rows - first), k = i - first * columns;
+    row = first + k % in;
+    column = k / in;
 }
 
 template <class T>
@@ -187,38 +281,65 @@ struct Model {
 
 // Rows of C are classes and its columns rows of the batch, so that a lane has the values of one row in its registers.
 template <class T, class S>
-__global__ __launch_bounds__(S::THREADS) void lse_kernel(Model<T> m, int64_t class_tiles, int64_t tiles, float2 *parts, float *target_logit)
+__global__ __launch_bounds__(S::THREADS, 2) void lse_kernel(Model<T> m, uint32_t row_tiles, uint32_t class_tiles, float2 *parts, float *target_logit)
 {
     extern __shared__ char lds[];
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t class0 = tile % class_tiles * S::M, row0 = tile / class_tiles * S::N;
-        Acc c[S::MT][S::NT];
-        product<T, S, true, true>(m.weight, m.hidden, class0, row0, 0, m.hidden.depth, lds, c);
-        float *bias = reinterpret_cast<float *>(lds);
-        float2 *most = reinterpret_cast<float2 *>(bias + S::M);  // [WAVES_M][N]
-        for (int i = threadIdx.x; i < S::M; i += S::THREADS)
-            bias[i] = class0 + i < m.weight.rows ? (m.bias ? m.bias[class0 + i] : 0.0f) : -INFINITY;
-        __syncthreads();
+    float *numbers = reinterpret_cast<float *>(lds + 2 * Products<T, S, true, true>::BYTES);
+    float2 *most = reinterpret_cast<float2 *>(numbers);  // [WAVES_M][N]
+    float *bias = numbers + 2 * S::WAVES_M * S::N;       // [2][M], for tiles in turn
+    Products<T, S, true, true> products(m.weight, m.hidden, lds);
+    const uint32_t tiles = row_tiles * class_tiles;
+    uint32_t class_tile = 0, row_tile = 0;
+    auto aim = [&](uint32_t tile) {
+        if (tile >= tiles) return;
+        tile_of(tile, row_tiles, class_tiles, row_tile, class_tile);
+        products.aim(int64_t{S::M} * class_tile, int64_t{S::N} * row_tile, 0, m.hidden.depth, row_tile + class_tile);
+    };
+    aim(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint32_t this_class_tile = class_tile;
+        const int64_t class0 = int64_t{S::M} * class_tile, row0 = int64_t{S::N} * row_tile;
+        // What the end needs is read before the product, whose barriers come between.
+        int targets[S::NT];  // among this lane's classes of each column, in the order of its results; -1: not there
 #pragma unroll
         for (int nt = 0; nt < S::NT; ++nt) {
-            const int64_t row = row0 + S::column(nt);
-            const int64_t target = row < m.hidden.rows ? m.target[row] - class0 : -1;
+            const int64_t row = row0 + S::column(nt), target = row < m.hidden.rows ? m.target[row] : -1;
+            const int64_t in = target < m.weight.rows ? target - class0 - S::row(0, 0) : -1;
+            targets[nt] = in >= 0 && in < S::MT * 32 && in % 8 < 4 ? static_cast<int>(in / 8 * 4 + in % 4) : -1;
+        }
+        for (int i = threadIdx.x; i < S::M; i += S::THREADS)
+            bias[i] = class0 + i < m.weight.rows ? (m.bias ? m.bias[class0 + i] : 0.0f) : -INFINITY;
+        Acc c[S::MT][S::NT];
+        products.run(c, [&] { aim(tile + gridDim.x); });
+        const float *own_bias = bias + S::row(0, 0);
+#pragma unroll
+        for (int nt = 0; nt < S::NT; ++nt) {
             float top = -INFINITY;
 #pragma unroll
             for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float v = c[mt][nt][i] += bias[S::row(mt, i)];
-                    top = fmaxf(top, v);
-                    if (target == S::row(mt, i) && class0 + target < m.weight.rows) target_logit[row] = v;
+                for (int i = 0; i < 16; i += 4) {
+                    const Chunk b = *reinterpret_cast<const Chunk *>(own_bias + mt * 32 + i * 2);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = fmaxf(top, c[mt][nt][i + k] += b[k]);
                 }
+            int target = targets[nt];
+            if (__any(target >= 0)) {  // few wavefronts have a target among their classes
+                asm volatile("" : "+v"(target));  // nor are the comparisons made ahead of the branch
+                float v = 0;
+#pragma unroll
+                for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v = target == mt * 16 + i ? c[mt][nt][i] : v;
+                if (target >= 0) target_logit[row0 + S::column(nt)] = v;
+            }
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float from = top > -INFINITY ? top : 0.0f;
             float sum = 0;
 #pragma unroll
             for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum += exp_of(c[mt][nt][i] - from);
+                for (int i = 0; i < 16; ++i) sum += exp_from<T>(c[mt][nt][i], from);
             sum += __shfl_xor(sum, 32, 64);
             if (threadIdx.x % 64 < 32) most[S::wave_m() * S::N + S::column(nt)] = make_float2(top, sum);
         }
@@ -229,10 +350,11 @@ __global__ __launch_bounds__(S::THREADS) void lse_kernel(Model<T> m, int64_t cla
                 for (int w = 1; w < S::WAVES_M; ++w) {
                     const float2 o = most[w * S::N + i];
                     const float top = fmaxf(all.x, o.x), from = top > -INFINITY ? top : 0.0f;
-                    all = make_float2(top, all.y * exp_of(all.x - from) + o.y * exp_of(o.x - from));
+                    all = make_float2(top, all.y * exp_from<float>(all.x, from) + o.y * exp_from<float>(o.x, from));
                 }
-                parts[class0 / S::M * m.hidden.rows + row0 + i] = all;
+                parts[this_class_tile * m.hidden.rows + row0 + i] = all;
             }
+        bias = numbers + 2 * S::WAVES_M * S::N + (bias == numbers + 2 * S::WAVES_M * S::N) * S::M;
     }
 }
 
@@ -247,7 +369,7 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
         float2 all = make_float2(-INFINITY, 0);
         auto add = [&](float2 o) {
             const float top = fmaxf(all.x, o.x), from = top > -INFINITY ? top : 0.0f;
-            all = make_float2(top, all.y * exp_of(all.x - from) + o.y * exp_of(o.x - from));
+            all = make_float2(top, all.y * exp_from<float>(all.x, from) + o.y * exp_from<float>(o.x, from));
         };
         if (row < n_rows) {
 #pragma unroll 4
@@ -270,52 +392,83 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
 // p of the classes from `class0` on, [n_rows][stride]: whole tiles, zero where there is no class.  bias_parts: the sums of
 // a tile's rows, [tiles of rows][stride].
 template <class T, class S>
-__global__ __launch_bounds__(S::THREADS) void p_kernel(Model<T> m, const float *lse, const float *grad_loss, int64_t first_class,
-                                                       int64_t class_tiles, int64_t tiles, T *p, int64_t stride, float *bias_parts)
+__global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const float *lse, const float *grad_loss, int64_t first_class,
+                                                       uint32_t row_tiles, uint32_t class_tiles, T *p, int64_t stride, float *bias_parts)
 {
     extern __shared__ char lds[];
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t class0 = first_class + tile % class_tiles * S::N, row0 = tile / class_tiles * S::M;
-        Acc c[S::MT][S::NT];
-        product<T, S, true, true>(m.hidden, m.weight, row0, class0, 0, m.hidden.depth, lds, c);
-        float *row_lse = reinterpret_cast<float *>(lds), *row_grad = row_lse + S::M;
+    float *numbers = reinterpret_cast<float *>(lds + 2 * Products<T, S, true, true>::BYTES);
+    float *sums = numbers;  // [WAVES_M][N]
+    int turn = 0;           // for tiles in turn: [2][3][M]
+    Products<T, S, true, true> products(m.hidden, m.weight, lds);
+    const uint32_t tiles = row_tiles * class_tiles;
+    uint32_t class_tile = 0, row_tile = 0;
+    auto aim = [&](uint32_t tile) {
+        if (tile >= tiles) return;
+        tile_of(tile, row_tiles, class_tiles, row_tile, class_tile);
+        products.aim(int64_t{S::M} * row_tile, first_class + int64_t{S::N} * class_tile, 0, m.hidden.depth, row_tile + class_tile);
+    };
+    aim(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+        const uint32_t this_row_tile = row_tile;
+        const int64_t class0 = first_class + int64_t{S::N} * class_tile, row0 = int64_t{S::M} * row_tile;
+        // What the end needs is read before the product, whose barriers come between.
+        float *row_lse = numbers + S::WAVES_M * S::N + turn * 3 * S::M, *row_grad = row_lse + S::M;
         int *row_target = reinterpret_cast<int *>(row_grad + S::M);
-        float *sums = reinterpret_cast<float *>(row_target + S::M);  // [WAVES_M][N]
         for (int i = threadIdx.x; i < S::M; i += S::THREADS) {
             const int64_t row = row0 + i;
             const int target = row < m.hidden.rows ? m.target[row] : -1;
             const bool has = target >= 0 && target < m.weight.rows;
-            row_lse[i] = has ? lse[row] : 0.0f;
+            row_lse[i] = has ? lse[row] : INFINITY;  // so that p is 0
             row_grad[i] = has ? grad_loss[row] : 0.0f;
-            row_target[i] = has ? static_cast<int>(std::max<int64_t>(-1, std::min<int64_t>(S::N, target - class0))) : -2;
+            row_target[i] = has && target >= class0 && target < class0 + S::N ? static_cast<int>(target - class0) : -1;
         }
-        __syncthreads();
         float bias[S::NT], sum[S::NT] = {};
-        bool is_class[S::NT];
 #pragma unroll
         for (int nt = 0; nt < S::NT; ++nt) {
             const int64_t k = class0 + S::column(nt);
-            is_class[nt] = k < m.weight.rows;
-            bias[nt] = is_class[nt] && m.bias ? m.bias[k] : 0.0f;
+            bias[nt] = k < m.weight.rows ? (m.bias ? m.bias[k] : 0.0f) : -INFINITY;
         }
-        T *to = p + (class0 - first_class) + S::column(0);
+        Acc c[S::MT][S::NT];
+        products.run(c, [&] { aim(tile + gridDim.x); });
+        static_assert(S::NEXT, "a lane's classes are adjacent");
+        char *to = reinterpret_cast<char *>(p + (row0 + S::row(0, 0)) * stride + (class0 - first_class) + S::column(0));
+        int64_t row_bytes = stride * sizeof(T);
+        asm volatile("" : "+s"(row_bytes));  // or its multiples are kept in registers over all tiles
+        const int rows = static_cast<int>(std::min<int64_t>(S::M, m.hidden.rows - row0)) - S::row(0, 0);
+        const float *own_lse = row_lse + S::row(0, 0), *own_grad = row_grad + S::row(0, 0);
+        const int *own_target = row_target + S::row(0, 0);
+        // Few rows have their target among a wavefront's classes: a bit for each of its rows that does.
+        uint64_t targets[S::MT / 2];
+#pragma unroll
+        for (int k = 0; k < S::MT / 2; ++k) {
+            const int target = row_target[S::wave_m() * (S::MT * 32) + k * 64 + threadIdx.x % 64];
+            targets[k] = __ballot(target >= 0 && target / (S::NT * 32) == S::wave_n());
+        }
+        char *at = to;  // a lane's results are of four rows in every eight
 #pragma unroll
         for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = S::row(mt, i);
-                const float l = row_lse[r], g = row_grad[r];
-                const int target = row_target[r];
-                Pack<T, S::NT> out;
+            for (int i = 0; i < 16; i += 4, at += 8 * row_bytes) {
+                __builtin_amdgcn_sched_barrier(0);  // the numbers of four rows at a time, or they fill the registers
+                const int down = mt * 32 + i * 2;
+                const Chunk l = *reinterpret_cast<const Chunk *>(own_lse + down), g = *reinterpret_cast<const Chunk *>(own_grad + down);
+                auto rows_of_four = [&](auto TARGETS) {
 #pragma unroll
-                for (int nt = 0; nt < S::NT; ++nt) {
-                    float v = g * (exp_of(c[mt][nt][i] + bias[nt] - l) - (S::column(nt) == target ? 1.0f : 0.0f));
-                    if (!is_class[nt] || target == -2) v = 0;
-                    sum[nt] += v;
-                    out.v[nt] = narrow<T>(v);
-                }
-                static_assert(S::NEXT, "a lane's classes are adjacent");
-                if (row0 + r < m.hidden.rows) *reinterpret_cast<Pack<T, S::NT> *>(to + (row0 + r) * stride) = out;
+                    for (int k = 0; k < 4; ++k) {
+                        Pack<T, S::NT> out;
+#pragma unroll
+                        for (int nt = 0; nt < S::NT; ++nt) {
+                            float e = exp_from<T>(c[mt][nt][i + k] + bias[nt], l[k]);
+                            if (TARGETS() && own_target[down + k] == S::column(nt)) e -= 1.0f;
+                            e *= g[k];
+                            sum[nt] += e;
+                            out.v[nt] = narrow<T>(e);
+                        }
+                        if (down + k < rows) *reinterpret_cast<Pack<T, S::NT> *>(at + k * row_bytes) = out;
+                    }
+                };
+                if (targets[mt / 2] >> (mt % 2 * 32 + i * 2) & 255) rows_of_four(std::true_type());
+                else rows_of_four(std::false_type());
             }
         if (bias_parts) {
 #pragma unroll
@@ -327,7 +480,7 @@ __global__ __launch_bounds__(S::THREADS) void p_kernel(Model<T> m, const float *
             for (int i = threadIdx.x; i < S::N; i += S::THREADS) {
                 float all = sums[i];
                 for (int w = 1; w < S::WAVES_M; ++w) all += sums[w * S::N + i];
-                bias_parts[row0 / S::M * stride + (class0 - first_class) + i] = all;
+                bias_parts[this_row_tile * stride + (class0 - first_class) + i] = all;
             }
         }
     }
@@ -336,31 +489,47 @@ __global__ __launch_bounds__(S::THREADS) void p_kernel(Model<T> m, const float *
 // C = A B with B across memory.  Each of `splits` parts of the sum's axis goes to a result of its own, [splits][rows][dim]
 // float32, added to what is there where `add` says so; or (out) the one part is the result.
 template <class T, class S, bool A_ALONG>
-__global__ __launch_bounds__(S::THREADS) void product_kernel(Operand<T> a, Operand<T> b, int64_t dim, int64_t row_tiles, int64_t column_tiles,
-                                                             int64_t split_depth, int64_t tiles, float *parts, bool add, T *out)
+__global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Operand<T> b, int64_t dim, uint32_t row_tiles,
+                                                             uint32_t column_tiles, uint32_t splits, int64_t split_depth, float *parts,
+                                                             bool add, T *out)
 {
     extern __shared__ char lds[];
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t column0 = tile % column_tiles * S::N, row0 = tile / column_tiles % row_tiles * S::M;
-        const int64_t split = tile / column_tiles / row_tiles, depth0 = split * split_depth;
+    Products<T, S, A_ALONG, false> products(a, b, lds);
+    const uint32_t tiles = row_tiles * column_tiles * splits;
+    uint32_t column_tile = 0, row_tile = 0;
+    auto aim = [&](uint32_t tile) {
+        if (tile >= tiles) return;
+        tile_of(tile, row_tiles * splits, column_tiles, row_tile, column_tile);
+        const int64_t depth0 = row_tile / row_tiles * split_depth;
+        products.aim(int64_t{S::M} * (row_tile % row_tiles), int64_t{S::N} * column_tile, depth0, std::min(a.depth, depth0 + split_depth), 0);
+    };
+    aim(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * (row_tile % row_tiles), split = row_tile / row_tiles;
         Acc c[S::MT][S::NT];
-        product<T, S, A_ALONG, false>(a, b, row0, column0, depth0, std::min(a.depth, depth0 + split_depth), lds, c);
+        products.run(c, [&] { aim(tile + gridDim.x); });
+        const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
+        const int64_t at = (row0 + S::row(0, 0)) * dim + column0 + S::column(0);
+        auto each = [&](auto store) {
 #pragma unroll
-        for (int mt = 0; mt < S::MT; ++mt)
-#pragma unroll
-            for (int nt = 0; nt < S::NT; ++nt) {
-                const int64_t column = column0 + S::column(nt);
+            for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int64_t row = row0 + S::row(mt, i);
-                    if (row >= a.rows || column >= dim) continue;
-                    if (out) out[row * dim + column] = narrow<T>(c[mt][nt][i]);
-                    else {
-                        float *to = parts + (split * a.rows + row) * dim + column;
-                        *to = add ? *to + c[mt][nt][i] : c[mt][nt][i];
-                    }
+                    const int down = mt * 32 + i / 4 * 8 + i % 4;
+#pragma unroll
+                    for (int nt = 0; nt < S::NT; ++nt)
+                        if (down < rows && column0 + S::column(nt) < dim) store(down * dim + nt * 32, c[mt][nt][i]);
                 }
-            }
+        };
+        static_assert(!S::NEXT, "a lane's columns are 32 apart");
+        if (out) {
+            T *to = out + at;
+            each([&](int64_t k, float v) { to[k] = narrow<T>(v); });
+        } else {
+            float *to = parts + split * a.rows * dim + at;
+            if (add) each([&](int64_t k, float v) { to[k] += v; });
+            else each([&](int64_t k, float v) { to[k] = v; });
+        }
     }
 }
 
@@ -403,25 +572,60 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t stride
 
 // ---- what a call launches
 
-using Forward = Shape<128, 128, 2, 2, false>;
-using Backward = Shape<128, 128, 2, 2, true>;
-using Gradient = Shape<128, 128, 2, 2, false>;
+// A workgroup of 4 wavefronts and tiles of 128 x 128, of which a CU has two; or, where bfloat16 products have so many tiles, one of 8
+// and 256 x 256: half the traffic to LDS, and a third less from it, for as many products (16,384 x 65,536 logits over 512 values: 1.32
+// ms, against 1.58).  float32 products are bound by the matrix core, and gain nothing (loss_f32's logits: 257 us, against 255).
+struct Small {
+    static constexpr int TILE = 128, RESIDENT = 512;
+    template <bool NEXT>
+    using Of = Shape<128, 128, 2, 2, NEXT>;
+};
+struct Large {
+    static constexpr int TILE = 256, RESIDENT = 256;
+    template <bool NEXT>
+    using Of = Shape<256, 256, 2, 4, NEXT>;
+};
 
 template <class S>
 constexpr size_t lds_bytes()
 {
-    return 2 * (S::M + S::N) * STEP;
+    // two steps' tiles; what tiles are finished with, at most: of the wavefronts [WAVES_M][N] pairs, and twice [3][M] numbers
+    return 2 * (S::M + S::N) * STEP + (2 * S::WAVES_M * S::N + 6 * S::M) * sizeof(float);
 }
 
-dim3 grid_of(int64_t n) { return dim3(static_cast<uint32_t>(std::max<int64_t>(1, std::min(n, MAX_GRID)))); }
+// More than 64 KB of LDS has to be asked for, once for each kernel and device.
+template <auto *KERNEL>
+hipError_t allow_lds(size_t bytes)
+{
+    constexpr int DEVICES = 64;
+    static std::atomic<bool> done[DEVICES];
+    int device = -1;
+    if (const hipError_t e = hipGetDevice(&device)) return e;
+    if (device >= 0 && device < DEVICES && done[device].load(std::memory_order_relaxed)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == hipSuccess && device >= 0 && device < DEVICES) done[device].store(true, std::memory_order_relaxed);
+    return e;
+}
+
+template <class S, auto *KERNEL, class... Args>
+hipError_t launch_product(dim3 grid, hipStream_t stream, Args... args)
+{
+    if (const hipError_t e = allow_lds<KERNEL>(lds_bytes<S>())) return e;
+    hipLaunchKernelGGL(KERNEL, grid, dim3(S::THREADS), lds_bytes<S>(), stream, args...);
+    return hipGetLastError();
+}
+
+dim3 grid_of(int64_t n, int64_t most = 8192) { return dim3(static_cast<uint32_t>(std::max<int64_t>(1, std::min(n, most)))); }
 
 // The parts of a call's workspace, in bytes from its start; and its sizes.
 struct Plan {
+    bool large;                     // Large or Small, and what they are
+    int64_t tile, resident;
     int64_t packed;                 // values of a packed row
     int64_t hidden = -1, weight = -1;  // packed operands; -1: used where they are
     int64_t class_tiles, row_tiles;
     int64_t parts, target;          // forward
-    int64_t piece, pieces;          // classes of a piece, a multiple of a tile's
+    int64_t piece, pieces, stride;  // classes of a piece, a multiple of a tile's; values of a row of p
     int64_t p, bias, hidden_splits, hidden_parts, weight_splits, weight_parts;
     int64_t bytes = 0;
 
@@ -437,6 +641,9 @@ Plan plan_operands(const head_classes &c)
 {
     Plan p{};
     p.hidden = p.weight = -1;
+    p.large = c.dtype == HEAD_BF16 && ceil_div(c.n_rows, Large::TILE) * ceil_div(c.n_classes, Large::TILE) >= Large::RESIDENT;
+    p.tile = p.large ? Large::TILE : Small::TILE;
+    p.resident = p.large ? Large::RESIDENT : Small::RESIDENT;
     const int e = value_bytes(c.dtype);
     p.packed = round_up(c.dim, 16 / e);
     auto whole = [&](const void *at, int64_t stride) { return (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(c.dim * e)) % 16 == 0; };
@@ -448,17 +655,17 @@ Plan plan_operands(const head_classes &c)
 Plan plan_forward(const head_classes &c)
 {
     Plan p = plan_operands(c);
-    p.class_tiles = ceil_div(c.n_classes, Forward::M);
-    p.row_tiles = ceil_div(c.n_rows, Forward::N);
+    p.class_tiles = ceil_div(c.n_classes, p.tile);
+    p.row_tiles = ceil_div(c.n_rows, p.tile);
     p.parts = p.part(p.class_tiles * c.n_rows * static_cast<int64_t>(sizeof(float2)));
     p.target = p.part(c.n_rows * 4);
     return p;
 }
 
-// Parts of a sum of `depth` such that `tiles` tiles of each fill the device twice over, each part having at least 8 steps.
-int64_t splits_of(int64_t tiles, int64_t depth, int64_t step)
+// Parts of a sum of `depth` such that `tiles` tiles of each fill the device, each part having at least 8 steps.
+int64_t splits_of(int64_t tiles, int64_t resident, int64_t depth, int64_t step)
 {
-    return std::max<int64_t>(1, std::min(512 / std::max<int64_t>(1, tiles), ceil_div(depth, 8 * step)));
+    return std::max<int64_t>(1, std::min(resident / std::max<int64_t>(1, tiles), ceil_div(depth, 8 * step)));
 }
 
 Plan plan_backward(const head_classes &c)
@@ -466,15 +673,17 @@ Plan plan_backward(const head_classes &c)
     Plan p = plan_operands(c);
     const int e = value_bytes(c.dtype);
     const int64_t step = STEP / e;
-    p.piece = std::min(round_up(c.n_classes, Backward::N), std::max<int64_t>(1024, PIECE_BYTES / (std::max<int64_t>(1, c.n_rows) * e) / 1024 * 1024));
+    p.piece = std::min(round_up(c.n_classes, p.tile), std::max<int64_t>(1024, PIECE_BYTES / (std::max<int64_t>(1, c.n_rows) * e) / 1024 * 1024));
     p.pieces = ceil_div(c.n_classes, p.piece);
-    p.row_tiles = ceil_div(c.n_rows, Backward::M);
-    p.p = p.part(c.n_rows * p.piece * e);
-    p.bias = p.part(p.row_tiles * p.piece * 4);
-    const int64_t columns = ceil_div(c.dim, Gradient::N);
-    p.hidden_splits = splits_of(ceil_div(c.n_rows, Gradient::M) * columns, p.piece, step);
+    p.row_tiles = ceil_div(c.n_rows, p.tile);
+    // Rows a power of two apart would lie in few of the memory's channels: a row more than a piece by 256 bytes goes through all.
+    p.stride = p.piece + 256 / e;
+    p.p = p.part(c.n_rows * p.stride * e);
+    p.bias = p.part(p.row_tiles * p.stride * 4);
+    const int64_t columns = ceil_div(c.dim, p.tile);
+    p.hidden_splits = splits_of(p.row_tiles * columns, p.resident, p.piece, step);
     p.hidden_parts = p.hidden_splits * p.pieces > 1 ? p.part(p.hidden_splits * c.n_rows * c.dim * 4) : -1;
-    p.weight_splits = splits_of(ceil_div(p.piece, Gradient::M) * columns, c.n_rows, step);
+    p.weight_splits = splits_of(ceil_div(p.piece, p.tile) * columns, p.resident, c.n_rows, step);
     p.weight_parts = p.weight_splits > 1 ? p.part(p.weight_splits * p.piece * c.dim * 4) : -1;
     return p;
 }
@@ -486,7 +695,7 @@ Model<T> model_of(const head_classes &c, const Plan &p, char *workspace, hipStre
         const T *from = static_cast<const T *>(at);
         if (packed_at < 0) return Operand<T>{from, stride, rows, c.dim};
         T *to = reinterpret_cast<T *>(workspace + packed_at);
-        hipLaunchKernelGGL((pack_kernel<T>), grid_of(std::min<int64_t>(8192, ceil_div(rows * p.packed, 256))), dim3(256), 0, stream, from, stride,
+        hipLaunchKernelGGL((pack_kernel<T>), grid_of(ceil_div(rows * p.packed, 256)), dim3(256), 0, stream, from, stride,
                            rows, c.dim, to, p.packed);
         return Operand<T>{to, p.packed, rows, p.packed};
     };
@@ -494,75 +703,85 @@ Model<T> model_of(const head_classes &c, const Plan &p, char *workspace, hipStre
                     c.target};
 }
 
-template <class T>
-hipError_t forward(const head_classes &c, float *loss, float *lse, char *workspace, hipStream_t stream)
+template <class T, class Size>
+hipError_t forward(const head_classes &c, const Plan &p, float *loss, float *lse, char *workspace, hipStream_t stream)
 {
-    const Plan p = plan_forward(c);
+    using Forward = typename Size::template Of<false>;
     const Model<T> m = model_of<T>(c, p, workspace, stream);
     if (const hipError_t e = hipGetLastError()) return e;
     float2 *parts = reinterpret_cast<float2 *>(workspace + p.parts);
     float *target_logit = reinterpret_cast<float *>(workspace + p.target);
     const int64_t tiles = p.class_tiles * p.row_tiles;
-    hipLaunchKernelGGL((lse_kernel<T, Forward>), grid_of(tiles), dim3(Forward::THREADS), lds_bytes<Forward>(), stream, m, p.class_tiles, tiles,
-                       parts, target_logit);
+    if (const hipError_t e = launch_product<Forward, lse_kernel<T, Forward>>(grid_of(tiles, Size::RESIDENT), stream, m, static_cast<uint32_t>(p.row_tiles),
+                                                                                static_cast<uint32_t>(p.class_tiles), parts, target_logit)) return e;
     hipLaunchKernelGGL(lse_join_kernel, grid_of(ceil_div(c.n_rows, 32)), dim3(256), 0, stream, c.n_rows, c.n_classes, p.class_tiles, parts,
                        target_logit, c.target, loss, lse);
     return hipGetLastError();
 }
 
-template <class T>
-hipError_t backward(const head_classes &c, const float *lse, const float *grad_loss, T *grad_hidden, T *grad_weight, float *grad_bias,
+template <class T, class Size>
+hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, const float *grad_loss, T *grad_hidden, T *grad_weight, float *grad_bias,
                     char *workspace, hipStream_t stream)
 {
+    using Backward = typename Size::template Of<true>;
+    using Gradient = typename Size::template Of<false>;
     if (c.n_rows == 0) {
-        hipLaunchKernelGGL((zero_kernel<T>), grid_of(std::min<int64_t>(8192, ceil_div(c.n_classes * c.dim, 256))), dim3(256), 0, stream,
+        hipLaunchKernelGGL((zero_kernel<T>), grid_of(ceil_div(c.n_classes * c.dim, 256)), dim3(256), 0, stream,
                            grad_weight, c.n_classes * c.dim);
         if (grad_bias)
-            hipLaunchKernelGGL((zero_kernel<float>), grid_of(std::min<int64_t>(8192, ceil_div(c.n_classes, 256))), dim3(256), 0, stream, grad_bias,
+            hipLaunchKernelGGL((zero_kernel<float>), grid_of(ceil_div(c.n_classes, 256)), dim3(256), 0, stream, grad_bias,
                                c.n_classes);
         return hipGetLastError();
     }
-    const Plan plan = plan_backward(c);
     const Model<T> m = model_of<T>(c, plan, workspace, stream);
     if (const hipError_t e = hipGetLastError()) return e;
     T *p = reinterpret_cast<T *>(workspace + plan.p);
     float *bias_parts = grad_bias ? reinterpret_cast<float *>(workspace + plan.bias) : nullptr;
     float *hidden_parts = plan.hidden_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.hidden_parts);
     float *weight_parts = plan.weight_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.weight_parts);
-    const int64_t step = STEP / sizeof(T), columns = ceil_div(c.dim, Gradient::N);
+    const int64_t step = STEP / sizeof(T);
+    const uint32_t columns = static_cast<uint32_t>(ceil_div(c.dim, Gradient::N));
     for (int64_t piece = 0; piece < plan.pieces; ++piece) {
         const int64_t first = piece * plan.piece, classes = std::min(plan.piece, c.n_classes - first);
-        const int64_t class_tiles = ceil_div(classes, Backward::N), stride = plan.piece;
+        const int64_t class_tiles = ceil_div(classes, Backward::N), stride = plan.stride;
         const int64_t p_tiles = class_tiles * plan.row_tiles;
-        hipLaunchKernelGGL((p_kernel<T, Backward>), grid_of(p_tiles), dim3(Backward::THREADS), lds_bytes<Backward>(), stream, m, lse, grad_loss,
-                           first, class_tiles, p_tiles, p, stride, bias_parts);
+        if (const hipError_t e = launch_product<Backward, p_kernel<T, Backward>>(grid_of(p_tiles, Size::RESIDENT), stream, m, lse, grad_loss, first,
+                                                                                 static_cast<uint32_t>(plan.row_tiles),
+                                                                                 static_cast<uint32_t>(class_tiles), p, stride, bias_parts))
+            return e;
         if (grad_bias)
             hipLaunchKernelGGL(bias_kernel, dim3(static_cast<uint32_t>(ceil_div(classes, 256))), dim3(256), 0, stream, bias_parts,
                                plan.row_tiles, stride, classes, grad_bias + first);
         // grad_hidden [n_rows][dim] += p [n_rows][classes] weight [classes][dim]
         {
-            const int64_t row_tiles = ceil_div(c.n_rows, Gradient::M), depth = round_up(ceil_div(classes, plan.hidden_splits), step);
+            const uint32_t row_tiles = static_cast<uint32_t>(ceil_div(c.n_rows, Gradient::M));
+            const int64_t depth = round_up(ceil_div(classes, plan.hidden_splits), step);
             const Operand<T> a{p, stride, c.n_rows, classes}, b{m.weight.at + first * m.weight.stride, m.weight.stride, m.weight.depth, classes};
-            const int64_t tiles = row_tiles * columns * plan.hidden_splits;
-            hipLaunchKernelGGL((product_kernel<T, Gradient, true>), grid_of(tiles), dim3(Gradient::THREADS), lds_bytes<Gradient>(), stream, a, b,
-                               c.dim, row_tiles, columns, depth, tiles, hidden_parts, piece > 0, hidden_parts ? nullptr : grad_hidden);
+            const int64_t tiles = int64_t{row_tiles} * columns * plan.hidden_splits;
+            if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, true>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
+                                                                                                 static_cast<uint32_t>(plan.hidden_splits), depth, hidden_parts,
+                                                                                                 piece > 0, hidden_parts ? nullptr : grad_hidden))
+                return e;
         }
         // grad_weight [classes][dim] = p^T [classes][n_rows] hidden [n_rows][dim]
         {
-            const int64_t row_tiles = ceil_div(classes, Gradient::M), depth = round_up(ceil_div(c.n_rows, plan.weight_splits), step);
+            const uint32_t row_tiles = static_cast<uint32_t>(ceil_div(classes, Gradient::M));
+            const int64_t depth = round_up(ceil_div(c.n_rows, plan.weight_splits), step);
             const Operand<T> a{p, stride, classes, c.n_rows}, b{m.hidden.at, m.hidden.stride, m.hidden.depth, c.n_rows};
-            const int64_t tiles = row_tiles * columns * plan.weight_splits;
+            const int64_t tiles = int64_t{row_tiles} * columns * plan.weight_splits;
             T *out = grad_weight + first * c.dim;
-            hipLaunchKernelGGL((product_kernel<T, Gradient, false>), grid_of(tiles), dim3(Gradient::THREADS), lds_bytes<Gradient>(), stream, a, b,
-                               c.dim, row_tiles, columns, depth, tiles, weight_parts, false, weight_parts ? nullptr : out);
+            if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, false>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
+                                                                                                  static_cast<uint32_t>(plan.weight_splits), depth, weight_parts,
+                                                                                                  false, weight_parts ? nullptr : out))
+                return e;
             if (weight_parts)
-                hipLaunchKernelGGL((parts_kernel<T>), grid_of(std::min<int64_t>(8192, ceil_div(classes * c.dim, 256))), dim3(256), 0, stream,
+                hipLaunchKernelGGL((parts_kernel<T>), grid_of(ceil_div(classes * c.dim, 256)), dim3(256), 0, stream,
                                    weight_parts, plan.weight_splits, classes * c.dim, out);
         }
         if (const hipError_t e = hipGetLastError()) return e;
     }
     if (hidden_parts)
-        hipLaunchKernelGGL((parts_kernel<T>), grid_of(std::min<int64_t>(8192, ceil_div(c.n_rows * c.dim, 256))), dim3(256), 0, stream, hidden_parts,
+        hipLaunchKernelGGL((parts_kernel<T>), grid_of(ceil_div(c.n_rows * c.dim, 256)), dim3(256), 0, stream, hidden_parts,
                            plan.hidden_splits, c.n_rows * c.dim, grad_hidden);
     return hipGetLastError();
 }
@@ -574,7 +793,9 @@ int64_t cross_entropy_bytes(const head_classes &c) { return c.n_rows ? plan_forw
 hipError_t launch_cross_entropy(const head_classes &c, float *loss, float *lse, void *workspace, hipStream_t stream)
 {
     char *w = static_cast<char *>(workspace);
-    return c.dtype == HEAD_BF16 ? forward<bf16>(c, loss, lse, w, stream) : forward<float>(c, loss, lse, w, stream);
+    const Plan p = plan_forward(c);
+    if (c.dtype == HEAD_F32) return forward<float, Small>(c, p, loss, lse, w, stream);
+    return p.large ? forward<bf16, Large>(c, p, loss, lse, w, stream) : forward<bf16, Small>(c, p, loss, lse, w, stream);
 }
 
 int64_t cross_entropy_grad_bytes(const head_classes &c) { return c.n_rows ? plan_backward(c).bytes : 0; }
@@ -583,9 +804,13 @@ hipError_t launch_cross_entropy_grad(const head_classes &c, const float *lse, co
                                      void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream)
 {
     char *w = static_cast<char *>(workspace);
-    if (c.dtype == HEAD_BF16)
-        return backward(c, lse, grad_loss, static_cast<bf16 *>(grad_hidden), static_cast<bf16 *>(grad_weight), grad_bias, w, stream);
-    return backward(c, lse, grad_loss, static_cast<float *>(grad_hidden), static_cast<float *>(grad_weight), grad_bias, w, stream);
+    const Plan p = plan_backward(c);
+    if (c.dtype == HEAD_F32)
+        return backward<float, Small>(c, p, lse, grad_loss, static_cast<float *>(grad_hidden), static_cast<float *>(grad_weight), grad_bias, w,
+                                      stream);
+    bf16 *gh = static_cast<bf16 *>(grad_hidden), *gw = static_cast<bf16 *>(grad_weight);
+    return p.large ? backward<bf16, Large>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream)
+                   : backward<bf16, Small>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream);
 }
 
 }  // namespace head_impl

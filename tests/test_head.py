@@ -386,8 +386,19 @@ def _cross_entropy(h, w, b, t):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,dim,classes", LOSS)
 def test_cross_entropy_and_its_gradient(n, dim, classes, dtype):
+    _check_cross_entropy(n, dim, classes, dtype, ((0, 0, True), (3, 1, False), (8, 8, True)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,dim,classes", [(4099, 72, 4200), (300, 24, 40_000), (9000, 300, 2050)])
+def test_cross_entropy_in_large_tiles(n, dim, classes):
+    """Enough tiles of 256 x 256 that bfloat16 products run in them, with rows, classes and dim that end inside one."""
+    _check_cross_entropy(n, dim, classes, "bfloat16", ((0, 0, True),))
+
+
+def _check_cross_entropy(n, dim, classes, dtype, variants):
     rng = np.random.default_rng(n * 13 + dim * 5 + classes)
-    for spread, shift, biased in ((0, 0, True), (3, 1, False), (8, 8, True)):
+    for spread, shift, biased in variants:
         h, h64 = _rows(rng, n, dim, dtype, spread, shift)
         w, w64 = _rows(rng, classes, dim, dtype, spread, shift)
         h *= 0.7
