@@ -40,6 +40,38 @@ __device__ __forceinline__ int64_t vector_of(const Ids &s, const int32_t *row, i
     return id >= 0 && v >= 0 && v < s.n_vectors ? v : -1;
 }
 
+// A piece of V values as the machine word it is read as.  A value that is to count for nothing is masked there, by all ones or
+// none: as a choice between values it would be a branch for the compiler, and the loads of a loop would not be on their way together.
+template <int BYTES> struct WordOf;
+template <> struct WordOf<2> { using Type = uint16_t; };
+template <> struct WordOf<4> { using Type = uint32_t; };
+template <> struct WordOf<8> { using Type = uint32_t __attribute__((ext_vector_type(2))); };
+template <> struct WordOf<16> { using Type = uint32_t __attribute__((ext_vector_type(4))); };
+template <class T, int V>
+using Word = typename WordOf<sizeof(T) * V>::Type;
+
+__device__ __forceinline__ void add(float (&a)[1], uint16_t w) { a[0] += __uint_as_float(static_cast<uint32_t>(w) << 16); }
+__device__ __forceinline__ void add(float (&a)[1], uint32_t w) { a[0] += __uint_as_float(w); }
+__device__ __forceinline__ void add(float (&a)[2], uint32_t w)
+{
+    a[0] += __uint_as_float(w << 16);
+    a[1] += __uint_as_float(w & 0xFFFF0000u);
+}
+template <int V, class W>
+__device__ __forceinline__ void add(float (&a)[V], W w)
+{
+    constexpr int WORDS = sizeof(W) / 4;
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) {
+        if constexpr (V == WORDS) {
+            a[k] += __uint_as_float(w[k]);
+        } else {
+            a[2 * k] += __uint_as_float(w[k] << 16);
+            a[2 * k + 1] += __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+    }
+}
+
 // `lanes` lanes of a group read a vector; `team` groups share a row.
 template <class T, int V>
 __global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Ids s, const T *table, int64_t table_stride, float scale,
@@ -54,14 +86,23 @@ __global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Id
         float a[V] = {};
         if (row < n_rows && c < dim) {
             const int32_t *ids = s.id + row * s.stride;
-#pragma unroll 8
-            for (int64_t t = member; t < s.n_ids; t += team) {
-                const int64_t v = vector_of(s, ids, t);
-                if (v >= 0) {
-                    const Pack<T, V> p = *reinterpret_cast<const Pack<T, V> *>(table + v * table_stride + c);
+            constexpr int AHEAD = 8;  // vectors on their way
+            int64_t last = 0;  // read again, and dropped, where an id stands for nothing: a load without a branch around it
+            for (int64_t t0 = member; t0 < s.n_ids; t0 += int64_t{AHEAD} * team) {
+                int64_t v[AHEAD];
+                Word<T, V> p[AHEAD];
 #pragma unroll
-                    for (int k = 0; k < V; ++k) a[k] += widen(p.v[k]);
+                for (int j = 0; j < AHEAD; ++j) {
+                    const int64_t t = t0 + j * team;
+                    v[j] = t < s.n_ids ? vector_of(s, ids, t) : -1;
                 }
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) {
+                    last = v[j] >= 0 ? v[j] : last;
+                    p[j] = *reinterpret_cast<const Word<T, V> *>(table + last * table_stride + c);
+                }
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) add(a, static_cast<Word<T, V>>(p[j] & static_cast<uint32_t>(~(v[j] >> 63))));
             }
         }
         if (team > 1) {
@@ -89,6 +130,52 @@ __global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Id
             for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[k]);
             *reinterpret_cast<Pack<T, V> *>(out + row * dim + c) = p;
         }
+    }
+}
+
+// Many rows with many ids: a group of G lanes takes ROWS rows at once, all groups go through the ids in the same order, and so
+// few of them are launched that all are resident: what is read at a time is the vectors of a few ids (trees), which an L2
+// holds, and not the whole table.  The G lanes read G ids of a row at once, and each gets every one of them from its neighbours.
+template <class T, int V, int G, int ROWS>
+__global__ __launch_bounds__(THREADS) void sweep_kernel(int64_t n_rows, int dim, Ids s, const T *table, uint32_t stride_bytes, float scale,
+                                                        T *out)
+{
+    const int lane = threadIdx.x % G, c = (blockIdx.y * G + lane) * V;
+    const bool in = c < dim;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * (THREADS / G) * ROWS;
+    for (int64_t row0 = (static_cast<int64_t>(blockIdx.x) * (THREADS / G) + threadIdx.x / G) * ROWS; row0 - threadIdx.x / G * ROWS < n_rows;
+         row0 += step) {
+        float a[ROWS][V] = {};
+        int32_t last[ROWS] = {};  // read again, and dropped, where an id stands for nothing: a load without a branch around it
+        const char *from = reinterpret_cast<const char *>(table + (in ? c : 0));
+        for (int64_t t0 = 0; t0 < s.n_ids; t0 += G) {
+            int32_t v[ROWS];  // of id t0 + lane; -1: none
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+                v[r] = row0 + r < n_rows && t0 + lane < s.n_ids ? static_cast<int32_t>(vector_of(s, s.id + (row0 + r) * s.stride, t0 + lane)) : -1;
+#pragma unroll 2
+            for (int t = 0; t < G; ++t) {
+                Word<T, V> p[ROWS];
+                uint32_t mask[ROWS];
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const int32_t at = __shfl(v[r], t, G);
+                    mask[r] = ~static_cast<uint32_t>(at >> 31);
+                    last[r] = at >= 0 ? at : last[r];
+                    p[r] = *reinterpret_cast<const Word<T, V> *>(from + static_cast<uint64_t>(static_cast<uint32_t>(last[r])) * stride_bytes);
+                }
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) add(a[r], p[r] & mask[r]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            if (in && row0 + r < n_rows) {
+                Pack<T, V> p;
+#pragma unroll
+                for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[r][k]);
+                *reinterpret_cast<Pack<T, V> *>(out + (row0 + r) * dim + c) = p;
+            }
     }
 }
 
@@ -348,6 +435,19 @@ hipError_t by_piece(int wide, F f)
     }
 }
 
+template <class F>
+hipError_t by_lanes(int lanes, F f)
+{
+    switch (lanes) {
+        case 4: return f(std::integral_constant<int, 4>());
+        case 8: return f(std::integral_constant<int, 8>());
+        case 16: return f(std::integral_constant<int, 16>());
+        case 32: return f(std::integral_constant<int, 32>());
+        case 64: return f(std::integral_constant<int, 64>());
+        default: return hipErrorInvalidValue;
+    }
+}
+
 int power_at_least(int64_t n, int most)
 {
     int p = 1;
@@ -359,9 +459,20 @@ template <class T>
 hipError_t embed(const head_ids &ids, int64_t dim, const T *table, int64_t table_stride, float scale, T *out, hipStream_t stream)
 {
     const uint64_t bits = address(table) | address(out) | static_cast<uint64_t>(table_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));
-    const Ids s{ids.ids, ids.offset, ids.ids_stride, ids.n_vectors, ids.n_ids};
+    // an id without a vector may read vector 0: where there are no vectors there are no ids
+    const Ids s{ids.ids, ids.offset, ids.ids_stride, ids.n_vectors, ids.n_vectors ? ids.n_ids : 0};
     return by_piece<T>(piece(bits, sizeof(T)), [&](auto V) {
         const int lanes = power_at_least(ceil_div(dim, V()), 64), in_wave = 64 / lanes;
+        constexpr int ROWS = 4;
+        if constexpr (V() * sizeof(T) == 16)
+            if (lanes >= 4 && ids.n_ids >= 16 && ids.n_rows >= int64_t{1024} * ROWS * in_wave && table_stride * sizeof(T) <= UINT32_MAX)
+                return by_lanes(lanes, [&](auto G) {
+                    const dim3 grid(static_cast<uint32_t>(std::min(ceil_div(ids.n_rows, ROWS * (THREADS / G())), MAX_GRID)),
+                                    static_cast<uint32_t>(ceil_div(dim, G() * V())));
+                    hipLaunchKernelGGL((sweep_kernel<T, V(), G(), ROWS>), grid, dim3(THREADS), 0, stream, ids.n_rows, static_cast<int>(dim), s,
+                                       table, static_cast<uint32_t>(table_stride * sizeof(T)), scale, out);
+                    return hipGetLastError();
+                });
         // a group for each row, a wavefront's groups, or a workgroup's
         const bool few = ids.n_rows <= 1024 && ids.n_ids >= 4 * in_wave;
         const int threads = few ? 1024 : THREADS;
