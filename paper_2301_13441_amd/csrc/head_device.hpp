@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "../../include/head.h"
@@ -44,6 +45,20 @@ template <class P>
 inline uint64_t address(const P *p)
 {
     return reinterpret_cast<uintptr_t>(p);
+}
+
+// More than 64 KB of LDS has to be asked for, once for each kernel and device.
+template <auto *KERNEL>
+hipError_t allow_lds(size_t bytes)
+{
+    constexpr int DEVICES = 64;
+    static std::atomic<bool> done[DEVICES];
+    int device = -1;
+    if (const hipError_t e = hipGetDevice(&device)) return e;
+    if (device >= 0 && device < DEVICES && done[device].load(std::memory_order_relaxed)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == hipSuccess && device >= 0 && device < DEVICES) done[device].store(true, std::memory_order_relaxed);
+    return e;
 }
 
 hipError_t launch_embed(const head_ids &ids, int32_t dtype, int64_t dim, const void *table, int64_t table_stride, float scale,

@@ -181,44 +181,57 @@ __global__ __launch_bounds__(THREADS) void sweep_kernel(int64_t n_rows, int dim,
 
 // ---- the sort
 
-constexpr int DIGIT = 8, DIGITS = 1 << DIGIT;
+// A digit has at most MAX_DIGIT bits: as many passes as the largest key needs with that, and as few bits as do with those passes.
+constexpr int MAX_DIGIT = 10;
+constexpr int LANES = 512, WAVES = LANES / 64;
 constexpr int ITEMS = 16;                // pairs of a lane
-constexpr int TILE = THREADS * ITEMS;    // pairs of a workgroup
-constexpr int WAVES = THREADS / 64;
+constexpr int TILE = LANES * ITEMS;      // pairs of a workgroup: at 9 bits 16 of each digit, 128 bytes that are written together
+
+// of move_kernel: the tile's pairs, and for a digit its place away and a count for each wavefront; at 9 bits two workgroups of a CU
+constexpr size_t move_lds(int bits) { return TILE * 8 + ((4 + 2 * WAVES) << bits); }
+
+struct Pair {
+    uint32_t key, row;
+};
 
 // Where pairs come from: the ids of the batch on the first pass, the last pass's output on the others.
 struct Pairs {
     Ids s;
-    const uint32_t *key, *row;   // null on the first pass
+    const Pair *pair;              // null on the first pass
     uint32_t n;
     uint32_t n_ids, magic, shift;  // division by n_ids of a number below 2^31
 };
 
-__device__ __forceinline__ uint32_t row_of(const Pairs &p, uint32_t i)
+// What a pass reads: the last pass's output, or ids, without and with offsets.
+enum { LAST_PASS, IDS, IDS_AND_OFFSETS };
+
+// Pair i.  An id that stands for no vector sorts behind all that do.
+template <int FROM>
+__device__ __forceinline__ Pair pair_of(const Pairs &p, uint32_t i)
 {
-    return p.n_ids == 1 ? i : __umulhi(i, p.magic) >> p.shift;
-}
-// An id that stands for no vector sorts behind all that do.
-__device__ __forceinline__ uint32_t key_of(const Pairs &p, uint32_t i, uint32_t row)
-{
-    if (p.key) return p.key[i];
-    const int64_t v = vector_of(p.s, p.s.id + row * p.s.stride, i - row * p.n_ids);
-    return static_cast<uint32_t>(v < 0 ? p.s.n_vectors : v);
+    if constexpr (FROM == LAST_PASS) return p.pair[i];
+    const uint32_t row = p.n_ids == 1 ? i : __umulhi(i, p.magic) >> p.shift, t = i - row * p.n_ids;
+    const int32_t id = p.s.id[row * p.s.stride + t];
+    const int64_t v = id + (FROM == IDS_AND_OFFSETS ? p.s.offset[t] : 0);
+    return Pair{static_cast<uint32_t>(id >= 0 && v >= 0 && v < p.s.n_vectors ? v : p.s.n_vectors), row};
 }
 
-__global__ __launch_bounds__(THREADS) void count_kernel(Pairs p, int bit, uint32_t n_tiles, uint32_t *counts)
+template <int FROM>
+__global__ __launch_bounds__(LANES) void count_kernel(Pairs p, int bit, int bits, uint32_t n_tiles, uint32_t *counts)
 {
-    __shared__ uint32_t count[DIGITS];
-    count[threadIdx.x] = 0;
+    __shared__ uint32_t count[1 << MAX_DIGIT];
+    const int digits = 1 << bits;
+    for (int d = threadIdx.x; d < digits; d += LANES) count[d] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * TILE + threadIdx.x;
+    uint32_t key[ITEMS];
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        const uint32_t i = first + k * THREADS;
-        if (i < p.n) atomicAdd(&count[key_of(p, i, p.key ? 0 : row_of(p, i)) >> bit & (DIGITS - 1)], 1u);
-    }
+    for (int k = 0; k < ITEMS; ++k) key[k] = pair_of<FROM>(p, std::min(first + k * LANES, p.n - 1)).key;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+        if (first + k * LANES < p.n) atomicAdd(&count[key[k] >> bit & (digits - 1)], 1u);
     __syncthreads();
-    counts[threadIdx.x * n_tiles + blockIdx.x] = count[threadIdx.x];
+    for (int d = threadIdx.x; d < digits; d += LANES) counts[static_cast<uint32_t>(d) * n_tiles + blockIdx.x] = count[d];
 }
 
 // Sum of v over the lanes before this one of the workgroup; `all`: over the whole workgroup.
@@ -244,11 +257,11 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t &all, uint32
 }
 
 // A workgroup for each digit: its counts become sums over the tiles before, and the digit's total goes behind them.
-__global__ __launch_bounds__(THREADS) void tiles_kernel(uint32_t n_tiles, uint32_t *counts, uint32_t *totals)
+__global__ __launch_bounds__(LANES) void tiles_kernel(uint32_t n_tiles, uint32_t *counts, uint32_t *totals)
 {
     __shared__ uint32_t lds[WAVES];
     uint32_t *row = counts + static_cast<int64_t>(blockIdx.x) * n_tiles, sum = 0;
-    for (uint32_t first = 0; first < n_tiles; first += THREADS) {
+    for (uint32_t first = 0; first < n_tiles; first += LANES) {
         const uint32_t i = first + threadIdx.x;
         uint32_t all;
         const uint32_t before = sum_before(i < n_tiles ? row[i] : 0, all, lds);
@@ -265,59 +278,84 @@ __device__ __forceinline__ void in_order()
     __builtin_amdgcn_wave_barrier();
 }
 
-__global__ __launch_bounds__(THREADS) void move_kernel(Pairs p, int bit, uint32_t n_tiles, const uint32_t *counts, const uint32_t *totals,
-                                                       uint32_t *key_out, uint32_t *row_out)
+// A tile is sorted by the digit in LDS and then goes out in that order, so that neighbours write neighbouring places.
+template <int FROM>
+__global__ __launch_bounds__(LANES, 4) void move_kernel(Pairs p, int bit, int bits, uint32_t n_tiles, const uint32_t *counts,
+                                                     const uint32_t *totals, Pair *out)
 {
-    __shared__ uint32_t place[WAVES][DIGITS];  // where a wavefront's next pair of a digit goes
+    extern __shared__ __align__(16) char shared[];  // [TILE] pairs, [digits] differences, [WAVES][digits] counts
     __shared__ uint32_t lds[WAVES];
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) place[w][threadIdx.x] = 0;
+    const int digits = 1 << bits, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    Pair *sorted = reinterpret_cast<Pair *>(shared);
+    uint32_t *away = reinterpret_cast<uint32_t *>(sorted + TILE);  // a digit's place in the output less its place in the tile
+    uint16_t *place = reinterpret_cast<uint16_t *>(away + digits);  // where a wavefront's next pair of a digit goes in the tile
+    for (int d = threadIdx.x; d < WAVES * digits; d += LANES) place[d] = 0;
     __syncthreads();
     // A wavefront has ITEMS * 64 adjacent pairs, 64 at a time.
     const uint32_t first = blockIdx.x * TILE + wave * (ITEMS * 64) + lane;
-    uint32_t key[ITEMS], row[ITEMS];
+    uint16_t *own = place + wave * digits;
+    Pair pair[ITEMS];
     uint16_t before[ITEMS];  // pairs of the same digit that the wavefront had before
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        const uint32_t i = first + k * 64;
-        const bool here = i < p.n;
-        row[k] = here ? (p.key ? p.row[i] : row_of(p, i)) : 0;
-        key[k] = here ? key_of(p, i, row[k]) : 0;
-        const uint32_t digit = key[k] >> bit & (DIGITS - 1);
-        uint64_t same = __ballot(here);
+    for (int k = 0; k < ITEMS; ++k) pair[k] = pair_of<FROM>(p, std::min(first + k * 64, p.n - 1));
 #pragma unroll
-        for (int j = 0; j < DIGIT; ++j) {
-            const uint64_t set = __ballot(digit >> j & 1);
-            same &= digit >> j & 1 ? set : ~set;
+    for (int k = 0; k < ITEMS; ++k) {
+        const bool here = first + k * 64 < p.n;
+        const uint32_t digit = pair[k].key >> bit & (digits - 1);
+        const uint64_t all = __ballot(here);
+        uint32_t low = static_cast<uint32_t>(all), high = static_cast<uint32_t>(all >> 32);  // lanes that have this lane's digit
+#pragma unroll 2
+        for (int j = 0; j < bits; ++j) {
+            const int32_t own_bit = static_cast<int32_t>(digit << (31 - j)) >> 31;  // all ones or none
+            const uint64_t set = __ballot(own_bit < 0);
+            low &= ~(static_cast<uint32_t>(set) ^ own_bit);
+            high &= ~(static_cast<uint32_t>(set >> 32) ^ own_bit);
         }
-        const int ahead = __popcll(same & ((1ull << lane) - 1));
+        const int ahead = __builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0));
         uint32_t had = 0;
-        if (here) had = place[wave][digit];
+        if (here) had = own[digit];
         in_order();  // all have read before the first lane of each digit writes
-        if (here && ahead == 0) place[wave][digit] = had + __popcll(same);
+        if (here && ahead == 0) own[digit] = static_cast<uint16_t>(had + __popc(low) + __popc(high));
         in_order();
         before[k] = static_cast<uint16_t>(had + ahead);
     }
     __syncthreads();
-    {   // lane = digit: the places of the wavefronts one after the other, from the digit's and the tile's
-        uint32_t all;
-        uint32_t at = sum_before(totals[threadIdx.x], all, lds) + counts[threadIdx.x * n_tiles + blockIdx.x];
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const uint32_t had = place[w][threadIdx.x];
-            place[w][threadIdx.x] = at;
-            at += had;
+    // Lanes are digits: places in the output from the digits' totals and the tiles before, places in the tile from its own counts.
+    uint32_t in_all = 0, in_tile = 0;
+    for (int d0 = 0; d0 < digits; d0 += LANES) {
+        const int d = d0 + threadIdx.x;
+        uint32_t sum = 0, all;
+        if (d < digits)
+            for (int w = 0; w < WAVES; ++w) sum += place[w * digits + d];
+        const uint32_t to = in_all + sum_before(d < digits ? totals[d] : 0, all, lds);
+        in_all += all;
+        uint32_t at = in_tile + sum_before(sum, all, lds);
+        in_tile += all;
+        if (d < digits) {
+            away[d] = to + counts[static_cast<uint32_t>(d) * n_tiles + blockIdx.x] - at;
+            for (int w = 0; w < WAVES; ++w) {
+                const uint32_t had = place[w * digits + d];
+                place[w * digits + d] = static_cast<uint16_t>(at);
+                at += had;
+            }
         }
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k)
-        if (first + k * 64 < p.n) {
-            const uint32_t to = place[wave][key[k] >> bit & (DIGITS - 1)] + before[k];
-            key_out[to] = key[k];
-            row_out[to] = row[k];
-        }
+        if (first + k * 64 < p.n) sorted[own[pair[k].key >> bit & (digits - 1)] + before[k]] = pair[k];
+    __syncthreads();
+    const uint32_t some = std::min<uint32_t>(TILE, p.n - blockIdx.x * TILE);
+    auto write = [&](uint32_t i) {
+        const Pair o = sorted[i];
+        out[away[o.key >> bit & (digits - 1)] + i] = o;
+    };
+    if (some == TILE) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) write(k * LANES + threadIdx.x);
+    } else {
+        for (uint32_t i = threadIdx.x; i < some; i += LANES) write(i);
+    }
 }
 
 // ---- the sums
@@ -335,7 +373,7 @@ __global__ __launch_bounds__(THREADS) void zero_kernel(T *to, int64_t n)
 }
 
 struct Sorted {
-    const uint32_t *key, *row;
+    const Pair *pair;
     uint32_t n, n_vectors;  // pairs whose key is n_vectors stand for nothing
     uint32_t chunk, n_chunks;
 };
@@ -350,9 +388,9 @@ __global__ __launch_bounds__(THREADS) void sum_kernel(Sorted s, int dim, const T
     const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * V;
     if (group >= s.n_chunks || c >= dim) return;
     const uint32_t first = group * s.chunk, end = std::min(s.n, first + s.chunk);
-    uint32_t key = s.key[first];
+    uint32_t key = s.pair[first].key;
     if (key >= s.n_vectors) return;
-    bool begun = first > 0 && s.key[first - 1] == key;  // before this chunk
+    bool begun = first > 0 && s.pair[first - 1].key == key;  // before this chunk
     float a[V] = {};
     auto store = [&](bool ends) {
         if (begun || !ends) {
@@ -373,12 +411,13 @@ __global__ __launch_bounds__(THREADS) void sum_kernel(Sorted s, int dim, const T
     for (uint32_t i = first; i < end; i += AHEAD) {
         uint32_t keys[AHEAD];
         Pack<T, V> p[AHEAD];
+        Pair pair[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) keys[j] = i + j < end ? s.key[i + j] : s.n_vectors;
+        for (int j = 0; j < AHEAD; ++j) pair[j] = s.pair[std::min(i + j, end - 1)];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const uint32_t row = keys[j] < s.n_vectors ? s.row[i + j] : 0;
-            p[j] = *reinterpret_cast<const Pack<T, V> *>(grad + row * grad_stride + c);
+            keys[j] = i + j < end ? pair[j].key : s.n_vectors;
+            p[j] = *reinterpret_cast<const Pack<T, V> *>(grad + pair[j].row * grad_stride + c);
         }
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
@@ -394,7 +433,7 @@ __global__ __launch_bounds__(THREADS) void sum_kernel(Sorted s, int dim, const T
             for (int k = 0; k < V; ++k) a[k] += widen(p[j].v[k]);
         }
     }
-    store(end == s.n || s.key[end] != key);
+    store(end == s.n || s.pair[end].key != key);
 }
 
 // A group of lanes for each chunk: if a run begins in the chunk and goes on, all its parts.
@@ -405,13 +444,13 @@ __global__ __launch_bounds__(THREADS) void join_kernel(Sorted s, int dim, const 
     const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * V;
     if (group + 1 >= s.n_chunks || c >= dim) return;  // no run goes on from the last chunk
     const uint32_t first = group * s.chunk, end = first + s.chunk;
-    const uint32_t key = s.key[end - 1];
-    if (key >= s.n_vectors || s.key[end] != key) return;
-    if (s.key[first] == key && first > 0 && s.key[first - 1] == key) return;
+    const uint32_t key = s.pair[end - 1].key;
+    if (key >= s.n_vectors || s.pair[end].key != key) return;
+    if (s.pair[first].key == key && first > 0 && s.pair[first - 1].key == key) return;
     float a[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) a[k] = parts[(2 * static_cast<int64_t>(group) + 1) * dim + c + k];
-    for (uint32_t g = group + 1; g < s.n_chunks && s.key[g * s.chunk] == key; ++g)
+    for (uint32_t g = group + 1; g < s.n_chunks && s.pair[g * s.chunk].key == key; ++g)
 #pragma unroll
         for (int k = 0; k < V; ++k) a[k] += parts[2 * static_cast<int64_t>(g) * dim + c + k];
     Pack<T, V> p;
@@ -490,8 +529,8 @@ hipError_t embed(const head_ids &ids, int64_t dim, const T *table, int64_t table
 // The parts of the workspace of the backward pass, in bytes from its start.
 struct GradPlan {
     uint32_t n, n_tiles, chunk, n_chunks;
-    int passes;
-    int64_t key[2], row[2], counts, totals, parts, bytes;
+    int passes, bits;
+    int64_t pair[2], counts, totals, parts, bytes;
 };
 
 GradPlan plan_grad(const head_ids &ids, int64_t dim)
@@ -499,9 +538,11 @@ GradPlan plan_grad(const head_ids &ids, int64_t dim)
     GradPlan p{};
     p.n = static_cast<uint32_t>(ids.n_rows * ids.n_ids);
     p.n_tiles = static_cast<uint32_t>(ceil_div(p.n, TILE));
-    p.passes = 1;
-    while (ids.n_vectors >> (DIGIT * p.passes)) ++p.passes;
-    p.chunk = 64;
+    int bits = 1;
+    while (ids.n_vectors >> bits) ++bits;
+    p.passes = static_cast<int>(ceil_div(bits, MAX_DIGIT));
+    p.bits = static_cast<int>(ceil_div(bits, p.passes));
+    p.chunk = 128;
     p.n_chunks = static_cast<uint32_t>(ceil_div(p.n, p.chunk));
     int64_t at = 0;
     auto part = [&](int64_t bytes) {
@@ -509,12 +550,9 @@ GradPlan plan_grad(const head_ids &ids, int64_t dim)
         at += round_up(bytes, 256);
         return from;
     };
-    for (int k = 0; k < 2; ++k) {
-        p.key[k] = part(int64_t{4} * p.n);
-        p.row[k] = part(int64_t{4} * p.n);
-    }
-    p.counts = part(int64_t{4} * DIGITS * p.n_tiles);
-    p.totals = part(4 * DIGITS);
+    for (int64_t &pair : p.pair) pair = part(int64_t{sizeof(Pair)} * p.n);
+    p.counts = part((int64_t{4} << p.bits) * p.n_tiles);
+    p.totals = part(int64_t{4} << p.bits);
     p.parts = part(int64_t{8} * p.n_chunks * dim);
     p.bytes = p.n ? at : 0;
     return p;
@@ -541,19 +579,23 @@ hipError_t embed_grad(const head_ids &ids, int64_t dim, const T *grad, int64_t g
         p.magic = static_cast<uint32_t>((uint64_t{1} << (31 + k)) / p.n_ids + 1);
         p.shift = static_cast<uint32_t>(k - 1);
     }
-    for (int pass = 0; pass < plan.passes; ++pass) {
-        if (pass > 0) {
-            p.key = words(plan.key[(pass - 1) % 2]);
-            p.row = words(plan.row[(pass - 1) % 2]);
-        }
-        hipLaunchKernelGGL(count_kernel, dim3(plan.n_tiles), dim3(THREADS), 0, stream, p, pass * DIGIT, plan.n_tiles, words(plan.counts));
-        hipLaunchKernelGGL(tiles_kernel, dim3(DIGITS), dim3(THREADS), 0, stream, plan.n_tiles, words(plan.counts), words(plan.totals));
-        hipLaunchKernelGGL(move_kernel, dim3(plan.n_tiles), dim3(THREADS), 0, stream, p, pass * DIGIT, plan.n_tiles, words(plan.counts),
-                           words(plan.totals), words(plan.key[pass % 2]), words(plan.row[pass % 2]));
-        if (const hipError_t e = hipGetLastError()) return e;
-    }
-    const int last = (plan.passes - 1) % 2;
-    const Sorted s{words(plan.key[last]), words(plan.row[last]), plan.n, static_cast<uint32_t>(ids.n_vectors), plan.chunk, plan.n_chunks};
+    auto pairs = [&](int which) { return reinterpret_cast<Pair *>(workspace + plan.pair[which]); };
+    const size_t lds = move_lds(plan.bits);
+    auto pass = [&](auto FROM, int k) {
+        if (const hipError_t e = allow_lds<move_kernel<FROM()>>(move_lds(MAX_DIGIT))) return e;
+        const int bit = k * plan.bits;
+        hipLaunchKernelGGL((count_kernel<FROM()>), dim3(plan.n_tiles), dim3(LANES), 0, stream, p, bit, plan.bits, plan.n_tiles,
+                           words(plan.counts));
+        hipLaunchKernelGGL(tiles_kernel, dim3(1u << plan.bits), dim3(LANES), 0, stream, plan.n_tiles, words(plan.counts), words(plan.totals));
+        hipLaunchKernelGGL((move_kernel<FROM()>), dim3(plan.n_tiles), dim3(LANES), lds, stream, p, bit, plan.bits, plan.n_tiles,
+                           words(plan.counts), words(plan.totals), pairs(k % 2));
+        p.pair = pairs(k % 2);
+        return hipGetLastError();
+    };
+    hipError_t e = ids.offset ? pass(std::integral_constant<int, IDS_AND_OFFSETS>(), 0) : pass(std::integral_constant<int, IDS>(), 0);
+    for (int k = 1; k < plan.passes && e == hipSuccess; ++k) e = pass(std::integral_constant<int, LAST_PASS>(), k);
+    if (e != hipSuccess) return e;
+    const Sorted s{pairs((plan.passes - 1) % 2), plan.n, static_cast<uint32_t>(ids.n_vectors), plan.chunk, plan.n_chunks};
     float *parts = reinterpret_cast<float *>(workspace + plan.parts);
     const uint64_t bits = address(grad) | address(out) | static_cast<uint64_t>(grad_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));
     return by_piece<T>(piece(bits, sizeof(T)), [&](auto V) {

@@ -16,7 +16,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cstdint>
 
 #include "head_device.hpp"
@@ -591,20 +590,6 @@ constexpr size_t lds_bytes()
 {
     // two steps' tiles; what tiles are finished with, at most: of the wavefronts [WAVES_M][N] pairs, and twice [3][M] numbers
     return 2 * (S::M + S::N) * STEP + (2 * S::WAVES_M * S::N + 6 * S::M) * sizeof(float);
-}
-
-// More than 64 KB of LDS has to be asked for, once for each kernel and device.
-template <auto *KERNEL>
-hipError_t allow_lds(size_t bytes)
-{
-    constexpr int DEVICES = 64;
-    static std::atomic<bool> done[DEVICES];
-    int device = -1;
-    if (const hipError_t e = hipGetDevice(&device)) return e;
-    if (device >= 0 && device < DEVICES && done[device].load(std::memory_order_relaxed)) return hipSuccess;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-    if (e == hipSuccess && device >= 0 && device < DEVICES) done[device].store(true, std::memory_order_relaxed);
-    return e;
 }
 
 template <class S, auto *KERNEL, class... Args>
