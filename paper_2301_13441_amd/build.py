@@ -11,6 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libforest_hip.so")
 SHORT_CALL = os.path.join(HERE, "_short_call.so")  # CPython extension: predict() as one native call
+HEAD_CALL = os.path.join(HERE, "_head_call.so")    # the same for the head's operators
 SOURCES = ["forest_pack.cpp", "forest_api_host.cpp", "forest_api.cpp", "forest_kernels.hip", "forest_kernels_reg.hip",
            "forest_kernels_rank.hip", "forest_kernels_ranklds.hip", "forest_kernels_rankbank.hip", "forest_kernels_split.hip",
            "forest_kernels_walk.hip", "forest_kernels_deep.hip", "forest_probe.hip",
@@ -59,6 +60,14 @@ def ranklds_variant_flags(flags: list[str], verbose: bool = False) -> list[str]:
 
 
 def build_short_call(verbose: bool = False) -> str:
+    return _build_extension("short_call.cpp", SHORT_CALL, verbose)
+
+
+def build_head_call(verbose: bool = False) -> str:
+    return _build_extension("head_call.cpp", HEAD_CALL, verbose)
+
+
+def _build_extension(src: str, out: str, verbose: bool) -> str:
     """Host code against torch's headers and libraries; importing torch brings the libraries it needs."""
     import sysconfig
 
@@ -67,19 +76,19 @@ def build_short_call(verbose: bool = False) -> str:
     include = [*cpp_extension.include_paths(), "/opt/rocm/include", sysconfig.get_paths()["include"]]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{d}" for d in include),
-           os.path.join(CSRC, "short_call.cpp"), "-o", SHORT_CALL, "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
+           os.path.join(CSRC, src), "-o", out, "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
            "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    return SHORT_CALL
+    return out
 
 
 def build(verbose: bool = False, extra: list[str] | None = None) -> str:
     os.makedirs(OBJ, exist_ok=True)
     extra = list(extra or [])
-    with ThreadPoolExecutor(max_workers=len(SOURCES) + 2) as pool:
-        short_call = pool.submit(build_short_call, verbose)
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 3) as pool:
+        short_call, head_call = pool.submit(build_short_call, verbose), pool.submit(build_head_call, verbose)
         variant = pool.submit(ranklds_variant_flags, [*FLAGS, *extra], verbose)
         others = [s for s in SOURCES if s != RANKLDS]
         objs = list(pool.map(lambda s: _compile(s, extra, verbose), others))
@@ -88,7 +97,8 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
-        short_call.result()  # last: the library does not need it
+        short_call.result()  # last: the library does not need them
+        head_call.result()
     return LIB
 
 

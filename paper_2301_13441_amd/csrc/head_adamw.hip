@@ -2,8 +2,8 @@
 //
 // Bound by memory: 28 bytes a value with float32 gradients and states, 14 with bfloat16 gradients and states in 8 bits.
 // A launch takes up to TENSORS tensors, whose addresses go by value with its arguments: there is no table on the
-// device to keep, and a captured launch carries its own.  A workgroup finds its tensor by the number of its first block of
-// VALUES values and takes one block.  A lane takes 8 adjacent values, so that 16 lanes hold the HEAD_BLOCK = 128 values
+// device to keep, and a captured launch carries its own.  A workgroup finds its tensor by the number of its block, the
+// tensors' blocks being counted through.  A lane takes 8 adjacent values, so that 16 lanes hold the HEAD_BLOCK = 128 values
 // of an 8-bit scale and their largest magnitude is four exchanges away.
 #include <hip/hip_runtime.h>
 
@@ -18,9 +18,9 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int EACH = 8;                   // values of a lane
-constexpr int VALUES = THREADS * EACH;    // values of a workgroup
+constexpr int VALUES_EACH = 16;           // of adamw_values_kernel, which reads two bytes for each
 constexpr int TENSORS = 40;               // tensors of a launch
-constexpr int64_t MAX_GRID = 1 << 22;     // workgroups of a launch: 2^30 threads
+constexpr int64_t MAX_GRID = 8192;      // workgroups of a launch, several for each CU: each makes its table once
 static_assert(HEAD_BLOCK == 16 * EACH, "a scale's values are those of 16 lanes");
 
 struct Tensor {
@@ -49,13 +49,25 @@ __host__ __device__ inline uint32_t hash(uint32_t x)  // a multiply and xor-shif
     return x ^ (x >> 16);
 }
 
-// What an e4m3 code stands for, times 2^(s - 134).
-__device__ __forceinline__ float decode(uint32_t code, int s)
+template <class T, int N = EACH>
+struct alignas(16) Values {
+    T v[N];
+};
+
+// What the e4m3 codes of a lane stand for, times 2^(s - 134).
+template <int N>
+__device__ __forceinline__ void decode(const Values<uint8_t, N> &code, int s, float (&x)[N])
 {
-    const int exponent = (code >> 3) & 15, digits = code & 7;
-    if ((code & 127) == 127) return __builtin_nanf("");
-    const float y = ldexpf(static_cast<float>(digits + (exponent ? 8 : 0)), (exponent ? exponent : 1) - 144 + s);
-    return code & 128 ? -y : y;
+#pragma unroll
+    for (int w = 0; w < N / 4; ++w) {
+        const uint32_t four = reinterpret_cast<const uint32_t *>(code.v)[w];
+        x[4 * w] = __builtin_amdgcn_cvt_f32_fp8(four, 0);
+        x[4 * w + 1] = __builtin_amdgcn_cvt_f32_fp8(four, 1);
+        x[4 * w + 2] = __builtin_amdgcn_cvt_f32_fp8(four, 2);
+        x[4 * w + 3] = __builtin_amdgcn_cvt_f32_fp8(four, 3);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = ldexpf(x[i], s - 134);
 }
 
 // Scale byte of a block whose largest finite magnitude is `most`: its exponent + 127, at least 1; 0 for a block of zeros.
@@ -84,35 +96,30 @@ __device__ __forceinline__ uint32_t encode(float x, int s, float factor, uint32_
     return code | (x < 0 ? 128u : 0u);
 }
 
-template <class T>
-struct Values {
-    T v[EACH];
-};
-
-// 8 adjacent values, `some` of which exist; `wide`: all do, and their address is whole in 16 bytes or their own length.
-template <class T>
-__device__ __forceinline__ void take(Values<T> &to, const T *from, int some, bool wide)
+// N adjacent values, `some` of which exist; `wide`: all do, and their address is whole in 16 bytes or their own length.
+template <class T, int N>
+__device__ __forceinline__ void take(Values<T, N> &to, const T *from, int some, bool wide)
 {
-    constexpr int P = sizeof(T) * EACH > 16 ? 16 / sizeof(T) : EACH;
+    constexpr int P = sizeof(T) * N > 16 ? 16 / sizeof(T) : N;
     if (wide) {
 #pragma unroll
-        for (int i = 0; i < EACH; i += P) *reinterpret_cast<Pack<T, P> *>(to.v + i) = *reinterpret_cast<const Pack<T, P> *>(from + i);
+        for (int i = 0; i < N; i += P) *reinterpret_cast<Pack<T, P> *>(to.v + i) = *reinterpret_cast<const Pack<T, P> *>(from + i);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) to.v[i] = i < some ? from[i] : T(0);
+    for (int i = 0; i < N; ++i) to.v[i] = i < some ? from[i] : T(0);
 }
-template <class T>
-__device__ __forceinline__ void put(T *to, const Values<T> &from, int some, bool wide)
+template <class T, int N>
+__device__ __forceinline__ void put(T *to, const Values<T, N> &from, int some, bool wide)
 {
-    constexpr int P = sizeof(T) * EACH > 16 ? 16 / sizeof(T) : EACH;
+    constexpr int P = sizeof(T) * N > 16 ? 16 / sizeof(T) : N;
     if (wide) {
 #pragma unroll
-        for (int i = 0; i < EACH; i += P) *reinterpret_cast<Pack<T, P> *>(to + i) = *reinterpret_cast<const Pack<T, P> *>(from.v + i);
+        for (int i = 0; i < N; i += P) *reinterpret_cast<Pack<T, P> *>(to + i) = *reinterpret_cast<const Pack<T, P> *>(from.v + i);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
+    for (int i = 0; i < N; ++i)
         if (i < some) to[i] = from.v[i];
 }
 
@@ -127,7 +134,8 @@ __device__ __forceinline__ float block_most(const float (&x)[EACH])
     return most;
 }
 
-// The tensor of a block, and the block's first value in it.
+// The tensor of a block, and a lane's first value in it.
+template <int N>
 __device__ __forceinline__ int find(const Batch &b, int64_t block, int64_t &at)
 {
     int t = 0, end = b.count;  // the last tensor that begins at the block or before
@@ -136,7 +144,7 @@ __device__ __forceinline__ int find(const Batch &b, int64_t block, int64_t &at)
         if (b.first[mid] <= block) t = mid;
         else end = mid;
     }
-    at = (block - b.first[t]) * VALUES + static_cast<int64_t>(threadIdx.x) * EACH;
+    at = (block - b.first[t]) * (THREADS * N) + static_cast<int64_t>(threadIdx.x) * N;
     return t;
 }
 
@@ -151,7 +159,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Batch b, const Num
     const int64_t blocks = b.first[b.count];
     for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
         int64_t at;
-        const Tensor &t = b.tensor[find(b, block, at)];
+        const Tensor &t = b.tensor[find<EACH>(b, block, at)];
         const int some = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(EACH, t.n - at)));
         const bool wide = some == EACH && t.wide;
         if (!EIGHT && some == 0) continue;
@@ -164,12 +172,10 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Batch b, const Num
             take(mc, static_cast<const uint8_t *>(t.m) + at, some, wide);
             take(vc, static_cast<const uint8_t *>(t.v) + at, some, wide);
             const int ms = some ? t.m_scale[at / HEAD_BLOCK] : 0, vs = some ? t.v_scale[at / HEAD_BLOCK] : 0;
+            decode(mc, ms, m.v);
+            decode(vc, vs, v.v);
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                m.v[i] = decode(mc.v[i], ms);
-                v.v[i] = decode(vc.v[i], vs);
-                v.v[i] *= v.v[i];
-            }
+            for (int i = 0; i < EACH; ++i) v.v[i] *= v.v[i];
         } else {
             take(m, static_cast<const float *>(t.m) + at, some, wide);
             take(v, static_cast<const float *>(t.v) + at, some, wide);
@@ -215,32 +221,34 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Batch b, const Num
 // `param` and `copy` are where m and v go.
 __global__ __launch_bounds__(THREADS) void adamw_values_kernel(const Batch b)
 {
+    constexpr int N = VALUES_EACH;
     const int64_t blocks = b.first[b.count];
     for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
         int64_t at;
-        const Tensor &t = b.tensor[find(b, block, at)];
-        const int some = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(EACH, t.n - at)));
-        const bool wide = some == EACH && t.wide;
+        const Tensor &t = b.tensor[find<N>(b, block, at)];
+        const int some = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(N, t.n - at)));
+        const bool wide = some == N && t.wide;
         if (some == 0) continue;
-        Values<uint8_t> mc, vc;
+        Values<uint8_t, N> mc, vc;
         take(mc, static_cast<const uint8_t *>(t.m) + at, some, wide);
         take(vc, static_cast<const uint8_t *>(t.v) + at, some, wide);
-        const int ms = t.m_scale[at / HEAD_BLOCK], vs = t.v_scale[at / HEAD_BLOCK];
-        Values<bf16> m, v;
+        float x[N], root[N];
+        decode(mc, t.m_scale[at / HEAD_BLOCK], x);
+        decode(vc, t.v_scale[at / HEAD_BLOCK], root);
+        Values<bf16, N> m, v;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            m.v[i] = narrow<bf16>(decode(mc.v[i], ms));
-            const float root = decode(vc.v[i], vs);
-            v.v[i] = narrow<bf16>(root * root);
+        for (int i = 0; i < N; ++i) {
+            m.v[i] = narrow<bf16>(x[i]);
+            v.v[i] = narrow<bf16>(root[i] * root[i]);
         }
         put(reinterpret_cast<bf16 *>(t.param) + at, m, some, wide);
         put(t.copy + at, v, some, wide);
     }
 }
 
-// Launches `kernel` for all tensors that have values, TENSORS at a time.
+// Launches for all tensors that have values, TENSORS at a time; a workgroup's block has `values` of them.
 template <class Fill, class Launch>
-hipError_t in_batches(int32_t n_tensors, Fill fill, Launch launch)
+hipError_t in_batches(int32_t n_tensors, int values, Fill fill, Launch launch)
 {
     Batch b{};
     for (int32_t i = 0; i <= n_tensors; ++i) {
@@ -254,7 +262,7 @@ hipError_t in_batches(int32_t n_tensors, Fill fill, Launch launch)
         Tensor &t = b.tensor[b.count];
         fill(i, t);
         if (t.n == 0) continue;
-        b.first[b.count + 1] = b.first[b.count] + ceil_div(t.n, VALUES);
+        b.first[b.count + 1] = b.first[b.count] + ceil_div(t.n, values);
         ++b.count;
     }
     return hipSuccess;
@@ -271,7 +279,7 @@ hipError_t launch_adamw(const head_adamw_rule &rule, const head_adamw_tensor *te
                     static_cast<float>(1 / std::sqrt(1 - std::pow(rule.beta2, step))), static_cast<float>(rule.eps)};
     const uint32_t key = hash(rule.seed + 0x9E3779B9u * static_cast<uint32_t>(rule.step));
     return in_batches(
-        n_tensors,
+        n_tensors, THREADS * EACH,
         [&](int32_t i, Tensor &t) {
             const head_adamw_tensor &s = tensors[i];
             t = Tensor{s.param, s.grad, s.m, s.v, s.m_scale, s.v_scale, static_cast<bf16 *>(s.copy), s.n,
@@ -291,11 +299,11 @@ hipError_t launch_adamw_values(const head_adamw_tensor *tensors, void *const *ou
                                hipStream_t stream)
 {
     return in_batches(
-        n_tensors,
+        n_tensors, THREADS * VALUES_EACH,
         [&](int32_t i, Tensor &t) {
             const head_adamw_tensor &s = tensors[i];
             t = Tensor{static_cast<float *>(out_m[i]), nullptr, s.m, s.v, s.m_scale, s.v_scale, static_cast<bf16 *>(out_v[i]), s.n, 0, 0};
-            t.wide = (address(s.m) | address(s.v)) % EACH == 0 && (address(out_m[i]) | address(out_v[i])) % 16 == 0;
+            t.wide = (address(s.m) | address(s.v) | address(out_m[i]) | address(out_v[i])) % 16 == 0;
         },
         [&](const Batch &b, dim3 grid) { hipLaunchKernelGGL(adamw_values_kernel, grid, dim3(THREADS), 0, stream, b); });
 }

@@ -63,7 +63,8 @@ struct Tile {
     static __device__ __forceinline__ int key(int r)
     {
         if constexpr (ALONG) return r / (256 / STEP) % SLOTS;
-        return sizeof(T) == 2 ? r % 4 * 4 : r / 4 % 2 * 8;
+        if constexpr (sizeof(T) == 4) return r / 4 % 2 * 8;
+        return ROWS >= 128 ? r % 4 * 4 : r / 2 % 2 * 4;  // rows of 256 bytes or more lie in the same banks, of 128 every other
     }
 
     const T *from[LOADS];  // this lane's chunks at depth 0; rows past the end are the last one again, of whose results nobody reads
@@ -437,10 +438,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
         const float *own_lse = row_lse + S::row(0, 0), *own_grad = row_grad + S::row(0, 0);
         const int *own_target = row_target + S::row(0, 0);
         // Few rows have their target among a wavefront's classes: a bit for each of its rows that does.
-        uint64_t targets[S::MT / 2];
+        uint64_t targets[(S::MT + 1) / 2];
 #pragma unroll
-        for (int k = 0; k < S::MT / 2; ++k) {
-            const int target = row_target[S::wave_m() * (S::MT * 32) + k * 64 + threadIdx.x % 64];
+        for (int k = 0; k < (S::MT + 1) / 2; ++k) {
+            const int r = k * 64 + threadIdx.x % 64;
+            const int target = r < S::MT * 32 ? row_target[S::wave_m() * (S::MT * 32) + r] : -1;
             targets[k] = __ballot(target >= 0 && target / (S::NT * 32) == S::wave_n());
         }
         char *at = to;  // a lane's results are of four rows in every eight
@@ -571,9 +573,15 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t stride
 
 // ---- what a call launches
 
-// A workgroup of 4 wavefronts and tiles of 128 x 128, of which a CU has two; or, where bfloat16 products have so many tiles, one of 8
+// A workgroup of 4 wavefronts and tiles of 128 x 128, of which a CU has two; tiles of 64 x 64 where there are so few that their number is
+// not what counts but the time of one (1,021 rows, 10 classes: 22 us for all of head_cross_entropy_grad, against 42); or, where bfloat16 products have so many tiles, one of 8
 // and 256 x 256: half the traffic to LDS, and a third less from it, for as many products (16,384 x 65,536 logits over 512 values: 1.32
 // ms, against 1.58).  float32 products are bound by the matrix core, and gain nothing (loss_f32's logits: 257 us, against 255).
+struct Tiny {
+    static constexpr int TILE = 64, RESIDENT = 512;
+    template <bool NEXT>
+    using Of = Shape<64, 64, 2, 2, NEXT>;
+};
 struct Small {
     static constexpr int TILE = 128, RESIDENT = 512;
     template <bool NEXT>
@@ -602,9 +610,11 @@ hipError_t launch_product(dim3 grid, hipStream_t stream, Args... args)
 
 dim3 grid_of(int64_t n, int64_t most = 8192) { return dim3(static_cast<uint32_t>(std::max<int64_t>(1, std::min(n, most)))); }
 
+enum { TINY, SMALL, LARGE };
+
 // The parts of a call's workspace, in bytes from its start; and its sizes.
 struct Plan {
-    bool large;                     // Large or Small, and what they are
+    int size;                       // and what it is
     int64_t tile, resident;
     int64_t packed;                 // values of a packed row
     int64_t hidden = -1, weight = -1;  // packed operands; -1: used where they are
@@ -626,9 +636,10 @@ Plan plan_operands(const head_classes &c)
 {
     Plan p{};
     p.hidden = p.weight = -1;
-    p.large = c.dtype == HEAD_BF16 && ceil_div(c.n_rows, Large::TILE) * ceil_div(c.n_classes, Large::TILE) >= Large::RESIDENT;
-    p.tile = p.large ? Large::TILE : Small::TILE;
-    p.resident = p.large ? Large::RESIDENT : Small::RESIDENT;
+    auto tiles = [&](int64_t tile) { return ceil_div(c.n_rows, tile) * ceil_div(c.n_classes, tile); };
+    p.size = c.dtype == HEAD_BF16 && tiles(Large::TILE) >= Large::RESIDENT ? LARGE : tiles(Small::TILE) < Small::RESIDENT / 4 ? TINY : SMALL;
+    p.tile = p.size == LARGE ? Large::TILE : p.size == TINY ? Tiny::TILE : Small::TILE;
+    p.resident = p.size == LARGE ? Large::RESIDENT : p.size == TINY ? Tiny::RESIDENT : Small::RESIDENT;
     const int e = value_bytes(c.dtype);
     p.packed = round_up(c.dim, 16 / e);
     auto whole = [&](const void *at, int64_t stride) { return (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(c.dim * e)) % 16 == 0; };
@@ -647,10 +658,10 @@ Plan plan_forward(const head_classes &c)
     return p;
 }
 
-// Parts of a sum of `depth` such that `tiles` tiles of each fill the device, each part having at least 8 steps.
+// Parts of a sum of `depth` such that `tiles` tiles of each fill the device, each part having at least 2 steps.
 int64_t splits_of(int64_t tiles, int64_t resident, int64_t depth, int64_t step)
 {
-    return std::max<int64_t>(1, std::min(resident / std::max<int64_t>(1, tiles), ceil_div(depth, 8 * step)));
+    return std::max<int64_t>(1, std::min(resident / std::max<int64_t>(1, tiles), ceil_div(depth, 2 * step)));
 }
 
 Plan plan_backward(const head_classes &c)
@@ -779,8 +790,11 @@ hipError_t launch_cross_entropy(const head_classes &c, float *loss, float *lse, 
 {
     char *w = static_cast<char *>(workspace);
     const Plan p = plan_forward(c);
-    if (c.dtype == HEAD_F32) return forward<float, Small>(c, p, loss, lse, w, stream);
-    return p.large ? forward<bf16, Large>(c, p, loss, lse, w, stream) : forward<bf16, Small>(c, p, loss, lse, w, stream);
+    if (c.dtype == HEAD_F32)
+        return p.size == TINY ? forward<float, Tiny>(c, p, loss, lse, w, stream) : forward<float, Small>(c, p, loss, lse, w, stream);
+    return p.size == LARGE  ? forward<bf16, Large>(c, p, loss, lse, w, stream)
+           : p.size == TINY ? forward<bf16, Tiny>(c, p, loss, lse, w, stream)
+                            : forward<bf16, Small>(c, p, loss, lse, w, stream);
 }
 
 int64_t cross_entropy_grad_bytes(const head_classes &c) { return c.n_rows ? plan_backward(c).bytes : 0; }
@@ -790,12 +804,15 @@ hipError_t launch_cross_entropy_grad(const head_classes &c, const float *lse, co
 {
     char *w = static_cast<char *>(workspace);
     const Plan p = plan_backward(c);
-    if (c.dtype == HEAD_F32)
-        return backward<float, Small>(c, p, lse, grad_loss, static_cast<float *>(grad_hidden), static_cast<float *>(grad_weight), grad_bias, w,
-                                      stream);
+    if (c.dtype == HEAD_F32) {
+        float *gh = static_cast<float *>(grad_hidden), *gw = static_cast<float *>(grad_weight);
+        return p.size == TINY ? backward<float, Tiny>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream)
+                              : backward<float, Small>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream);
+    }
     bf16 *gh = static_cast<bf16 *>(grad_hidden), *gw = static_cast<bf16 *>(grad_weight);
-    return p.large ? backward<bf16, Large>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream)
-                   : backward<bf16, Small>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream);
+    return p.size == LARGE  ? backward<bf16, Large>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream)
+           : p.size == TINY ? backward<bf16, Tiny>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream)
+                            : backward<bf16, Small>(c, p, lse, grad_loss, gh, gw, grad_bias, w, stream);
 }
 
 }  // namespace head_impl

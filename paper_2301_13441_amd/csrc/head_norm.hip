@@ -21,7 +21,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_GRID = 1 << 22;       // workgroups of the forward pass: 2^30 threads, a grid's axis has room for 2^32
-constexpr int MAX_WORKGROUPS = 1024;  // of the backward pass: rows of its workspace
+constexpr int MAX_WORKGROUPS = 768;   // of the backward pass, three for each of 256 CUs: rows of its workspace
 
 template <int LANES>
 __device__ __forceinline__ float team_sum(float v, float *lds)
@@ -50,58 +50,80 @@ __device__ __forceinline__ int column(int i)
     return (i * LANES + static_cast<int>(threadIdx.x % LANES)) * V;
 }
 
-template <class T, int V, int LANES, int N>
+// A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.
+template <class T, int V, int LANES, int N, int ROWS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, const T *x, int64_t x_stride, const float *weight,
                                                        const float *bias, float eps, T *y, float *mean, float *rstd)
 {
     __shared__ float lds[THREADS / 64];
     constexpr int TEAMS = THREADS / LANES;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * TEAMS;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * TEAMS; first < n_rows; first += step) {
-        const int64_t row = first + threadIdx.x / LANES;
-        const bool here = row < n_rows;
-        const T *from = x + (here ? row : 0) * x_stride;
-        float a[N][V];
-        float sum = 0;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * TEAMS * ROWS;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * TEAMS * ROWS; first < n_rows; first += step) {
+        const int64_t row0 = first + threadIdx.x / LANES;  // and every TEAMS rows from there
+        float a[ROWS][N][V], m[ROWS], r[ROWS];
+        Pack<T, V> p[ROWS][N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = column<V, LANES>(i);
-            Pack<T, V> p{};
-            if (c < dim) p = *reinterpret_cast<const Pack<T, V> *>(from + c);
+        for (int k = 0; k < ROWS; ++k) {
+            const T *from = x + std::min(row0 + k * TEAMS, n_rows - 1) * x_stride;
 #pragma unroll
-            for (int k = 0; k < V; ++k) sum += a[i][k] = widen(p.v[k]);
+            for (int i = 0; i < N; ++i) {
+                const int c = column<V, LANES>(i);
+                p[k][i] = *reinterpret_cast<const Pack<T, V> *>(from + (c < dim ? c : 0));
+            }
         }
-        const float m = team_sum<LANES>(sum, lds) / dim;
-        float squares = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (column<V, LANES>(i) < dim)
+        for (int k = 0; k < ROWS; ++k) {
+            float sum = 0;
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    a[i][k] -= m;
-                    squares = fmaf(a[i][k], a[i][k], squares);
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum += a[k][i][j] = column<V, LANES>(i) < dim ? widen(p[k][i].v[j]) : 0.0f;
+            m[k] = team_sum<LANES>(sum, lds) / dim;
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            float squares = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    a[k][i][j] -= m[k];
+                    squares = column<V, LANES>(i) < dim ? fmaf(a[k][i][j], a[k][i][j], squares) : squares;
                 }
-        const float r = 1.0f / sqrtf(team_sum<LANES>(squares, lds) / dim + eps);
-        if (!here) continue;
-        T *to = y + row * dim;
+            r[k] = 1.0f / sqrtf(team_sum<LANES>(squares, lds) / dim + eps);
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = column<V, LANES>(i);
             if (c < dim) {
-                Pack<T, V> p;
+                float w[V], b[V];
 #pragma unroll
-                for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(fmaf(a[i][k] * r, weight[c + k], bias ? bias[c + k] : 0.0f));
-                *reinterpret_cast<Pack<T, V> *>(to + c) = p;
+                for (int j = 0; j < V; ++j) {
+                    w[j] = weight[c + j];
+                    b[j] = bias ? bias[c + j] : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    Pack<T, V> o;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) o.v[j] = narrow<T>(fmaf(a[k][i][j] * r[k], w[j], b[j]));
+                    const int64_t row = row0 + k * TEAMS;
+                    if (row < n_rows) *reinterpret_cast<Pack<T, V> *>(y + row * dim + c) = o;
+                }
             }
         }
-        if (threadIdx.x % LANES == 0) {
-            mean[row] = m;
-            rstd[row] = r;
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t row = row0 + k * TEAMS;
+            if (threadIdx.x % LANES == 0 && row < n_rows) {
+                mean[row] = m[k];
+                rstd[row] = r[k];
+            }
         }
     }
 }
 
-template <class T, int V, int LANES, int N>
+template <class T, int V, int LANES, int N, int ROWS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(int64_t n_rows, int dim, const T *grad, int64_t grad_stride, const T *x,
                                                             int64_t x_stride, const float *weight, const float *mean,
                                                             const float *rstd, T *grad_x, float *parts)
@@ -113,50 +135,59 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(int64_t n_rows, int 
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
+        for (int j = 0; j < V; ++j) {
             const int c = column<V, LANES>(i);
-            w[i][k] = c < dim ? weight[c + k] : 0.0f;
+            w[i][j] = c < dim ? weight[c + j] : 0.0f;
         }
     // Every team makes the same number of rounds: the sums of a whole workgroup meet in barriers.
-    const int64_t step = static_cast<int64_t>(gridDim.x) * TEAMS;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * TEAMS; first < n_rows; first += step) {
-        const int64_t row = first + threadIdx.x / LANES;
-        const bool here = row < n_rows;
-        const float m = here ? mean[row] : 0.0f, r = here ? rstd[row] : 0.0f;
-        float g[N][V], u[N][V], along = 0, across = 0;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * TEAMS * ROWS;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * TEAMS * ROWS; first < n_rows; first += step) {
+        const int64_t row0 = first + threadIdx.x / LANES;  // and every TEAMS rows from there
+        Pack<T, V> pg[ROWS][N], px[ROWS][N];
+        float m[ROWS], r[ROWS];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = column<V, LANES>(i);
-            const bool in = here && c < dim;
-            Pack<T, V> pg{}, px{};
-            if (in) {
-                pg = *reinterpret_cast<const Pack<T, V> *>(grad + row * grad_stride + c);
-                px = *reinterpret_cast<const Pack<T, V> *>(x + row * x_stride + c);
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                g[i][k] = widen(pg.v[k]);
-                u[i][k] = in ? (widen(px.v[k]) - m) * r : 0.0f;
-                dw[i][k] = fmaf(g[i][k], u[i][k], dw[i][k]);
-                db[i][k] += g[i][k];
-                g[i][k] *= w[i][k];
-                along += g[i][k];
-                across = fmaf(g[i][k], u[i][k], across);
-            }
-        }
-        along = team_sum<LANES>(along, lds) / dim;
-        across = team_sum<LANES>(across, lds) / dim;
-        if (here)
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t row = row0 + k * TEAMS;
+            const bool here = row < n_rows;
+            m[k] = here ? mean[row] : 0.0f;
+            r[k] = here ? rstd[row] : 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int c = column<V, LANES>(i);
-                if (c < dim) {
-                    Pack<T, V> p;
-#pragma unroll
-                    for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(r * (g[i][k] - along - u[i][k] * across));
-                    *reinterpret_cast<Pack<T, V> *>(grad_x + row * dim + c) = p;
+                pg[k][i] = px[k][i] = Pack<T, V>{};  // nothing is added where g is 0
+                if (here && c < dim) {
+                    pg[k][i] = *reinterpret_cast<const Pack<T, V> *>(grad + row * grad_stride + c);
+                    px[k][i] = *reinterpret_cast<const Pack<T, V> *>(x + row * x_stride + c);
                 }
             }
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t row = row0 + k * TEAMS;
+            float g[N][V], u[N][V], along = 0, across = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    g[i][j] = widen(pg[k][i].v[j]);
+                    u[i][j] = (widen(px[k][i].v[j]) - m[k]) * r[k];
+                    dw[i][j] = fmaf(g[i][j], u[i][j], dw[i][j]);
+                    db[i][j] += g[i][j];
+                    g[i][j] *= w[i][j];
+                    along += g[i][j];
+                    across = fmaf(g[i][j], u[i][j], across);
+                }
+            along = team_sum<LANES>(along, lds) / dim;
+            across = team_sum<LANES>(across, lds) / dim;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = column<V, LANES>(i);
+                Pack<T, V> o;
+#pragma unroll
+                for (int j = 0; j < V; ++j) o.v[j] = narrow<T>(r[k] * (g[i][j] - along - u[i][j] * across));
+                if (row < n_rows && c < dim) *reinterpret_cast<Pack<T, V> *>(grad_x + row * dim + c) = o;
+            }
+        }
     }
     float *part = parts + static_cast<int64_t>(blockIdx.x) * 2 * dim;
     // The teams add their sums one after the other.
@@ -167,18 +198,18 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(int64_t n_rows, int 
                 const int c = column<V, LANES>(i);
                 if (c < dim)
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        float a = dw[i][k], b = db[i][k];
+                    for (int j = 0; j < V; ++j) {
+                        float a = dw[i][j], b = db[i][j];
                         if (team > 0) {
-                            a += columns[c + k];
-                            b += columns[dim + c + k];
+                            a += columns[c + j];
+                            b += columns[dim + c + j];
                         }
                         if (team + 1 < TEAMS) {
-                            columns[c + k] = a;
-                            columns[dim + c + k] = b;
+                            columns[c + j] = a;
+                            columns[dim + c + j] = b;
                         } else {
-                            part[c + k] = a;
-                            part[dim + c + k] = b;
+                            part[c + j] = a;
+                            part[dim + c + j] = b;
                         }
                     }
             }
@@ -186,20 +217,22 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(int64_t n_rows, int 
     }
 }
 
-// The columns' sums over the workgroups: 16 columns at a time, 16 lanes on each.
-__global__ __launch_bounds__(THREADS) void norm_columns_kernel(int n_parts, int dim, const float *parts, float *grad_weight,
-                                                               float *grad_bias)
+// The columns' sums over the workgroups: 16 columns at a time, 64 lanes on each.
+__global__ __launch_bounds__(1024) void norm_columns_kernel(int n_parts, int dim, const float *parts, float *grad_weight, float *grad_bias)
 {
-    __shared__ float lds[16][17];
+    __shared__ float lds[64][17];
     const int c = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
     float s = 0;
-    if (c < 2 * dim)
-        for (int p = lane; p < n_parts; p += 16) s += parts[static_cast<int64_t>(p) * 2 * dim + c];
+    if (c < 2 * dim) {
+#pragma unroll 8
+        for (int p = lane; p < n_parts; p += 64) s += parts[static_cast<int64_t>(p) * 2 * dim + c];
+    }
     lds[lane][threadIdx.x % 16] = s;
     __syncthreads();
     if (lane == 0 && c < 2 * dim) {
         float all = 0;
-        for (int p = 0; p < 16; ++p) all += lds[p][threadIdx.x];
+#pragma unroll
+        for (int p = 0; p < 64; ++p) all += lds[p][threadIdx.x];
         (c < dim ? grad_weight : grad_bias)[c < dim ? c : c - dim] = all;
     }
 }
@@ -245,8 +278,9 @@ hipError_t norm(int64_t n_rows, int64_t dim, const T *x, int64_t x_stride, const
 {
     const uint64_t bits = address(x) | address(y) | static_cast<uint64_t>(x_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));
     return by_shape<T>(piece(bits, sizeof(T)), dim, [&](auto V, auto LANES, auto N) {
-        const int64_t teams = THREADS / LANES();
-        hipLaunchKernelGGL((norm_kernel<T, V(), LANES(), N()>), dim3(static_cast<uint32_t>(std::min<int64_t>(ceil_div(n_rows, teams), MAX_GRID))), dim3(THREADS), 0,
+        constexpr int ROWS = V() * N() <= 8 ? 4 : V() * N() <= 16 ? 2 : 1;
+        const int64_t rows = THREADS / LANES() * ROWS;
+        hipLaunchKernelGGL((norm_kernel<T, V(), LANES(), N(), ROWS>), dim3(static_cast<uint32_t>(std::min<int64_t>(ceil_div(n_rows, rows), MAX_GRID))), dim3(THREADS), 0,
                            stream, n_rows, static_cast<int>(dim), x, x_stride, weight, bias, eps, y, mean, rstd);
         return hipGetLastError();
     });
@@ -263,9 +297,10 @@ hipError_t norm_grad(int64_t n_rows, int64_t dim, const T *grad, int64_t grad_st
                           static_cast<uint64_t>(grad_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));
     return by_shape<T>(piece(bits, sizeof(T)), dim, [&](auto V, auto LANES, auto N) {
         const int64_t teams = THREADS / LANES();
-        n_parts = grad_workgroups(ceil_div(n_rows, teams));
+        constexpr int ROWS = V() * N() <= 4 ? 4 : V() * N() <= 8 ? 2 : 1;
+        n_parts = grad_workgroups(ceil_div(n_rows, teams * ROWS));
         const size_t bytes = teams > 1 ? static_cast<size_t>(2 * dim) * sizeof(float) : 0;
-        hipLaunchKernelGGL((norm_grad_kernel<T, V(), LANES(), N()>), dim3(static_cast<uint32_t>(n_parts)), dim3(THREADS), bytes, stream,
+        hipLaunchKernelGGL((norm_grad_kernel<T, V(), LANES(), N(), ROWS>), dim3(static_cast<uint32_t>(n_parts)), dim3(THREADS), bytes, stream,
                            n_rows, static_cast<int>(dim), grad, grad_stride, x, x_stride, weight, mean, rstd, grad_x, parts);
         return hipGetLastError();
     });
@@ -301,7 +336,7 @@ hipError_t launch_layer_norm_grad(int32_t dtype, int64_t n_rows, int64_t dim, co
                             mean, rstd, static_cast<float *>(grad_x), parts, n_parts, stream);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(norm_columns_kernel, dim3(static_cast<uint32_t>(ceil_div(2 * dim, 16))), dim3(THREADS), 0, stream,
+    hipLaunchKernelGGL(norm_columns_kernel, dim3(static_cast<uint32_t>(ceil_div(2 * dim, 16))), dim3(1024), 0, stream,
                        static_cast<int>(n_parts), static_cast<int>(dim), parts, grad_weight, grad_bias);
     return hipGetLastError();
 }

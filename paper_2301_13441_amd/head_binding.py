@@ -10,9 +10,10 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import warnings
 from typing import NamedTuple, Optional
 
-from .binding import load_library
+from .binding import entry_point, load_library
 
 _p = ctypes.c_void_p
 _i32, _i64, _u32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32
@@ -75,6 +76,43 @@ def _lib():
         fn.restype, fn.argtypes = result, args
     _ready = lib
     return lib
+
+
+class _Declines:
+    """In the native calls' place where the extension is missing: the general way is complete without them."""
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+_calls = None
+
+
+def _native():
+    """The calls as one native call each (csrc/head_call.cpp), for plain contiguous tensors on the current stream; None from one of
+    them: it goes the general way."""
+    global _calls
+    if _calls is None:
+        lib = _lib()
+        try:
+            import torch  # noqa: F401 - the extension is linked against its libraries
+            from . import _head_call
+            _head_call.bind(*(entry_point(getattr(lib, name)) for name in (
+                "head_embed", "head_embed_grad_bytes", "head_embed_grad", "head_layer_norm", "head_layer_norm_grad_bytes",
+                "head_layer_norm_grad", "head_cross_entropy_bytes", "head_cross_entropy", "head_cross_entropy_grad_bytes",
+                "head_cross_entropy_grad", "head_adamw", "head_adamw_values")))
+            _calls = _head_call
+        except ImportError as exc:
+            warnings.warn(f"the native calls of the head cannot be imported ({exc}): calls take some microseconds more; "
+                          "build them with `python -m paper_2301_13441_amd.build`", RuntimeWarning, stacklevel=4)
+            _calls = _Declines()
+    return _calls
+
+
+def _done(got, what: str):
+    """What a native call returned, which did not decline."""
+    if type(got) is int:
+        raise HeadError(got, what)
+    return got
 
 
 def _check(code: int, what: str) -> int:
@@ -174,6 +212,10 @@ def head_embed(table, ids, offsets=None, scale: float = 1.0, stream=None):
     offsets: int64 [n_ids] or None (zeros); with the ids of Forest.predict_leaves, the forest's tree_offset[:-1].  A
     negative id, or one without a vector, adds nothing.  Returns [n_rows, dim] of the table's type.
     """
+    if stream is None:
+        got = _native().embed(table, ids, offsets, scale)
+        if got is not None:
+            return _done(got, "head_embed")
     import torch
     _tensor(table, "table", shape=(None, None))
     dtype = _dtype(table, "table")
@@ -187,6 +229,10 @@ def head_embed(table, ids, offsets=None, scale: float = 1.0, stream=None):
 def head_embed_grad(grad, ids, n_vectors: int, offsets=None, scale: float = 1.0, stream=None):
     """The gradient of head_embed's table: [n_vectors, dim] of the type of grad, [n_rows, dim]; zero for vectors that no id
     stands for."""
+    if stream is None:
+        got = _native().embed_grad(grad, ids, n_vectors, offsets, scale)
+        if got is not None:
+            return _done(got, "head_embed_grad")
     import torch
     _tensor(grad, "grad", shape=(None, None))
     dtype = _dtype(grad, "grad")
@@ -206,6 +252,10 @@ def head_embed_grad(grad, ids, n_vectors: int, offsets=None, scale: float = 1.0,
 def head_layer_norm(x, weight, bias=None, eps: float = 1e-5, stream=None):
     """Layer norm of the rows of x, [n_rows, dim] float32 or bfloat16, with weight and bias (or None) float32 [dim].
     Returns (y, mean, rstd): y like x, mean and rstd float32 [n_rows], which the gradient needs."""
+    if stream is None:
+        got = _native().layer_norm(x, weight, bias, eps)
+        if got is not None:
+            return _done(got, "head_layer_norm")
     import torch
     _tensor(x, "x", shape=(None, None))
     dtype, (n, dim) = _dtype(x, "x"), x.shape
@@ -224,6 +274,10 @@ def head_layer_norm(x, weight, bias=None, eps: float = 1e-5, stream=None):
 def head_layer_norm_grad(grad, x, weight, mean, rstd, stream=None):
     """The gradients of head_layer_norm from grad, that of y.  Returns (grad_x, grad_weight, grad_bias): grad_x like x, the others
     float32 [dim]."""
+    if stream is None:
+        got = _native().layer_norm_grad(grad, x, weight, mean, rstd)
+        if got is not None:
+            return _done(got, "head_layer_norm_grad")
     import torch
     _tensor(x, "x", shape=(None, None))
     dtype, (n, dim) = _dtype(x, "x"), x.shape
@@ -263,6 +317,10 @@ def head_cross_entropy(hidden, weight, targets, bias=None, stream=None):
     targets: int32 [n_rows]; a row whose target is no class (-1, say) has loss 0 and no gradient.  Returns (loss, lse),
     float32 [n_rows]: a row's loss, and the logarithm of the sum of its logits' exponentials, which the gradient needs.
     """
+    if stream is None:
+        got = _native().cross_entropy(hidden, weight, targets, bias)
+        if got is not None:
+            return _done(got, "head_cross_entropy")
     import torch
     desc = _classes(hidden, weight, targets, bias)
     lib = _lib()
@@ -279,6 +337,10 @@ def head_cross_entropy_grad(grad_loss, hidden, weight, targets, lse, bias=None, 
     """The gradients of sum_r grad_loss[r] * loss[r] (for the mean loss: 1 / the number of rows with a target), given
     head_cross_entropy's lse for the same arguments.  Returns (grad_hidden, grad_weight, grad_bias): like hidden, like weight,
     and float32 [n_classes], None without a bias."""
+    if stream is None:
+        got = _native().cross_entropy_grad(grad_loss, hidden, weight, targets, lse, bias)
+        if got is not None:
+            return _done(got, "head_cross_entropy_grad")
     import torch
     desc = _classes(hidden, weight, targets, bias)
     n = hidden.shape[0]
@@ -351,6 +413,11 @@ def head_adamw(params, grads, states, step: int, rate: float, beta1: float = 0.9
     kind for all.  step: 1 for the first step.  copies: None, or a bfloat16 tensor or None for each parameter, which becomes a
     copy of the new parameter.  seed: of the 8-bit states' rounding.  No tensor may be in the lists twice.
     """
+    if stream is None:
+        got = _native().adamw(params, grads, states, copies, step, rate, beta1, beta2, eps, decay, seed)
+        if got is not None:
+            _done(got, "head_adamw")
+            return
     import torch
     n = len(params)
     if len(grads) != n or len(states) != n or (copies is not None and len(copies) != n):
@@ -378,6 +445,10 @@ def head_adamw(params, grads, states, step: int, rate: float, beta1: float = 0.9
 
 def head_adamw_values(states, params, stream=None):
     """What 8-bit states stand for: a list of (m, v), bfloat16 tensors of the shapes of params."""
+    if stream is None:
+        got = _native().adamw_values(states, params)
+        if got is not None:
+            return _done(got, "head_adamw_values")
     import torch
     if len(states) != len(params):
         raise ValueError("states and params must be of one length")
