@@ -184,11 +184,13 @@ __global__ __launch_bounds__(THREADS) void sweep_kernel(int64_t n_rows, int dim,
 // A digit has at most MAX_DIGIT bits: as many passes as the largest key needs with that, and as few bits as do with those passes.
 constexpr int MAX_DIGIT = 10;
 constexpr int LANES = 512, WAVES = LANES / 64;
-constexpr int ITEMS = 16;                // pairs of a lane
-constexpr int TILE = LANES * ITEMS;      // pairs of a workgroup: at 9 bits 16 of each digit, 128 bytes that are written together
+// Pairs of a lane.  16: a workgroup's tile has at 9 bits 16 of each digit, 128 bytes that are written together.  4 where there are
+// few, whose tiles are not many either way, and are sorted faster (8,000 pairs: 6 us a pass, against 15).
+constexpr int MANY = 16, FEW = 4;
+constexpr uint32_t FEW_PAIRS = 1 << 20;
 
 // of move_kernel: the tile's pairs, and for a digit its place away and a count for each wavefront; at 9 bits two workgroups of a CU
-constexpr size_t move_lds(int bits) { return TILE * 8 + ((4 + 2 * WAVES) << bits); }
+constexpr size_t move_lds(int items, int bits) { return LANES * items * 8 + ((4 + 2 * WAVES) << bits); }
 
 struct Pair {
     uint32_t key, row;
@@ -216,9 +218,10 @@ __device__ __forceinline__ Pair pair_of(const Pairs &p, uint32_t i)
     return Pair{static_cast<uint32_t>(id >= 0 && v >= 0 && v < p.s.n_vectors ? v : p.s.n_vectors), row};
 }
 
-template <int FROM>
+template <int FROM, int ITEMS>
 __global__ __launch_bounds__(LANES) void count_kernel(Pairs p, int bit, int bits, uint32_t n_tiles, uint32_t *counts)
 {
+    constexpr int TILE = LANES * ITEMS;
     __shared__ uint32_t count[1 << MAX_DIGIT];
     const int digits = 1 << bits;
     for (int d = threadIdx.x; d < digits; d += LANES) count[d] = 0;
@@ -279,10 +282,11 @@ __device__ __forceinline__ void in_order()
 }
 
 // A tile is sorted by the digit in LDS and then goes out in that order, so that neighbours write neighbouring places.
-template <int FROM>
+template <int FROM, int ITEMS>
 __global__ __launch_bounds__(LANES, 4) void move_kernel(Pairs p, int bit, int bits, uint32_t n_tiles, const uint32_t *counts,
-                                                     const uint32_t *totals, Pair *out)
+                                                        const uint32_t *totals, Pair *out)
 {
+    constexpr int TILE = LANES * ITEMS;
     extern __shared__ __align__(16) char shared[];  // [TILE] pairs, [digits] differences, [WAVES][digits] counts
     __shared__ uint32_t lds[WAVES];
     const int digits = 1 << bits, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
@@ -436,27 +440,71 @@ __global__ __launch_bounds__(THREADS) void sum_kernel(Sorted s, int dim, const T
     store(end == s.n || s.pair[end].key != key);
 }
 
-// A group of lanes for each chunk: if a run begins in the chunk and goes on, all its parts.
+// A group of lanes for each chunk: if a run begins in the chunk and goes on, all its parts.  The parts of a long run (a vector
+// that very many rows have) are added by the wavefront's groups together, each in turn and several on their way at a time.
 template <class T, int V>
 __global__ __launch_bounds__(THREADS) void join_kernel(Sorted s, int dim, const float *parts, float scale, T *out, int lanes)
 {
+    constexpr uint32_t AHEAD = 8;
     const uint32_t group = (blockIdx.x * THREADS + threadIdx.x) / lanes;
-    const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * V;
-    if (group + 1 >= s.n_chunks || c >= dim) return;  // no run goes on from the last chunk
-    const uint32_t first = group * s.chunk, end = first + s.chunk;
-    const uint32_t key = s.pair[end - 1].key;
-    if (key >= s.n_vectors || s.pair[end].key != key) return;
-    if (s.pair[first].key == key && first > 0 && s.pair[first - 1].key == key) return;
-    float a[V];
+    const int c = (blockIdx.y * lanes + threadIdx.x % lanes) * V, at = c < dim ? c : 0;
+    uint32_t key = 0;
+    bool joins = group + 1 < s.n_chunks;  // no run goes on from the last chunk
+    if (joins) {
+        const uint32_t first = group * s.chunk, end = first + s.chunk;
+        key = s.pair[end - 1].key;
+        joins = key < s.n_vectors && s.pair[end].key == key && !(s.pair[first].key == key && first > 0 && s.pair[first - 1].key == key);
+    }
+    float a[V] = {};
+    // Parts first, first + step, ...: AHEAD of them, as many as are of the run; false if the run ends with them.
+    auto add = [&](uint32_t first, uint32_t step, uint32_t of) {
+        uint32_t keys[AHEAD];
+        float p[AHEAD][V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) a[k] = parts[(2 * static_cast<int64_t>(group) + 1) * dim + c + k];
-    for (uint32_t g = group + 1; g < s.n_chunks && s.pair[g * s.chunk].key == key; ++g)
+        for (uint32_t j = 0; j < AHEAD; ++j) {
+            const uint32_t g = std::min(first + j * step, s.n_chunks - 1);
+            keys[j] = s.pair[g * s.chunk].key;
 #pragma unroll
-        for (int k = 0; k < V; ++k) a[k] += parts[2 * static_cast<int64_t>(g) * dim + c + k];
-    Pack<T, V> p;
+            for (int k = 0; k < V; ++k) p[j][k] = parts[2 * static_cast<int64_t>(g) * dim + at + k];
+        }
 #pragma unroll
-    for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[k]);
-    *reinterpret_cast<Pack<T, V> *>(out + static_cast<int64_t>(key) * dim + c) = p;
+        for (uint32_t j = 0; j < AHEAD; ++j) {
+            if (first + j * step >= s.n_chunks || keys[j] != of) return false;
+#pragma unroll
+            for (int k = 0; k < V; ++k) a[k] += p[j][k];
+        }
+        return true;
+    };
+    bool more = false;
+    if (joins) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) a[k] = parts[(2 * static_cast<int64_t>(group) + 1) * dim + at + k];
+        more = add(group + 1, 1, key);
+    }
+    const int own = threadIdx.x % 64 / lanes, groups = 64 / lanes;
+    for (int g = 0; g < groups; ++g) {
+        if (!__shfl(static_cast<int>(more), g * lanes, 64)) continue;  // the same for the whole wavefront
+        const uint32_t of = __shfl(key, g * lanes, 64);
+        float before[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            before[k] = a[k];
+            a[k] = 0;
+        }
+        uint32_t next = group - own + g + 1 + AHEAD + own;
+        while (add(next, groups, of)) next += AHEAD * groups;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            for (int d = lanes; d < 64; d *= 2) a[k] += __shfl_xor(a[k], d, 64);
+            a[k] = own == g ? before[k] + a[k] : before[k];
+        }
+    }
+    if (joins && c < dim) {
+        Pack<T, V> p;
+#pragma unroll
+        for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(scale * a[k]);
+        *reinterpret_cast<Pack<T, V> *>(out + static_cast<int64_t>(key) * dim + c) = p;
+    }
 }
 
 // ---- what a call launches
@@ -529,7 +577,7 @@ hipError_t embed(const head_ids &ids, int64_t dim, const T *table, int64_t table
 // The parts of the workspace of the backward pass, in bytes from its start.
 struct GradPlan {
     uint32_t n, n_tiles, chunk, n_chunks;
-    int passes, bits;
+    int items, passes, bits;
     int64_t pair[2], counts, totals, parts, bytes;
 };
 
@@ -537,12 +585,15 @@ GradPlan plan_grad(const head_ids &ids, int64_t dim)
 {
     GradPlan p{};
     p.n = static_cast<uint32_t>(ids.n_rows * ids.n_ids);
-    p.n_tiles = static_cast<uint32_t>(ceil_div(p.n, TILE));
+    p.items = p.n < FEW_PAIRS ? FEW : MANY;
+    p.n_tiles = static_cast<uint32_t>(ceil_div(p.n, LANES * p.items));
     int bits = 1;
     while (ids.n_vectors >> bits) ++bits;
     p.passes = static_cast<int>(ceil_div(bits, MAX_DIGIT));
     p.bits = static_cast<int>(ceil_div(bits, p.passes));
-    p.chunk = 128;
+    // long chunks have fewer runs that cross them (64 instead of 128: 20 us more for 10 million pairs), short ones fill the device
+    p.chunk = 8;
+    while (p.chunk < 128 && p.n / (2 * p.chunk) >= 16384) p.chunk *= 2;
     p.n_chunks = static_cast<uint32_t>(ceil_div(p.n, p.chunk));
     int64_t at = 0;
     auto part = [&](int64_t bytes) {
@@ -580,21 +631,23 @@ hipError_t embed_grad(const head_ids &ids, int64_t dim, const T *grad, int64_t g
         p.shift = static_cast<uint32_t>(k - 1);
     }
     auto pairs = [&](int which) { return reinterpret_cast<Pair *>(workspace + plan.pair[which]); };
-    const size_t lds = move_lds(plan.bits);
-    auto pass = [&](auto FROM, int k) {
-        if (const hipError_t e = allow_lds<move_kernel<FROM()>>(move_lds(MAX_DIGIT))) return e;
+    auto pass = [&](auto FROM, auto ITEMS, int k) {
+        if (const hipError_t e = allow_lds<move_kernel<FROM(), ITEMS()>>(move_lds(ITEMS(), MAX_DIGIT))) return e;
         const int bit = k * plan.bits;
-        hipLaunchKernelGGL((count_kernel<FROM()>), dim3(plan.n_tiles), dim3(LANES), 0, stream, p, bit, plan.bits, plan.n_tiles,
+        hipLaunchKernelGGL((count_kernel<FROM(), ITEMS()>), dim3(plan.n_tiles), dim3(LANES), 0, stream, p, bit, plan.bits, plan.n_tiles,
                            words(plan.counts));
         hipLaunchKernelGGL(tiles_kernel, dim3(1u << plan.bits), dim3(LANES), 0, stream, plan.n_tiles, words(plan.counts), words(plan.totals));
-        hipLaunchKernelGGL((move_kernel<FROM()>), dim3(plan.n_tiles), dim3(LANES), lds, stream, p, bit, plan.bits, plan.n_tiles,
-                           words(plan.counts), words(plan.totals), pairs(k % 2));
+        hipLaunchKernelGGL((move_kernel<FROM(), ITEMS()>), dim3(plan.n_tiles), dim3(LANES), move_lds(ITEMS(), plan.bits), stream, p, bit,
+                           plan.bits, plan.n_tiles, words(plan.counts), words(plan.totals), pairs(k % 2));
         p.pair = pairs(k % 2);
         return hipGetLastError();
     };
-    hipError_t e = ids.offset ? pass(std::integral_constant<int, IDS_AND_OFFSETS>(), 0) : pass(std::integral_constant<int, IDS>(), 0);
-    for (int k = 1; k < plan.passes && e == hipSuccess; ++k) e = pass(std::integral_constant<int, LAST_PASS>(), k);
-    if (e != hipSuccess) return e;
+    auto sort = [&](auto ITEMS) {
+        hipError_t e = ids.offset ? pass(std::integral_constant<int, IDS_AND_OFFSETS>(), ITEMS, 0) : pass(std::integral_constant<int, IDS>(), ITEMS, 0);
+        for (int k = 1; k < plan.passes && e == hipSuccess; ++k) e = pass(std::integral_constant<int, LAST_PASS>(), ITEMS, k);
+        return e;
+    };
+    if (const hipError_t e = plan.items == FEW ? sort(std::integral_constant<int, FEW>()) : sort(std::integral_constant<int, MANY>())) return e;
     const Sorted s{pairs((plan.passes - 1) % 2), plan.n, static_cast<uint32_t>(ids.n_vectors), plan.chunk, plan.n_chunks};
     float *parts = reinterpret_cast<float *>(workspace + plan.parts);
     const uint64_t bits = address(grad) | address(out) | static_cast<uint64_t>(grad_stride * sizeof(T)) | static_cast<uint64_t>(dim * sizeof(T));

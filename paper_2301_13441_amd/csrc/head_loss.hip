@@ -358,13 +358,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void lse_kernel(Model<T> m, uint32_t
     }
 }
 
-// The tiles' largest values and sums of a row become its lse.  32 rows of a workgroup, 8 lanes on each.
+// The tiles' largest values and sums of a row become its lse.  ROWS rows of a workgroup, 256 / ROWS lanes on each.
+template <int ROWS>
 __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n_classes, int64_t class_tiles, const float2 *parts,
                                                        const float *target_logit, const int32_t *target, float *loss, float *lse)
 {
-    __shared__ float2 lds[8][32];
-    const int lane = threadIdx.x / 32, r = threadIdx.x % 32;
-    for (int64_t row0 = int64_t{32} * blockIdx.x; row0 < n_rows; row0 += int64_t{32} * gridDim.x) {
+    constexpr int LANES = 256 / ROWS;
+    __shared__ float2 lds[LANES][ROWS];
+    const int lane = threadIdx.x / ROWS, r = threadIdx.x % ROWS;
+    for (int64_t row0 = int64_t{ROWS} * blockIdx.x; row0 < n_rows; row0 += int64_t{ROWS} * gridDim.x) {
         const int64_t row = row0 + r;
         float2 all = make_float2(-INFINITY, 0);
         auto add = [&](float2 o) {
@@ -373,13 +375,14 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
         };
         if (row < n_rows) {
 #pragma unroll 4
-            for (int64_t t = lane; t < class_tiles; t += 8) add(parts[t * n_rows + row]);
+            for (int64_t t = lane; t < class_tiles; t += LANES) add(parts[t * n_rows + row]);
         }
         __syncthreads();
         lds[lane][r] = all;
         __syncthreads();
         if (lane == 0 && row < n_rows) {
-            for (int i = 1; i < 8; ++i) add(lds[i][r]);
+            const int some = static_cast<int>(std::min<int64_t>(LANES, class_tiles));
+            for (int i = 1; i < some; ++i) add(lds[i][r]);
             const float log = logf(all.y);
             lse[row] = all.x + log;
             loss[row] = target[row] >= 0 && target[row] < n_classes ? log + (all.x - target_logit[row]) : 0.0f;
@@ -534,13 +537,38 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Op
     }
 }
 
+// The sum of the splits, a lane for each result.
 template <class T>
 __global__ __launch_bounds__(256) void parts_kernel(const float *parts, int64_t splits, int64_t n, T *out)
 {
     for (int64_t i = int64_t{256} * blockIdx.x + threadIdx.x; i < n; i += int64_t{256} * gridDim.x) {
-        float s = parts[i];
-        for (int64_t k = 1; k < splits; ++k) s += parts[k * n + i];
+        float s = 0;
+#pragma unroll 8
+        for (int64_t k = 0; k < splits; ++k) s += parts[k * n + i];
         out[i] = narrow<T>(s);
+    }
+}
+
+// The same where there are many splits, of few results: 64 of a workgroup, 16 wavefronts on them in turn (512 splits of 512 results: 4 us,
+// against 110).
+template <class T>
+__global__ __launch_bounds__(1024) void many_parts_kernel(const float *parts, int64_t splits, int64_t n, T *out)
+{
+    __shared__ float lds[16][64];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    for (int64_t i0 = int64_t{64} * blockIdx.x; i0 < n; i0 += int64_t{64} * gridDim.x) {
+        const int64_t i = std::min(i0 + lane, n - 1);
+        float s = 0;
+#pragma unroll 8
+        for (int64_t k = wave; k < splits; k += 16) s += parts[k * n + i];
+        __syncthreads();
+        lds[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && i0 + lane < n) {
+#pragma unroll
+            for (int w = 1; w < 16; ++w) s += lds[w][lane];
+            out[i] = narrow<T>(s);
+        }
     }
 }
 
@@ -573,10 +601,13 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t stride
 
 // ---- what a call launches
 
-// A workgroup of 4 wavefronts and tiles of 128 x 128, of which a CU has two; tiles of 64 x 64 where there are so few that their number is
-// not what counts but the time of one (1,021 rows, 10 classes: 22 us for all of head_cross_entropy_grad, against 42); or, where bfloat16 products have so many tiles, one of 8
-// and 256 x 256: half the traffic to LDS, and a third less from it, for as many products (16,384 x 65,536 logits over 512 values: 1.32
-// ms, against 1.58).  float32 products are bound by the matrix core, and gain nothing (loss_f32's logits: 257 us, against 255).
+// A workgroup's tile.  Small: 4 wavefronts and 128 x 128, of which a CU has two.  Large: 8 wavefronts and 256 x 256, where bfloat16
+// products have enough of them: half the traffic to LDS and a third less from it for as many products (16,384 x 65,536 logits over 512
+// values: 1.32 ms, against 1.58).  float32 products are bound by the matrix core and gain nothing (loss_f32's logits: 257 us, against 255).
+// Tiny: 64 x 64, where there are so few tiles that the time of one counts, or so few rows or classes that most of a larger one
+// would be empty; float32 products, whose steps take sixteen times as long, sooner than bfloat16 ones.  Both calls, in us: 1,021 rows
+// and 10 classes 31, against 57 in Small; 1 row and 100,000 classes 81, against 130 (both float32); 60 rows and 30,000 classes 50, against 57
+// (bfloat16).
 struct Tiny {
     static constexpr int TILE = 64, RESIDENT = 512;
     template <bool NEXT>
@@ -637,7 +668,9 @@ Plan plan_operands(const head_classes &c)
     Plan p{};
     p.hidden = p.weight = -1;
     auto tiles = [&](int64_t tile) { return ceil_div(c.n_rows, tile) * ceil_div(c.n_classes, tile); };
-    p.size = c.dtype == HEAD_BF16 && tiles(Large::TILE) >= Large::RESIDENT ? LARGE : tiles(Small::TILE) < Small::RESIDENT / 4 ? TINY : SMALL;
+    const bool narrow = c.n_rows <= Tiny::TILE || c.n_classes <= Tiny::TILE;
+    const bool tiny = c.dtype == HEAD_F32 ? narrow || tiles(Small::TILE) < Small::RESIDENT : tiles(Small::TILE) < Small::RESIDENT / 2;
+    p.size = c.dtype == HEAD_BF16 && tiles(Large::TILE) >= Large::RESIDENT ? LARGE : tiny ? TINY : SMALL;
     p.tile = p.size == LARGE ? Large::TILE : p.size == TINY ? Tiny::TILE : Small::TILE;
     p.resident = p.size == LARGE ? Large::RESIDENT : p.size == TINY ? Tiny::RESIDENT : Small::RESIDENT;
     const int e = value_bytes(c.dtype);
@@ -710,9 +743,17 @@ hipError_t forward(const head_classes &c, const Plan &p, float *loss, float *lse
     const int64_t tiles = p.class_tiles * p.row_tiles;
     if (const hipError_t e = launch_product<Forward, lse_kernel<T, Forward>>(grid_of(tiles, Size::RESIDENT), stream, m, static_cast<uint32_t>(p.row_tiles),
                                                                                 static_cast<uint32_t>(p.class_tiles), parts, target_logit)) return e;
-    hipLaunchKernelGGL(lse_join_kernel, grid_of(ceil_div(c.n_rows, 32)), dim3(256), 0, stream, c.n_rows, c.n_classes, p.class_tiles, parts,
-                       target_logit, c.target, loss, lse);
+    auto *join = c.n_rows <= 4096 ? lse_join_kernel<4> : lse_join_kernel<32>;
+    hipLaunchKernelGGL(join, grid_of(ceil_div(c.n_rows, c.n_rows <= 4096 ? 4 : 32)), dim3(256), 0, stream, c.n_rows, c.n_classes, p.class_tiles,
+                       parts, target_logit, c.target, loss, lse);
     return hipGetLastError();
+}
+
+template <class T>
+void add_parts(const float *parts, int64_t splits, int64_t n, T *out, hipStream_t stream)
+{
+    if (splits >= 32) hipLaunchKernelGGL((many_parts_kernel<T>), grid_of(ceil_div(n, 64)), dim3(1024), 0, stream, parts, splits, n, out);
+    else hipLaunchKernelGGL((parts_kernel<T>), grid_of(ceil_div(n, 256)), dim3(256), 0, stream, parts, splits, n, out);
 }
 
 template <class T, class Size>
@@ -770,15 +811,11 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
                                                                                                   static_cast<uint32_t>(plan.weight_splits), depth, weight_parts,
                                                                                                   false, weight_parts ? nullptr : out))
                 return e;
-            if (weight_parts)
-                hipLaunchKernelGGL((parts_kernel<T>), grid_of(ceil_div(classes * c.dim, 256)), dim3(256), 0, stream,
-                                   weight_parts, plan.weight_splits, classes * c.dim, out);
+            if (weight_parts) add_parts(weight_parts, plan.weight_splits, classes * c.dim, out, stream);
         }
         if (const hipError_t e = hipGetLastError()) return e;
     }
-    if (hidden_parts)
-        hipLaunchKernelGGL((parts_kernel<T>), grid_of(ceil_div(c.n_rows * c.dim, 256)), dim3(256), 0, stream, hidden_parts,
-                           plan.hidden_splits, c.n_rows * c.dim, grad_hidden);
+    if (hidden_parts) add_parts(hidden_parts, plan.hidden_splits, c.n_rows * c.dim, grad_hidden, stream);
     return hipGetLastError();
 }
 

@@ -77,9 +77,9 @@ class LeafHead:
         grads = [g_vectors, g_norm_weight, g_norm_bias, g_weight, g_bias]
         self.step += 1
         wide = [k for k, g in enumerate(grads) if g.dtype == grads[1].dtype]  # float32 gradients, and the others
-        for some in (wide, [k for k in range(len(grads)) if k not in wide]):
+        for call, some in enumerate((wide, [k for k in range(len(grads)) if k not in wide])):
             head_adamw([self.params()[k] for k in some], [grads[k] for k in some], [self.states[k] for k in some], self.step, rate,
-                       decay=decay, copies=None if self._copies is None else [self._copies[k] for k in some], seed=self.seed)
+                       decay=decay, copies=None if self._copies is None else [self._copies[k] for k in some], seed=2 * self.seed + call)
         return loss.sum() * share
 
     def linear(self, probabilities: bool = True):

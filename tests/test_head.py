@@ -126,7 +126,7 @@ def test_cross_entropy_refuses_bad_arguments_before_any_device_call():
         for bad in (dict(dtype=2), dict(n=-1), dict(dim=0), dict(classes=0), dict(h=None), dict(h=66), dict(hs=7), dict(w=None),
                     dict(ws=7), dict(b=66), dict(t=None), dict(t=66)):
             assert f(desc(**bad)) == -1, bad
-        for far in (dict(dim=16385), dict(n=10 ** 9 + 1), dict(classes=10 ** 9 + 1)):
+        for far in (dict(dim=16385), dict(n=10 ** 9 + 1), dict(classes=10 ** 9 + 1), dict(n=10 ** 9, classes=17_593)):
             assert f(desc(**far)) == -7, far
         assert f(desc(), work=None) == f(desc(), work=72) == f(desc(), lse=None) == -1
     assert call(desc(), loss=None) == call(desc(), loss=66) == -1
