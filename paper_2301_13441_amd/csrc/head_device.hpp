@@ -30,6 +30,21 @@ __device__ __forceinline__ T narrow(float x)  // to nearest even
     return static_cast<T>(x);
 }
 
+// The machine word of that many bytes.
+template <int BYTES> struct WordOf;
+template <> struct WordOf<2> { using Type = uint16_t; };
+template <> struct WordOf<4> { using Type = uint32_t; };
+template <> struct WordOf<8> { using Type = uint32_t __attribute__((ext_vector_type(2))); };
+template <> struct WordOf<16> { using Type = uint32_t __attribute__((ext_vector_type(4))); };
+
+// A store of what nobody reads soon.
+template <class T, int N>
+__device__ __forceinline__ void store_past(T *to, const Pack<T, N> &p)
+{
+    using Word = typename WordOf<sizeof(T) * N>::Type;
+    __builtin_nontemporal_store(*reinterpret_cast<const Word *>(&p), reinterpret_cast<Word *>(to));
+}
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 inline int value_bytes(int32_t dtype) { return dtype == HEAD_BF16 ? 2 : 4; }

@@ -42,11 +42,6 @@ __device__ __forceinline__ int64_t vector_of(const Ids &s, const int32_t *row, i
 
 // A piece of V values as the machine word it is read as.  A value that is to count for nothing is masked there, by all ones or
 // none: as a choice between values it would be a branch for the compiler, and the loads of a loop would not be on their way together.
-template <int BYTES> struct WordOf;
-template <> struct WordOf<2> { using Type = uint16_t; };
-template <> struct WordOf<4> { using Type = uint32_t; };
-template <> struct WordOf<8> { using Type = uint32_t __attribute__((ext_vector_type(2))); };
-template <> struct WordOf<16> { using Type = uint32_t __attribute__((ext_vector_type(4))); };
 template <class T, int V>
 using Word = typename WordOf<sizeof(T) * V>::Type;
 

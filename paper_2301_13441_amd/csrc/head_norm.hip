@@ -21,6 +21,9 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_GRID = 1 << 22;       // workgroups of the forward pass: 2^30 threads, a grid's axis has room for 2^32
+// A y of so many bytes is no more in the 32 MB of the L2s when it is read: its stores are non-temporal (515,345 x 90 float32: 90 us, 4.1 TB/s,
+// against 107).  The backward pass, which reads twice what it writes, gains nothing (295 us, against 296).
+constexpr int64_t PAST_BYTES = int64_t{64} << 20;
 constexpr int MAX_WORKGROUPS = 768;   // of the backward pass, three for each of 256 CUs: rows of its workspace
 
 template <int LANES>
@@ -53,7 +56,7 @@ __device__ __forceinline__ int column(int i)
 // A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.
 template <class T, int V, int LANES, int N, int ROWS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, const T *x, int64_t x_stride, const float *weight,
-                                                       const float *bias, float eps, T *y, float *mean, float *rstd)
+                                                       const float *bias, float eps, T *y, float *mean, float *rstd, bool past)
 {
     __shared__ float lds[THREADS / 64];
     constexpr int TEAMS = THREADS / LANES;
@@ -108,7 +111,9 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, 
 #pragma unroll
                     for (int j = 0; j < V; ++j) o.v[j] = narrow<T>(fmaf(a[k][i][j] * r[k], w[j], b[j]));
                     const int64_t row = row0 + k * TEAMS;
-                    if (row < n_rows) *reinterpret_cast<Pack<T, V> *>(y + row * dim + c) = o;
+                    if (row >= n_rows) continue;
+                    if (past) store_past(y + row * dim + c, o);
+                    else *reinterpret_cast<Pack<T, V> *>(y + row * dim + c) = o;
                 }
             }
         }
@@ -281,7 +286,8 @@ hipError_t norm(int64_t n_rows, int64_t dim, const T *x, int64_t x_stride, const
         constexpr int ROWS = V() * N() <= 8 ? 4 : V() * N() <= 16 ? 2 : 1;
         const int64_t rows = THREADS / LANES() * ROWS;
         hipLaunchKernelGGL((norm_kernel<T, V(), LANES(), N(), ROWS>), dim3(static_cast<uint32_t>(std::min<int64_t>(ceil_div(n_rows, rows), MAX_GRID))), dim3(THREADS), 0,
-                           stream, n_rows, static_cast<int>(dim), x, x_stride, weight, bias, eps, y, mean, rstd);
+                           stream, n_rows, static_cast<int>(dim), x, x_stride, weight, bias, eps, y, mean, rstd,
+                           n_rows * dim * static_cast<int64_t>(sizeof(T)) >= PAST_BYTES);
         return hipGetLastError();
     });
 }
