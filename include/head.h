@@ -15,8 +15,8 @@
  * the same bits.  Kernels only, so that every call can be captured into a graph.
  *
  * Values are float32 or bfloat16 (dtype).  Sums, statistics and states are float32; a bfloat16 output is rounded once,
- * to nearest even, and inside head_cross_entropy_grad the gradient of a logit is rounded to the dtype before it
- * is multiplied.  Pointers are aligned to their elements.  A row stride counts elements and is at least the row's length;
+ * to nearest even, and inside head_cross_entropy_grad the gradient of a logit is rounded before it is multiplied: to
+ * bfloat16 where there are many logits (from some 2^24 on), to two of them (16 bits) where there are few.  Pointers are aligned to their elements.  A row stride counts elements and is at least the row's length;
  * the elements of a row are adjacent.  Outputs are contiguous, and overlap neither inputs nor each other.
  */
 #ifndef HEAD_H_

@@ -17,6 +17,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "head_device.hpp"
 
@@ -193,9 +194,10 @@ struct Products {
 
     // Begins a tile.  Tiles begin at different steps (turn), so that workgroups side by side, whose rows may lie a power of
     // two apart, do not ask for the same few of the memory's channels at the same time.
-    __device__ __forceinline__ void aim(int64_t row0, int64_t column0, int64_t from, int64_t to, uint32_t turn)
+    // `plane`: A's values begin so many further on.
+    __device__ __forceinline__ void aim(int64_t row0, int64_t column0, int64_t from, int64_t to, uint32_t turn, int64_t plane = 0)
     {
-        ta.aim(a, row0);
+        ta.aim(Operand<T>{a.at + plane, a.stride, a.rows, a.depth}, row0);
         tb.aim(b, column0);
         depth0 = from;
         steps = from < to ? static_cast<int>((to - from + A::DEPTH - 1) / A::DEPTH) : 0;
@@ -203,14 +205,18 @@ struct Products {
         if (steps) load();
     }
 
-    // The product that aim() began; next() is called once, to begin the one after it.
-    template <class Next>
-    __device__ __forceinline__ void run(Acc (&c)[S::MT][S::NT], Next next)
+    static __device__ __forceinline__ void clear(Acc (&c)[S::MT][S::NT])
     {
 #pragma unroll
         for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
             for (int nt = 0; nt < S::NT; ++nt) c[mt][nt] = Acc{};
+    }
+
+    // Adds the product that aim() began; next() is called once, to begin the one after it.
+    template <class Next>
+    __device__ __forceinline__ void run(Acc (&c)[S::MT][S::NT], Next next)
+    {
         if (steps == 0) return next();
         const int count = steps;
         for (int done = 1; done <= count; ++done) {
@@ -310,6 +316,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void lse_kernel(Model<T> m, uint32_t
         for (int i = threadIdx.x; i < S::M; i += S::THREADS)
             bias[i] = class0 + i < m.weight.rows ? (m.bias ? m.bias[class0 + i] : 0.0f) : -INFINITY;
         Acc c[S::MT][S::NT];
+        products.clear(c);
         products.run(c, [&] { aim(tile + gridDim.x); });
         const float *own_bias = bias + S::row(0, 0);
 #pragma unroll
@@ -394,9 +401,15 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
 
 // p of the classes from `class0` on, [n_rows][stride]: whole tiles, zero where there is no class.  bias_parts: the sums of
 // a tile's rows, [tiles of rows][stride].
-template <class T, class S>
+// Where p is bfloat16, a row's largest value by far is that of its target, and its rounding, up to 2^-8 of it, would be the rounding of the
+// whole gradient.  So p is kept in two planes (TWO), the second one, `plane` values behind the first, being what the first one's
+// rounding left; the products with both cost little where there are few logits.  Where there are many, p is one plane, and grad_loss is divided
+// by its largest magnitude (`scale`) first, and the results are multiplied by it: values are near -1 then, which roundings of
+// many rows, of either sign, are right for on average, and not all of one factor times that (in a mean loss 1 / n_rows, say).
+template <class T, class S, bool TWO>
 __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const float *lse, const float *grad_loss, int64_t first_class,
-                                                       uint32_t row_tiles, uint32_t class_tiles, T *p, int64_t stride, float *bias_parts)
+                                                       uint32_t row_tiles, uint32_t class_tiles, T *p, int64_t stride, int64_t plane,
+                                                       const float *scale, float *bias_parts)
 {
     extern __shared__ char lds[];
     float *numbers = reinterpret_cast<float *>(lds + 2 * Products<T, S, true, true>::BYTES);
@@ -422,7 +435,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
             const int target = row < m.hidden.rows ? m.target[row] : -1;
             const bool has = target >= 0 && target < m.weight.rows;
             row_lse[i] = has ? lse[row] : INFINITY;  // so that p is 0
-            row_grad[i] = has ? grad_loss[row] : 0.0f;
+            row_grad[i] = has ? (scale ? grad_loss[row] / *scale : grad_loss[row]) : 0.0f;
             row_target[i] = has && target >= class0 && target < class0 + S::N ? static_cast<int>(target - class0) : -1;
         }
         float bias[S::NT], sum[S::NT] = {};
@@ -432,6 +445,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
             bias[nt] = k < m.weight.rows ? (m.bias ? m.bias[k] : 0.0f) : -INFINITY;
         }
         Acc c[S::MT][S::NT];
+        products.clear(c);
         products.run(c, [&] { aim(tile + gridDim.x); });
         static_assert(S::NEXT, "a lane's classes are adjacent");
         char *to = reinterpret_cast<char *>(p + (row0 + S::row(0, 0)) * stride + (class0 - first_class) + S::column(0));
@@ -459,7 +473,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
                 auto rows_of_four = [&](auto TARGETS) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        Pack<T, S::NT> out;
+                        Pack<T, S::NT> out, rest;
 #pragma unroll
                         for (int nt = 0; nt < S::NT; ++nt) {
                             float e = exp_from<T>(c[mt][nt][i + k] + bias[nt], l[k]);
@@ -467,8 +481,12 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
                             e *= g[k];
                             sum[nt] += e;
                             out.v[nt] = narrow<T>(e);
+                            if constexpr (TWO) rest.v[nt] = narrow<T>(e - widen(out.v[nt]));
                         }
-                        if (down + k < rows) *reinterpret_cast<Pack<T, S::NT> *>(at + k * row_bytes) = out;
+                        if (down + k < rows) {
+                            *reinterpret_cast<Pack<T, S::NT> *>(at + k * row_bytes) = out;
+                            if constexpr (TWO) *reinterpret_cast<Pack<T, S::NT> *>(at + k * row_bytes + plane * sizeof(T)) = rest;
+                        }
                     }
                 };
                 if (targets[mt / 2] >> (mt % 2 * 32 + i * 2) & 255) rows_of_four(std::true_type());
@@ -492,26 +510,30 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
 
 // C = A B with B across memory.  Each of `splits` parts of the sum's axis goes to a result of its own, [splits][rows][dim]
 // float32, added to what is there where `add` says so; or (out) the one part is the result.
-template <class T, class S, bool A_ALONG>
+// TWO: A has two planes, whose products are added.  scale: of the results, or null.
+template <class T, class S, bool A_ALONG, bool TWO>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Operand<T> b, int64_t dim, uint32_t row_tiles,
-                                                             uint32_t column_tiles, uint32_t splits, int64_t split_depth, float *parts,
-                                                             bool add, T *out)
+                                                             uint32_t column_tiles, uint32_t splits, int64_t split_depth, int64_t plane,
+                                                             const float *scale, float *parts, bool add, T *out)
 {
     extern __shared__ char lds[];
     Products<T, S, A_ALONG, false> products(a, b, lds);
     const uint32_t tiles = row_tiles * column_tiles * splits;
     uint32_t column_tile = 0, row_tile = 0;
-    auto aim = [&](uint32_t tile) {
+    auto aim = [&](uint32_t tile, int64_t from) {
         if (tile >= tiles) return;
         tile_of(tile, row_tiles * splits, column_tiles, row_tile, column_tile);
         const int64_t depth0 = row_tile / row_tiles * split_depth;
-        products.aim(int64_t{S::M} * (row_tile % row_tiles), int64_t{S::N} * column_tile, depth0, std::min(a.depth, depth0 + split_depth), 0);
+        products.aim(int64_t{S::M} * (row_tile % row_tiles), int64_t{S::N} * column_tile, depth0, std::min(a.depth, depth0 + split_depth), 0, from);
     };
-    aim(blockIdx.x);
+    aim(blockIdx.x, 0);
+    const float by = scale ? *scale : 1.0f;
     for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * (row_tile % row_tiles), split = row_tile / row_tiles;
         Acc c[S::MT][S::NT];
-        products.run(c, [&] { aim(tile + gridDim.x); });
+        products.clear(c);
+        if constexpr (TWO) products.run(c, [&] { aim(tile, plane); });
+        products.run(c, [&] { aim(tile + gridDim.x, 0); });
         const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
         const int64_t at = (row0 + S::row(0, 0)) * dim + column0 + S::column(0);
         auto each = [&](auto store) {
@@ -528,11 +550,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Op
         static_assert(!S::NEXT, "a lane's columns are 32 apart");
         if (out) {
             T *to = out + at;
-            each([&](int64_t k, float v) { to[k] = narrow<T>(v); });
+            each([&](int64_t k, float v) { to[k] = narrow<T>(by * v); });
         } else {
             float *to = parts + split * a.rows * dim + at;
-            if (add) each([&](int64_t k, float v) { to[k] += v; });
-            else each([&](int64_t k, float v) { to[k] = v; });
+            if (add) each([&](int64_t k, float v) { to[k] += by * v; });
+            else each([&](int64_t k, float v) { to[k] = by * v; });
         }
     }
 }
@@ -572,14 +594,32 @@ __global__ __launch_bounds__(1024) void many_parts_kernel(const float *parts, in
     }
 }
 
-__global__ __launch_bounds__(256) void bias_kernel(const float *parts, int64_t row_tiles, int64_t stride, int64_t n, float *grad_bias)
+__global__ __launch_bounds__(256) void bias_kernel(const float *parts, int64_t row_tiles, int64_t stride, int64_t n, const float *scale,
+                                                   float *grad_bias)
 {
     const int64_t k = int64_t{256} * blockIdx.x + threadIdx.x;
     if (k >= n) return;
     float s = 0;
 #pragma unroll 8
     for (int64_t t = 0; t < row_tiles; ++t) s += parts[t * stride + k];
-    grad_bias[k] = s;
+    grad_bias[k] = scale ? *scale * s : s;
+}
+
+// The largest finite magnitude of x; 1 where there is none above 0.
+__global__ __launch_bounds__(1024) void scale_kernel(const float *x, int64_t n, float *scale)
+{
+    __shared__ float lds[16];
+    float most = 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < n; i += 1024) most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.0f);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d, 64));
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w) most = fmaxf(most, lds[w]);
+        *scale = most > 0 ? most : 1.0f;
+    }
 }
 
 template <class T>
@@ -652,6 +692,7 @@ struct Plan {
     int64_t class_tiles, row_tiles;
     int64_t parts, target;          // forward
     int64_t piece, pieces, stride;  // classes of a piece, a multiple of a tile's; values of a row of p
+    int64_t plane, scale;           // values of a plane of p, where there are two (else 0); -1: grad_loss as it is
     int64_t p, bias, hidden_splits, hidden_parts, weight_splits, weight_parts;
     int64_t bytes = 0;
 
@@ -707,7 +748,10 @@ Plan plan_backward(const head_classes &c)
     p.row_tiles = ceil_div(c.n_rows, p.tile);
     // Rows a power of two apart would lie in few of the memory's channels: a row more than a piece by 256 bytes goes through all.
     p.stride = p.piece + 256 / e;
-    p.p = p.part(c.n_rows * p.stride * e);
+    const bool narrow = c.dtype == HEAD_BF16;
+    p.plane = narrow && p.size != LARGE ? c.n_rows * p.stride : 0;
+    p.scale = narrow && p.size == LARGE ? p.part(4) : -1;
+    p.p = p.part((p.plane ? 2 : 1) * c.n_rows * p.stride * e);
     p.bias = p.part(p.row_tiles * p.stride * 4);
     const int64_t columns = ceil_div(c.dim, p.tile);
     p.hidden_splits = splits_of(p.row_tiles * columns, p.resident, p.piece, step);
@@ -776,27 +820,30 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
     float *bias_parts = grad_bias ? reinterpret_cast<float *>(workspace + plan.bias) : nullptr;
     float *hidden_parts = plan.hidden_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.hidden_parts);
     float *weight_parts = plan.weight_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.weight_parts);
+    float *scale = plan.scale < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.scale);
+    if (scale) hipLaunchKernelGGL(scale_kernel, dim3(1), dim3(1024), 0, stream, grad_loss, c.n_rows, scale);
+    constexpr bool TWO = sizeof(T) == 2 && !std::is_same_v<Size, Large>;
     const int64_t step = STEP / sizeof(T);
     const uint32_t columns = static_cast<uint32_t>(ceil_div(c.dim, Gradient::N));
     for (int64_t piece = 0; piece < plan.pieces; ++piece) {
         const int64_t first = piece * plan.piece, classes = std::min(plan.piece, c.n_classes - first);
         const int64_t class_tiles = ceil_div(classes, Backward::N), stride = plan.stride;
         const int64_t p_tiles = class_tiles * plan.row_tiles;
-        if (const hipError_t e = launch_product<Backward, p_kernel<T, Backward>>(grid_of(p_tiles, Size::RESIDENT), stream, m, lse, grad_loss, first,
+        if (const hipError_t e = launch_product<Backward, p_kernel<T, Backward, TWO>>(grid_of(p_tiles, Size::RESIDENT), stream, m, lse, grad_loss, first,
                                                                                  static_cast<uint32_t>(plan.row_tiles),
-                                                                                 static_cast<uint32_t>(class_tiles), p, stride, bias_parts))
+                                                                                 static_cast<uint32_t>(class_tiles), p, stride, plan.plane, scale, bias_parts))
             return e;
         if (grad_bias)
             hipLaunchKernelGGL(bias_kernel, dim3(static_cast<uint32_t>(ceil_div(classes, 256))), dim3(256), 0, stream, bias_parts,
-                               plan.row_tiles, stride, classes, grad_bias + first);
+                               plan.row_tiles, stride, classes, scale, grad_bias + first);
         // grad_hidden [n_rows][dim] += p [n_rows][classes] weight [classes][dim]
         {
             const uint32_t row_tiles = static_cast<uint32_t>(ceil_div(c.n_rows, Gradient::M));
             const int64_t depth = round_up(ceil_div(classes, plan.hidden_splits), step);
             const Operand<T> a{p, stride, c.n_rows, classes}, b{m.weight.at + first * m.weight.stride, m.weight.stride, m.weight.depth, classes};
             const int64_t tiles = int64_t{row_tiles} * columns * plan.hidden_splits;
-            if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, true>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
-                                                                                                 static_cast<uint32_t>(plan.hidden_splits), depth, hidden_parts,
+            if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, true, TWO>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
+                                                                                                 static_cast<uint32_t>(plan.hidden_splits), depth, plan.plane, scale, hidden_parts,
                                                                                                  piece > 0, hidden_parts ? nullptr : grad_hidden))
                 return e;
         }
@@ -807,8 +854,8 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
             const Operand<T> a{p, stride, classes, c.n_rows}, b{m.hidden.at, m.hidden.stride, m.hidden.depth, c.n_rows};
             const int64_t tiles = int64_t{row_tiles} * columns * plan.weight_splits;
             T *out = grad_weight + first * c.dim;
-            if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, false>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
-                                                                                                  static_cast<uint32_t>(plan.weight_splits), depth, weight_parts,
+            if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, false, TWO>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
+                                                                                                  static_cast<uint32_t>(plan.weight_splits), depth, plan.plane, scale, weight_parts,
                                                                                                   false, weight_parts ? nullptr : out))
                 return e;
             if (weight_parts) add_parts(weight_parts, plan.weight_splits, classes * c.dim, out, stream);
