@@ -54,9 +54,9 @@ __device__ __forceinline__ int column(int i)
 }
 
 // A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.
-template <class T, int V, int LANES, int N, int ROWS>
+template <class T, int V, int LANES, int N, int ROWS, bool PAST>
 __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, const T *x, int64_t x_stride, const float *weight,
-                                                       const float *bias, float eps, T *y, float *mean, float *rstd, bool past)
+                                                       const float *bias, float eps, T *y, float *mean, float *rstd)
 {
     __shared__ float lds[THREADS / 64];
     constexpr int TEAMS = THREADS / LANES;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, 
                     for (int j = 0; j < V; ++j) o.v[j] = narrow<T>(fmaf(a[k][i][j] * r[k], w[j], b[j]));
                     const int64_t row = row0 + k * TEAMS;
                     if (row >= n_rows) continue;
-                    if (past) store_past(y + row * dim + c, o);
+                    if constexpr (PAST) store_past(y + row * dim + c, o);
                     else *reinterpret_cast<Pack<T, V> *>(y + row * dim + c) = o;
                 }
             }
@@ -285,9 +285,11 @@ hipError_t norm(int64_t n_rows, int64_t dim, const T *x, int64_t x_stride, const
     return by_shape<T>(piece(bits, sizeof(T)), dim, [&](auto V, auto LANES, auto N) {
         constexpr int ROWS = V() * N() <= 8 ? 4 : V() * N() <= 16 ? 2 : 1;
         const int64_t rows = THREADS / LANES() * ROWS;
-        hipLaunchKernelGGL((norm_kernel<T, V(), LANES(), N(), ROWS>), dim3(static_cast<uint32_t>(std::min<int64_t>(ceil_div(n_rows, rows), MAX_GRID))), dim3(THREADS), 0,
-                           stream, n_rows, static_cast<int>(dim), x, x_stride, weight, bias, eps, y, mean, rstd,
-                           n_rows * dim * static_cast<int64_t>(sizeof(T)) >= PAST_BYTES);
+        // two kernels: of a branch between the two kinds of store the compiler makes one of the ordinary kind
+        auto *kernel = n_rows * dim * static_cast<int64_t>(sizeof(T)) >= PAST_BYTES ? norm_kernel<T, V(), LANES(), N(), ROWS, true>
+                                                                                     : norm_kernel<T, V(), LANES(), N(), ROWS, false>;
+        hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(std::min<int64_t>(ceil_div(n_rows, rows), MAX_GRID))), dim3(THREADS), 0, stream,
+                           n_rows, static_cast<int>(dim), x, x_stride, weight, bias, eps, y, mean, rstd);
         return hipGetLastError();
     });
 }
