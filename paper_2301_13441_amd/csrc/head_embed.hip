@@ -67,7 +67,8 @@ __device__ __forceinline__ void add(float (&a)[V], W w)
     }
 }
 
-// `lanes` lanes of a group read a vector; `team` groups share a row.
+// `lanes` lanes of a group read a vector; `team` groups share a row.  Bound by the way from id to offset and vector in memory: one row of
+// 500 ids, 64 float32, 6.8 us; 4,096 rows of 128, 18.
 template <class T, int V>
 __global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Ids s, const T *table, int64_t table_stride, float scale,
                                                      T *out, int lanes, int team)
@@ -130,7 +131,8 @@ __global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Id
 
 // Many rows with many ids: a group of G lanes takes ROWS rows at once, all groups go through the ids in the same order, and so
 // few of them are launched that all are resident: what is read at a time is the vectors of a few ids (trees), which an L2
-// holds, and not the whole table.  The G lanes read G ids of a row at once, and each gets every one of them from its neighbours.
+// holds, and not the whole table (33 MB of leaves).  The G lanes read G ids of a row at once, and each gets every one of them from its neighbours.
+// Bound by the L2s: 103,069 rows of 128 ids, 128 bfloat16, 171 us, 17 TB/s.  Two rows of a group 201 us, eight 244, a wavefront for each row 381.
 template <class T, int V, int G, int ROWS>
 __global__ __launch_bounds__(THREADS) void sweep_kernel(int64_t n_rows, int dim, Ids s, const T *table, uint32_t stride_bytes, float scale,
                                                         T *out)
@@ -276,7 +278,8 @@ __device__ __forceinline__ void in_order()
     __builtin_amdgcn_wave_barrier();
 }
 
-// A tile is sorted by the digit in LDS and then goes out in that order, so that neighbours write neighbouring places.
+// A tile is sorted by the digit in LDS and then goes out in that order, so that neighbours write neighbouring places.  10 million pairs and
+// 9 bits: 60 us a pass, of which half is the traffic; straight to their places from registers, at 8 bits, 112.
 template <int FROM, int ITEMS>
 __global__ __launch_bounds__(LANES, 4) void move_kernel(Pairs p, int bit, int bits, uint32_t n_tiles, const uint32_t *counts,
                                                         const uint32_t *totals, Pair *out)
@@ -377,7 +380,8 @@ struct Sorted {
     uint32_t chunk, n_chunks;
 };
 
-// A group of `lanes` lanes adds up a chunk.  parts: [2 * chunk's number][dim], the part of the run that it begins in the
+// A group of `lanes` lanes adds up a chunk.  Bound by the L2s: 10 million rows of 64 float32, 192 us, 13 TB/s; the batch's 5 MB are a
+// fifth more than an L2 holds.  4 or 16 rows on their way instead of 8: 193 and 207.  parts: [2 * chunk's number][dim], the part of the run that it begins in the
 // midst of, then the part of the run that it ends in the midst of.
 template <class T, int V>
 __global__ __launch_bounds__(THREADS) void sum_kernel(Sorted s, int dim, const T *grad, int64_t grad_stride, float scale, T *out,

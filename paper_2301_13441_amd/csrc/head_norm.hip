@@ -53,7 +53,8 @@ __device__ __forceinline__ int column(int i)
     return (i * LANES + static_cast<int>(threadIdx.x % LANES)) * V;
 }
 
-// A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.
+// A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.  515,345 rows of 90 float32: 92
+// us, 4.0 TB/s; one row at a time 195, eight 118 (both with ordinary stores, as 107).
 template <class T, int V, int LANES, int N, int ROWS, bool PAST>
 __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, const T *x, int64_t x_stride, const float *weight,
                                                        const float *bias, float eps, T *y, float *mean, float *rstd)
@@ -128,6 +129,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, 
     }
 }
 
+// 262,147 rows of 1024 bfloat16: 302 us, 5.3 TB/s; two rows at a time, of 16 values a lane, 323.
 template <class T, int V, int LANES, int N, int ROWS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(int64_t n_rows, int dim, const T *grad, int64_t grad_stride, const T *x,
                                                             int64_t x_stride, const float *weight, const float *mean,
