@@ -36,8 +36,8 @@ struct Ids {
 __device__ __forceinline__ int64_t vector_of(const Ids &s, const int32_t *row, int64_t t)
 {
     const int32_t id = row[t];
-    const int64_t v = id + (s.offset ? s.offset[t] : 0);
-    return id >= 0 && v >= 0 && v < s.n_vectors ? v : -1;
+    const uint64_t v = static_cast<uint64_t>(id) + static_cast<uint64_t>(s.offset ? s.offset[t] : 0);  // below 0: far above all vectors
+    return id >= 0 && v < static_cast<uint64_t>(s.n_vectors) ? static_cast<int64_t>(v) : -1;
 }
 
 // A piece of V values as the machine word it is read as.  A value that is to count for nothing is masked there, by all ones or
@@ -211,8 +211,8 @@ __device__ __forceinline__ Pair pair_of(const Pairs &p, uint32_t i)
     if constexpr (FROM == LAST_PASS) return p.pair[i];
     const uint32_t row = p.n_ids == 1 ? i : __umulhi(i, p.magic) >> p.shift, t = i - row * p.n_ids;
     const int32_t id = p.s.id[row * p.s.stride + t];
-    const int64_t v = id + (FROM == IDS_AND_OFFSETS ? p.s.offset[t] : 0);
-    return Pair{static_cast<uint32_t>(id >= 0 && v >= 0 && v < p.s.n_vectors ? v : p.s.n_vectors), row};
+    const uint64_t v = static_cast<uint64_t>(id) + static_cast<uint64_t>(FROM == IDS_AND_OFFSETS ? p.s.offset[t] : 0), all = p.s.n_vectors;
+    return Pair{static_cast<uint32_t>(id >= 0 && v < all ? v : all), row};
 }
 
 template <int FROM, int ITEMS>

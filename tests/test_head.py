@@ -440,6 +440,18 @@ def _check_cross_entropy(n, dim, classes, dtype, variants):
 
 
 @pytest.mark.gpu
+def test_embed_offsets_that_lead_out_of_the_table():
+    """Offsets below zero, and so large that no sum of theirs is a vector."""
+    import torch
+    table = torch.arange(5, dtype=torch.float32, device="cuda")[:, None].expand(5, 8).contiguous()
+    ids = torch.tensor([[4, 3, 2 ** 31 - 1], [1, 0, 1], [-1, 2 ** 31 - 1, 0]], dtype=torch.int32, device="cuda")
+    off = torch.tensor([-1, 2 ** 63 - 1, 3 - 2 ** 31], dtype=torch.int64, device="cuda")
+    assert _np(pk.head_embed(table, ids, off))[:, 0].tolist() == [3 + 2, 0, 0]      # 4 - 1; 2^31 - 1 + 3 - 2^31; 1 - 1
+    got = pk.head_embed_grad(torch.tensor([[1.0], [2.0], [4.0]], device="cuda").expand(3, 8).contiguous(), ids, 5, off)
+    assert _np(got)[:, 0].tolist() == [2, 0, 1, 1, 0]
+
+
+@pytest.mark.gpu
 def test_cross_entropy_of_no_rows():
     import torch
     h, w, b = torch.empty(0, 8, device="cuda"), torch.randn(5, 8, device="cuda"), torch.zeros(5, device="cuda")
