@@ -598,31 +598,41 @@ __global__ __launch_bounds__(1024) void many_parts_kernel(const float *parts, in
     }
 }
 
-__global__ __launch_bounds__(256) void bias_kernel(const float *parts, int64_t row_tiles, int64_t stride, int64_t n, const float *scale,
-                                                   float *grad_bias)
+// The sum of the tiles of rows, of 64 classes a workgroup, 16 wavefronts on them in turn.
+__global__ __launch_bounds__(1024) void bias_kernel(const float *parts, int64_t row_tiles, int64_t stride, int64_t n, const float *scale,
+                                                    float *grad_bias)
 {
-    const int64_t k = int64_t{256} * blockIdx.x + threadIdx.x;
-    if (k >= n) return;
+    __shared__ float lds[16][64];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const int64_t k = int64_t{64} * blockIdx.x + lane;
     float s = 0;
-#pragma unroll 8
-    for (int64_t t = 0; t < row_tiles; ++t) s += parts[t * stride + k];
+#pragma unroll 4
+    for (int64_t t = wave; t < row_tiles; t += 16) s += parts[t * stride + std::min(k, n - 1)];
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave > 0 || k >= n) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += lds[w][lane];
     grad_bias[k] = scale ? *scale * s : s;
 }
 
-// The largest finite magnitude of x; 1 where there is none above 0.
-__global__ __launch_bounds__(1024) void scale_kernel(const float *x, int64_t n, float *scale)
+// The largest finite magnitude of x, a part of it for each workgroup; 1, in the last launch, where there is none above 0.
+constexpr int SCALE_PARTS = 256;
+
+__global__ __launch_bounds__(1024) void scale_kernel(const float *x, int64_t n, bool last, float *out)
 {
     __shared__ float lds[16];
     float most = 0;
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < n; i += 1024) most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.0f);
+    for (int64_t i = int64_t{1024} * blockIdx.x + threadIdx.x; i < n; i += int64_t{1024} * gridDim.x)
+        most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.0f);
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d, 64));
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < 16; ++w) most = fmaxf(most, lds[w]);
-        *scale = most > 0 ? most : 1.0f;
+        out[blockIdx.x] = most > 0 || !last ? most : 1.0f;
     }
 }
 
@@ -754,7 +764,7 @@ Plan plan_backward(const head_classes &c)
     p.stride = p.piece + 256 / e;
     const bool narrow = c.dtype == HEAD_BF16;
     p.plane = narrow && p.size != LARGE ? c.n_rows * p.stride : 0;
-    p.scale = narrow && p.size == LARGE ? p.part(4) : -1;
+    p.scale = narrow && p.size == LARGE ? p.part(4 * (1 + SCALE_PARTS)) : -1;
     p.p = p.part((p.plane ? 2 : 1) * c.n_rows * p.stride * e);
     p.bias = p.part(p.row_tiles * p.stride * 4);
     const int64_t columns = ceil_div(c.dim, p.tile);
@@ -825,7 +835,11 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
     float *hidden_parts = plan.hidden_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.hidden_parts);
     float *weight_parts = plan.weight_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.weight_parts);
     float *scale = plan.scale < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.scale);
-    if (scale) hipLaunchKernelGGL(scale_kernel, dim3(1), dim3(1024), 0, stream, grad_loss, c.n_rows, scale);
+    if (scale) {
+        const bool one = c.n_rows <= 1 << 16;  // else the parts of many workgroups, behind the scale, first
+        if (!one) hipLaunchKernelGGL(scale_kernel, dim3(SCALE_PARTS), dim3(1024), 0, stream, grad_loss, c.n_rows, false, scale + 1);
+        hipLaunchKernelGGL(scale_kernel, dim3(1), dim3(1024), 0, stream, one ? grad_loss : scale + 1, one ? c.n_rows : SCALE_PARTS, true, scale);
+    }
     constexpr bool TWO = sizeof(T) == 2 && !std::is_same_v<Size, Large>;
     const int64_t step = STEP / sizeof(T);
     const uint32_t columns = static_cast<uint32_t>(ceil_div(c.dim, Gradient::N));
@@ -838,7 +852,7 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
                                                                                  static_cast<uint32_t>(class_tiles), p, stride, plan.plane, scale, bias_parts))
             return e;
         if (grad_bias)
-            hipLaunchKernelGGL(bias_kernel, dim3(static_cast<uint32_t>(ceil_div(classes, 256))), dim3(256), 0, stream, bias_parts,
+            hipLaunchKernelGGL(bias_kernel, dim3(static_cast<uint32_t>(ceil_div(classes, 64))), dim3(1024), 0, stream, bias_parts,
                                plan.row_tiles, stride, classes, scale, grad_bias + first);
         // grad_hidden [n_rows][dim] += p [n_rows][classes] weight [classes][dim]
         {

@@ -440,6 +440,39 @@ def _check_cross_entropy(n, dim, classes, dtype, variants):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,dim,classes", [(70_001, 16, 10), (300_003, 8, 3)])
+def test_cross_entropy_of_many_rows_and_few_classes(n, dim, classes):
+    """Rows' tiles by the hundreds of few classes, a grad_loss of rows of very different weight, some of them none."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    h = torch.randn(n, dim, generator=g, device="cuda").bfloat16()
+    w = torch.randn(classes, dim, generator=g, device="cuda").bfloat16()
+    b = torch.randn(classes, generator=g, device="cuda")
+    t = torch.randint(0, classes, (n,), generator=g, device="cuda", dtype=torch.int32)
+    gl = torch.rand(n, generator=g, device="cuda") ** 8 / n
+    gl[::7] = 0
+    loss, lse = pk.head_cross_entropy(h, w, t, b)
+    gh, gw, gb = pk.head_cross_entropy_grad(gl, h, w, t, lse, b)
+    h64, w64 = h.double(), w.double()
+    logits = h64 @ w64.T + b.double()
+    want_lse = torch.logsumexp(logits, 1)
+    p = torch.softmax(logits, 1)
+    p[torch.arange(n, device="cuda"), t.long()] -= 1
+    p *= gl.double()[:, None]
+    # logits to 4 (dim + 2) U of their terms, which are below 60 here; p to that and its own rounding, relative to grad_loss
+    off = 4 * (dim + 2) * U * 60 + 64 * U
+    _close(lse, _np(want_lse), off)
+    size = gl.double()[:, None].expand(n, classes) * (2 * off) + p.abs() * 2.0 ** -8
+    want = p @ w64
+    _close(gh, _np(want), _np(size @ w64.abs()) * 1.01 + 2.0 ** -8 * 1.01 * np.abs(_np(want)))
+    want = p.T @ h64
+    _close(gw, _np(want), _np(size.T @ h64.abs()) * 1.01 + n * U / 16 * _np(p.abs().T @ h64.abs()) + 2.0 ** -8 * 1.01 * np.abs(_np(want)))
+    _close(gb, _np(p.sum(0)), _np((gl.double()[:, None] * 2 * off).sum(0)) + n * U / 16 * _np(p.abs().sum(0)))
+    none = pk.head_cross_entropy_grad(torch.zeros_like(gl), h, w, t, lse, b)
+    assert all((x == 0).all() for x in none)
+
+
+@pytest.mark.gpu
 def test_embed_offsets_that_lead_out_of_the_table():
     """Offsets below zero, and so large that no sum of theirs is a vector."""
     import torch
