@@ -100,7 +100,8 @@ int head_layer_norm_grad(int32_t dtype, int64_t n_rows, int64_t dim, const void 
 /*
  * A linear softmax model and its batch: logit[r][k] = sum_d hidden[r][d] * weight[k][d] + bias[k].  hidden [n_rows][dim]
  * and weight [n_classes][dim] of dtype, bias [n_classes] float32 or NULL (zeros).  target[r] outside [0, n_classes) (-1, say):
- * the row has no target, its loss is 0 and it has no gradient.
+ * the row has no target, its loss is 0 and it has no gradient: grad_hidden is 0 there, and what the row of hidden, lse and
+ * grad_loss holds, finite or not, counts for no gradient.
  */
 typedef struct head_classes {
     int32_t dtype;

@@ -38,13 +38,22 @@ using LdsChunk = __attribute__((address_space(3))) void *;
 using Half = short __attribute__((ext_vector_type(4)));  // of a chunk
 using LdsHalf = __attribute__((address_space(3))) Half *;
 
-// An operand: `rows` along the result's axis, `depth` along the sum's.
+// An operand: `rows` along the result's axis, `depth` along the sum's.  has: a bit for each row of the batch, or null, where those are one
+// of the axes; a row without its bit counts for nothing, whatever it holds.
 template <class T>
 struct Operand {
     const T *at;
     int64_t stride;
     int64_t rows, depth;
+    const uint64_t *has = nullptr;
 };
+
+// A word of the bits.  Those are written by a kernel before, which the compiler cannot know: a scalar load has to be asked for.
+template <class W>
+__device__ __forceinline__ W bits_of(const uint64_t *has, int64_t word)
+{
+    return reinterpret_cast<const __attribute__((address_space(4))) W *>(reinterpret_cast<uintptr_t>(has))[word];
+}
 
 // Tiles of ROWS x 128 bytes of an operand, brought to LDS by THREADS lanes, 16 bytes each at a time.
 // ALONG: the sum's axis lies along memory.  Row r of the tile is STEP bytes, its chunk c of 16 bytes in slot c ^ key(r): the
@@ -97,13 +106,30 @@ struct Tile {
         auto chunk = [&](int j, const void *p) {
             __builtin_amdgcn_global_load_lds((GlobalChunk)(p), (LdsChunk)(lds + (j * WAVES + wave) * 1024), 16, 0, 0);
         };
-        if (depth + DEPTH <= o.depth) {
+        // Zeros past the end of the sum, and in place of rows of the batch that count for nothing: their values, finite or not, would be
+        // multiplied by the zeros of p.
+        if constexpr (ALONG) {
+            const int left = static_cast<int>(std::min<int64_t>(DEPTH, o.depth - depth));
+            if (left == DEPTH) {
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) chunk(j, from[j] + ahead);
-        } else {  // the last one: zeros past the end of the sum
-            const int left = static_cast<int>(o.depth - depth);
+                for (int j = 0; j < LOADS; ++j) chunk(j, from[j] + ahead);
+            } else {
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) chunk(j, at[j] < left ? static_cast<const void *>(from[j] + ahead) : g_zeros);
+                for (int j = 0; j < LOADS; ++j) chunk(j, at[j] < left ? static_cast<const void *>(from[j] + ahead) : g_zeros);
+            }
+        } else {
+            using Bits = std::conditional_t<DEPTH == 64, uint64_t, uint32_t>;  // of a step's indexes, aligned in the words of `has`
+            static_assert(DEPTH == 8 * sizeof(Bits), "a step is a word of the bits");
+            constexpr Bits ALL = ~Bits{0};
+            Bits some = depth + DEPTH <= o.depth ? ALL : ALL >> (depth + DEPTH - o.depth);
+            if (o.has) some &= bits_of<Bits>(o.has, depth / DEPTH);
+            if (some == ALL) {
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) chunk(j, from[j] + ahead);
+            } else {
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) chunk(j, some >> at[j] & 1 ? static_cast<const void *>(from[j] + ahead) : g_zeros);
+            }
         }
     }
 
@@ -197,7 +223,7 @@ struct Products {
     // `plane`: A's values begin so many further on.
     __device__ __forceinline__ void aim(int64_t row0, int64_t column0, int64_t from, int64_t to, uint32_t turn, int64_t plane = 0)
     {
-        ta.aim(Operand<T>{a.at + plane, a.stride, a.rows, a.depth}, row0);
+        ta.aim(Operand<T>{a.at + plane, a.stride, a.rows, a.depth, nullptr}, row0);
         tb.aim(b, column0);
         depth0 = from;
         steps = from < to ? static_cast<int>((to - from + A::DEPTH - 1) / A::DEPTH) : 0;
@@ -408,12 +434,14 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
 // rounding left; the products with both cost little where there are few logits.  Where there are many, p is one plane, and grad_loss is divided
 // by its largest magnitude (`scale`) first, and the results are multiplied by it: values are near -1 then, which roundings of
 // many rows, of either sign, are right for on average, and not all of one factor times that (in a mean loss 1 / n_rows, say).
+// A row without a target has logits of -inf here, so that p is 0 whatever it holds, and no bit in `has_target`, by which the products leave it out.
 // 16,384 x 32,768 bfloat16: 730 us, of which the stores alone take about half.
 template <class T, class S, bool TWO>
 __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const float *lse, const float *grad_loss, int64_t first_class,
                                                        uint32_t row_tiles, uint32_t class_tiles, T *p, int64_t stride, int64_t plane,
-                                                       const float *scale, float *bias_parts)
+                                                       const float *scale, float *bias_parts, uint64_t *has_target)
 {
+    constexpr int ELSEWHERE = -1, NONE = -2;  // where a row's target is no class of the tile, or no class
     extern __shared__ char lds[];
     float *numbers = reinterpret_cast<float *>(lds + 2 * Products<T, S, true, true>::BYTES);
     float *sums = numbers;  // [WAVES_M][N]
@@ -437,9 +465,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
             const int64_t row = row0 + i;
             const int target = row < m.hidden.rows ? m.target[row] : -1;
             const bool has = target >= 0 && target < m.weight.rows;
-            row_lse[i] = has ? lse[row] : INFINITY;  // so that p is 0
+            row_lse[i] = has ? lse[row] : 0.0f;
             row_grad[i] = has ? (scale ? grad_loss[row] / *scale : grad_loss[row]) : 0.0f;
-            row_target[i] = has && target >= class0 && target < class0 + S::N ? static_cast<int>(target - class0) : -1;
+            row_target[i] = !has ? NONE : target >= class0 && target < class0 + S::N ? static_cast<int>(target - class0) : ELSEWHERE;
+            const uint64_t word = __ballot(has);
+            if (class0 == 0 && i % 64 == 0) has_target[row / 64] = word;
         }
         float bias[S::NT], sum[S::NT] = {};
 #pragma unroll
@@ -457,13 +487,24 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
         const int rows = static_cast<int>(std::min<int64_t>(S::M, m.hidden.rows - row0)) - S::row(0, 0);
         const float *own_lse = row_lse + S::row(0, 0), *own_grad = row_grad + S::row(0, 0);
         const int *own_target = row_target + S::row(0, 0);
-        // Few rows have their target among a wavefront's classes: a bit for each of its rows that does.
+        // Few rows have their target among a wavefront's classes, and few have none: a bit for each of its rows that does.
         uint64_t targets[(S::MT + 1) / 2];
 #pragma unroll
         for (int k = 0; k < (S::MT + 1) / 2; ++k) {
             const int r = k * 64 + threadIdx.x % 64;
-            const int target = r < S::MT * 32 ? row_target[S::wave_m() * (S::MT * 32) + r] : -1;
+            const int target = r < S::MT * 32 ? row_target[S::wave_m() * (S::MT * 32) + r] : ELSEWHERE;
             targets[k] = __ballot(target >= 0 && target / (S::NT * 32) == S::wave_n());
+            const uint64_t none = __ballot(target == NONE);
+#pragma unroll
+            for (int h = 0; h < 2 && k * 2 + h < S::MT; ++h) {
+                uint32_t bits = static_cast<uint32_t>(none >> (h * 32));
+                if (bits == 0) continue;
+                bits >>= threadIdx.x % 64 / 32 * 4;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)  // a lane's results are of four rows in each eight
+#pragma unroll
+                    for (int nt = 0; nt < S::NT; ++nt) c[k * 2 + h][nt][i] = bits >> (i / 4 * 8 + i % 4) & 1 ? -INFINITY : c[k * 2 + h][nt][i];
+            }
         }
         char *at = to;  // a lane's results are of four rows in every eight
 #pragma unroll
@@ -513,7 +554,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
 
 // C = A B with B across memory.  Each of `splits` parts of the sum's axis goes to a result of its own, [splits][rows][dim]
 // float32, added to what is there where `add` says so; or (out) the one part is the result.
-// TWO: A has two planes, whose products are added.  scale: of the results, or null.  p of 16,384 rows and 32,768
+// TWO: A has two planes, whose products are added.  Where A lies along memory its rows are the batch's, elsewhere the sum goes over those.
+// scale: of the results, or null.  p of 16,384 rows and 32,768
 // classes, 512 columns, bfloat16: 711 us for hidden's gradient, 630 for weight's, 773 and 872 TFLOP/s; 4,099 x 20,011, 128 columns, float32: 231 and 237 us, 91 and 89, the matrix core busy for 78 %.
 template <class T, class S, bool A_ALONG, bool TWO>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Operand<T> b, int64_t dim, uint32_t row_tiles,
@@ -540,16 +582,22 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Op
         products.run(c, [&] { aim(tile + gridDim.x, 0); });
         const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
         const int64_t at = (row0 + S::row(0, 0)) * dim + column0 + S::column(0);
+        const int wave_m = __builtin_amdgcn_readfirstlane(S::wave_m());
         auto each = [&](auto store) {
 #pragma unroll
-            for (int mt = 0; mt < S::MT; ++mt)
+            for (int mt = 0; mt < S::MT; ++mt) {
+                // rows of the batch without a target get zeros, whatever the weights are
+                uint32_t here = 0;
+                if constexpr (A_ALONG) here = bits_of<uint32_t>(a.has, row0 / 32 + wave_m * S::MT + mt) >> (threadIdx.x % 64 / 32 * 4);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int down = mt * 32 + i / 4 * 8 + i % 4;
 #pragma unroll
                     for (int nt = 0; nt < S::NT; ++nt)
-                        if (down < rows && column0 + S::column(nt) < dim) store(down * dim + nt * 32, c[mt][nt][i]);
+                        if (down < rows && column0 + S::column(nt) < dim)
+                            store(down * dim + nt * 32, !A_ALONG || here >> (i / 4 * 8 + i % 4) & 1 ? c[mt][nt][i] : 0.0f);
                 }
+            }
         };
         static_assert(!S::NEXT, "a lane's columns are 32 apart");
         if (out) {
@@ -707,6 +755,7 @@ struct Plan {
     int64_t parts, target;          // forward
     int64_t piece, pieces, stride;  // classes of a piece, a multiple of a tile's; values of a row of p
     int64_t plane, scale;           // values of a plane of p, where there are two (else 0); -1: grad_loss as it is
+    int64_t has;                    // a bit for each row that has a target, in whole tiles
     int64_t p, bias, hidden_splits, hidden_parts, weight_splits, weight_parts;
     int64_t bytes = 0;
 
@@ -765,6 +814,7 @@ Plan plan_backward(const head_classes &c)
     const bool narrow = c.dtype == HEAD_BF16;
     p.plane = narrow && p.size != LARGE ? c.n_rows * p.stride : 0;
     p.scale = narrow && p.size == LARGE ? p.part(4 * (1 + SCALE_PARTS)) : -1;
+    p.has = p.part(p.row_tiles * p.tile / 8);
     p.p = p.part((p.plane ? 2 : 1) * c.n_rows * p.stride * e);
     p.bias = p.part(p.row_tiles * p.stride * 4);
     const int64_t columns = ceil_div(c.dim, p.tile);
@@ -831,6 +881,7 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
     const Model<T> m = model_of<T>(c, plan, workspace, stream);
     if (const hipError_t e = hipGetLastError()) return e;
     T *p = reinterpret_cast<T *>(workspace + plan.p);
+    uint64_t *has = reinterpret_cast<uint64_t *>(workspace + plan.has);
     float *bias_parts = grad_bias ? reinterpret_cast<float *>(workspace + plan.bias) : nullptr;
     float *hidden_parts = plan.hidden_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.hidden_parts);
     float *weight_parts = plan.weight_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.weight_parts);
@@ -849,7 +900,7 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
         const int64_t p_tiles = class_tiles * plan.row_tiles;
         if (const hipError_t e = launch_product<Backward, p_kernel<T, Backward, TWO>>(grid_of(p_tiles, Size::RESIDENT), stream, m, lse, grad_loss, first,
                                                                                  static_cast<uint32_t>(plan.row_tiles),
-                                                                                 static_cast<uint32_t>(class_tiles), p, stride, plan.plane, scale, bias_parts))
+                                                                                 static_cast<uint32_t>(class_tiles), p, stride, plan.plane, scale, bias_parts, has))
             return e;
         if (grad_bias)
             hipLaunchKernelGGL(bias_kernel, dim3(static_cast<uint32_t>(ceil_div(classes, 64))), dim3(1024), 0, stream, bias_parts,
@@ -858,7 +909,7 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
         {
             const uint32_t row_tiles = static_cast<uint32_t>(ceil_div(c.n_rows, Gradient::M));
             const int64_t depth = round_up(ceil_div(classes, plan.hidden_splits), step);
-            const Operand<T> a{p, stride, c.n_rows, classes}, b{m.weight.at + first * m.weight.stride, m.weight.stride, m.weight.depth, classes};
+            const Operand<T> a{p, stride, c.n_rows, classes, has}, b{m.weight.at + first * m.weight.stride, m.weight.stride, m.weight.depth, classes};
             const int64_t tiles = int64_t{row_tiles} * columns * plan.hidden_splits;
             if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, true, TWO>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
                                                                                                  static_cast<uint32_t>(plan.hidden_splits), depth, plan.plane, scale, hidden_parts,
@@ -869,7 +920,7 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
         {
             const uint32_t row_tiles = static_cast<uint32_t>(ceil_div(classes, Gradient::M));
             const int64_t depth = round_up(ceil_div(c.n_rows, plan.weight_splits), step);
-            const Operand<T> a{p, stride, classes, c.n_rows}, b{m.hidden.at, m.hidden.stride, m.hidden.depth, c.n_rows};
+            const Operand<T> a{p, stride, classes, c.n_rows}, b{m.hidden.at, m.hidden.stride, m.hidden.depth, c.n_rows, has};
             const int64_t tiles = int64_t{row_tiles} * columns * plan.weight_splits;
             T *out = grad_weight + first * c.dim;
             if (const hipError_t e = launch_product<Gradient, product_kernel<T, Gradient, false, TWO>>(grid_of(tiles, Size::RESIDENT), stream, a, b, c.dim, row_tiles, columns,
