@@ -664,16 +664,21 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float *parts, int64_t 
     grad_bias[k] = scale ? *scale * s : s;
 }
 
-// The largest finite magnitude of x, a part of it for each workgroup; 1, in the last launch, where there is none above 0.
+// The largest finite magnitude of x over the rows that have a target (TARGETS), a part of it for each workgroup; 1, in
+// the last launch, where there is none above 0.
 constexpr int SCALE_PARTS = 256;
 
-__global__ __launch_bounds__(1024) void scale_kernel(const float *x, int64_t n, bool last, float *out)
+template <bool TARGETS>
+__global__ __launch_bounds__(1024) void scale_kernel(const float *x, const int32_t *target, int64_t n_classes, int64_t n, bool last, float *out)
 {
     __shared__ float lds[16];
     float most = 0;
 #pragma unroll 4
-    for (int64_t i = int64_t{1024} * blockIdx.x + threadIdx.x; i < n; i += int64_t{1024} * gridDim.x)
-        most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.0f);
+    for (int64_t i = int64_t{1024} * blockIdx.x + threadIdx.x; i < n; i += int64_t{1024} * gridDim.x) {
+        const float v = fabsf(x[i]);
+        const int32_t t = TARGETS ? target[i] : 0;
+        most = fmaxf(most, ((v < INFINITY) & (t >= 0) & (t < n_classes)) ? v : 0.0f);
+    }
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d, 64));
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = most;
@@ -888,8 +893,12 @@ hipError_t backward(const head_classes &c, const Plan &plan, const float *lse, c
     float *scale = plan.scale < 0 ? nullptr : reinterpret_cast<float *>(workspace + plan.scale);
     if (scale) {
         const bool one = c.n_rows <= 1 << 16;  // else the parts of many workgroups, behind the scale, first
-        if (!one) hipLaunchKernelGGL(scale_kernel, dim3(SCALE_PARTS), dim3(1024), 0, stream, grad_loss, c.n_rows, false, scale + 1);
-        hipLaunchKernelGGL(scale_kernel, dim3(1), dim3(1024), 0, stream, one ? grad_loss : scale + 1, one ? c.n_rows : SCALE_PARTS, true, scale);
+        if (one) {
+            hipLaunchKernelGGL(scale_kernel<true>, dim3(1), dim3(1024), 0, stream, grad_loss, c.target, c.n_classes, c.n_rows, true, scale);
+        } else {
+            hipLaunchKernelGGL(scale_kernel<true>, dim3(SCALE_PARTS), dim3(1024), 0, stream, grad_loss, c.target, c.n_classes, c.n_rows, false, scale + 1);
+            hipLaunchKernelGGL(scale_kernel<false>, dim3(1), dim3(1024), 0, stream, scale + 1, nullptr, c.n_classes, SCALE_PARTS, true, scale);
+        }
     }
     constexpr bool TWO = sizeof(T) == 2 && !std::is_same_v<Size, Large>;
     const int64_t step = STEP / sizeof(T);

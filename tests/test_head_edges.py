@@ -74,3 +74,19 @@ def test_cross_entropy_of_rows_none_of_which_has_a_target():
         assert (loss == 0).all() and torch.isfinite(lse).all()
         for x in pk.head_cross_entropy_grad(torch.ones(n, device="cuda"), h.fill_(float("inf")), w, t, lse, b):
             assert (x == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,dim,classes", [(4099, 72, 4200), (66_001, 16, 300)])
+def test_cross_entropy_rows_without_a_target_have_no_say_in_the_precision(n, dim, classes):
+    """bfloat16 in tiles of 256 divides grad_loss by its largest magnitude: that of the rows that count."""
+    import torch
+    h, w, b, t = _classes(n, n, dim, classes, torch.bfloat16)
+    none = (t < 0) | (t >= classes)
+    loss, lse = pk.head_cross_entropy(h, w, t, b)
+    gl = torch.rand(n, device="cuda") / n
+    gl[none] = 0
+    want = pk.head_cross_entropy_grad(gl, h, w, t, lse, b)
+    gl[none] = 3e38
+    for x, y, what in zip(pk.head_cross_entropy_grad(gl, h, w, t, lse, b), want, ("grad_hidden", "grad_weight", "grad_bias")):
+        assert torch.equal(x, y), what
