@@ -16,7 +16,8 @@
  *
  * Values are float32 or bfloat16 (dtype).  Sums, statistics and states are float32; a bfloat16 output is rounded once,
  * to nearest even, and inside head_cross_entropy_grad the gradient of a logit is rounded before it is multiplied: to
- * bfloat16 where there are many logits (from some 2^24 on), to two of them (16 bits) where there are few.  Pointers are aligned to their elements.  A row stride counts elements and is at least the row's length;
+ * bfloat16 where there are many logits (at least 256 rows and 256 classes, that fill or begin 256 tiles of 256 x 256: some 2^24), to two of
+ * them (16 bits) elsewhere.  Pointers are aligned to their elements.  A row stride counts elements and is at least the row's length;
  * the elements of a row are adjacent.  Outputs are contiguous, and overlap neither inputs nor each other.
  */
 #ifndef HEAD_H_

@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
 // a tile's rows, [tiles of rows][stride].
 // Where p is bfloat16, a row's largest value by far is that of its target, and its rounding, up to 2^-8 of it, would be the rounding of the
 // whole gradient.  So p is kept in two planes (TWO), the second one, `plane` values behind the first, being what the first one's
-// rounding left; the products with both cost little where there are few logits.  Where there are many, p is one plane, and grad_loss is divided
+// rounding left; the products with both cost little where there are few logits.  In tiles of 256, so where there are many, p is one plane, and grad_loss is divided
 // by its largest magnitude (`scale`) first, and the results are multiplied by it: values are near -1 then, which roundings of
 // many rows, of either sign, are right for on average, and not all of one factor times that (in a mean loss 1 / n_rows, say).
 // A row without a target has logits of -inf here, so that p is 0 whatever it holds, and no bit in `has_target`, by which the products leave it out.
@@ -711,6 +711,9 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t stride
 // A workgroup's tile.  Small: 4 wavefronts and 128 x 128, of which a CU has two.  Large: 8 wavefronts and 256 x 256, where bfloat16
 // products have enough of them: half the traffic to LDS and a third less from it for as many products (16,384 x 65,536 logits over 512
 // values: 1.32 ms, against 1.58).  float32 products are bound by the matrix core and gain nothing (4,099 x 20,011 logits over 128: 257 us, against 255).
+// Of fewer than 256 rows or classes it would be empty in part, and its one plane of p would have few of them to be right on average over: 1 row, 70,000
+// classes and 64 values take 72 us a step in Small, against 100; 66,001 rows, 10 classes and 512 values 150, against 179; but 255 rows, 66,000
+// classes and 512 values 250, with two planes, against 227 with one.
 // Tiny: 64 x 64, where there are so few tiles that the time of one counts, or so few rows or classes that most of a larger one
 // would be empty; float32 products, whose steps take sixteen times as long, sooner than bfloat16 ones.  Both calls, in us: 1,021 rows
 // and 10 classes 31, against 57 in Small; 1 row and 100,000 classes 81, against 130 (both float32); 60 rows and 30,000 classes 50, against 57
@@ -779,7 +782,8 @@ Plan plan_operands(const head_classes &c)
     auto tiles = [&](int64_t tile) { return ceil_div(c.n_rows, tile) * ceil_div(c.n_classes, tile); };
     const bool narrow = c.n_rows <= Tiny::TILE || c.n_classes <= Tiny::TILE;
     const bool tiny = c.dtype == HEAD_F32 ? narrow || tiles(Small::TILE) < Small::RESIDENT : tiles(Small::TILE) < Small::RESIDENT / 2;
-    p.size = c.dtype == HEAD_BF16 && tiles(Large::TILE) >= Large::RESIDENT ? LARGE : tiny ? TINY : SMALL;
+    const bool large = c.dtype == HEAD_BF16 && std::min(c.n_rows, c.n_classes) >= Large::TILE && tiles(Large::TILE) >= Large::RESIDENT;
+    p.size = large ? LARGE : tiny ? TINY : SMALL;
     p.tile = p.size == LARGE ? Large::TILE : p.size == TINY ? Tiny::TILE : Small::TILE;
     p.resident = p.size == LARGE ? Large::RESIDENT : p.size == TINY ? Tiny::RESIDENT : Small::RESIDENT;
     const int e = value_bytes(c.dtype);

@@ -90,3 +90,32 @@ def test_cross_entropy_rows_without_a_target_have_no_say_in_the_precision(n, dim
     gl[none] = 3e38
     for x, y, what in zip(pk.head_cross_entropy_grad(gl, h, w, t, lse, b), want, ("grad_hidden", "grad_weight", "grad_bias")):
         assert torch.equal(x, y), what
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,dim,classes", [(1, 64, 70_000), (5, 64, 100_000), (255, 24, 66_000), (66_001, 24, 10), (66_001, 24, 255), (500, 40, 3000)])
+def test_cross_entropy_of_few_rows_or_classes_keeps_gradients_of_logits_in_16_bits(n, dim, classes):
+    """Two bfloat16 planes hold the gradient of a logit to 2^-16 of itself, wherever there are fewer than 256 rows or classes, or few of both."""
+    import torch
+    h, w, b, t = _classes(n + classes, n, dim, classes, torch.bfloat16)
+    t[0] = classes - 1
+    has = (t >= 0) & (t < classes)
+    h64, w64 = h.double(), w.double()
+    logits, size = h64 @ w64.T + b.double(), h64.abs() @ w64.abs().T + b.double().abs()
+    lse64 = torch.logsumexp(logits, 1)
+    gl = torch.rand(n, device="cuda") / n
+    lse = lse64.float()
+    got_h, got_w, got_b = pk.head_cross_entropy_grad(gl, h, w, t, lse, b)
+    p = torch.exp(logits - lse64[:, None])
+    rel = 4 * (dim + 2) * U * size + 2 * U * (lse64.abs()[:, None] + logits.abs()) + 8 * U
+    g = (gl.double() * has)[:, None]
+    off = g * (2 * p * rel + 4 * U)
+    row = torch.nonzero(has)[:, 0]
+    p[row, t[row].long()] -= 1
+    p *= g
+    off += 2.0 ** -16 * p.abs()
+    want = p @ w64
+    _within(got_h, want, off @ w64.abs() * 1.01 + 4 * (classes + 8) * U * (p.abs() @ w64.abs()) + 2.0 ** -8 * 1.01 * want.abs(), "grad_hidden")
+    want = p.T @ h64
+    _within(got_w, want, off.T @ h64.abs() * 1.01 + 4 * (n + 8) * U * (p.abs().T @ h64.abs()) + 2.0 ** -8 * 1.01 * want.abs(), "grad_weight")
+    _within(got_b, p.sum(0), off.sum(0) + (n + 8) * U * p.abs().sum(0), "grad_bias")
