@@ -142,8 +142,8 @@ int head_cross_entropy_grad(const head_classes *c, const float *lse, const float
  *     param -= rate * decay * param + rate / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * bits == 32: m, v are float32 [n].  bits == 8: m, v are e4m3 codes [n], of m and of the root of v, and m_scale, v_scale
  * have a byte s for each HEAD_BLOCK values: a code's value counts times 2^(s - 134), where s - 127 is the exponent of the
- * block's largest magnitude (s == 0: a block of zeros; states start as zero bytes).  Codes are rounded up where the
- * fraction that they cannot hold plus a random number reaches one, so that they are right on average, and small changes
+ * block's largest magnitude, or -120 where that is less (s == 0: a block of zeros; states start as zero bytes).  Codes, of
+ * values times 2^(134 - s) to a float32 rounding, are rounded up where the fraction that they cannot hold plus a random number reaches one, so that they are right on average, and small changes
  * of v are not lost; a root of v above 0 never gets the code of 0, because m divided by it would have no bound.  The random
  * number is a hash of seed, step, the tensor's place in the list and the value's in the tensor.  A state that is not
  * finite is kept as the code of NaN, and does not count for the block's scale.

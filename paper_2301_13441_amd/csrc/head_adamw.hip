@@ -72,11 +72,12 @@ __device__ __forceinline__ void decode(const Values<uint8_t, N> &code, int s, fl
     for (int i = 0; i < N; ++i) x[i] = ldexpf(x[i], s - 134);
 }
 
-// Scale byte of a block whose largest finite magnitude is `most`: its exponent + 127, at least 1; 0 for a block of zeros.
+// Scale byte of a block whose largest finite magnitude is `most`: its exponent + 127, at least 7, for 2^(134 - 7) is the largest power
+// of two in float32; 0 for a block of zeros.
 __device__ __forceinline__ int scale_of(float most)
 {
     if (!(most > 0)) return 0;
-    return max(1, static_cast<int>(__float_as_uint(most) >> 23));
+    return max(7, static_cast<int>(__float_as_uint(most) >> 23));
 }
 
 // 2^(134 - s), by which a block of scale s is multiplied before it is coded.  By powf, which misses some powers by one rounding
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Batch b, const Num
 {
     __shared__ float factor[256];
     if constexpr (EIGHT) {
-        factor[threadIdx.x] = threadIdx.x ? factor_of(threadIdx.x) : 0.0f;  // a block of zeros
+        factor[threadIdx.x] = threadIdx.x >= 7 ? factor_of(threadIdx.x) : 0.0f;  // a block of zeros has scale 0
         __syncthreads();
     }
     const int64_t blocks = b.first[b.count];

@@ -119,3 +119,91 @@ def test_cross_entropy_of_few_rows_or_classes_keeps_gradients_of_logits_in_16_bi
     want = p.T @ h64
     _within(got_w, want, off.T @ h64.abs() * 1.01 + 4 * (n + 8) * U * (p.abs().T @ h64.abs()) + 2.0 ** -8 * 1.01 * want.abs(), "grad_weight")
     _within(got_b, p.sum(0), off.sum(0) + (n + 8) * U * p.abs().sum(0), "grad_bias")
+
+
+def _hash(x):
+    """The 32-bit hash of the 8-bit states' random numbers, of numbers held in 64 bits."""
+    x = ((x ^ (x >> 16)) * 0x7FEB352D) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0x846CA68B) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def _powers(k):
+    """2^k in float64, exactly: the power function may miss some by a rounding."""
+    import torch
+    return torch.tensor([2.0 ** i for i in range(-200, 200)], dtype=torch.float64, device="cuda")[k.long() + 200]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("exponent", [-9, -1, 40])
+def test_adamw_codes_of_8_bit_states_are_those_of_the_format(exponent):
+    """Every code of m and of the root of v, from exact powers of two, but for values whose sum with the random number is next to a
+    code's edge: what is coded may be off by a float32 rounding."""
+    import torch
+    n, seed, step = 1 << 23, 7, 1
+    g = torch.Generator(device="cuda").manual_seed(exponent + 100)
+    mantissa, down, sign = (torch.randint(0, k, (n,), generator=g, device="cuda") for k in (1 << 23, 5, 2))
+    x = (1 + mantissa * 2.0 ** -23) * _powers(exponent - down).float() * (1 - 2 * sign)
+    x[::128] = 1.75 * 2.0 ** exponent                    # the largest of each block or not: its exponent is
+    p = torch.zeros(n, device="cuda")
+    state = pk.head_adamw_state(p, 8)
+    pk.head_adamw([p], [x], [state], step, 0.0, 0.0, 0.0, seed=seed)      # m = x; the root of v is |x|
+    assert (state.m_scale == exponent + 127).all() and (state.v_scale == exponent + 127).all()
+    key = _hash((_hash((seed + 0x9E3779B9 * step) & 0xFFFFFFFF) + 0) & 0xFFFFFFFF)
+    random = _hash((torch.arange(n, device="cuda") + key) & 0xFFFFFFFF)
+    y = x.double().abs() * 2.0 ** (7 - exponent)
+    e = torch.frexp(y)[1] - 1
+    for code, u in ((state.m, random & 0xFFFF), (state.v, random >> 16)):
+        low, high = (torch.floor(y * (1 + off) * _powers(3 - e) + u.double() / 65536).long() for off in (-U, U))
+        assert (low != high).sum() < n / 2 ** 17
+        # steps of 2^(e - 3), of which 16 are the next exponent's first
+        have = code.long() - 8 * (e + 6).long() - (128 * (x < 0) if code is state.m else 0)
+        assert ((have >= low) & (have <= high)).all()
+
+
+@pytest.mark.gpu
+def test_adamw_8_bit_states_of_the_smallest_magnitudes():
+    """Blocks whose largest m is between 2^-149 and 2^-110, with exact zeros among them: within a step of the code, zeros stay zeros,
+    and what cannot be held is right on average."""
+    import torch
+    exponents = torch.arange(-149, -109, device="cuda")
+    n = 128 * len(exponents) * 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    top = exponents.repeat_interleave(64)                # 64 blocks of each
+    least = torch.clamp(top - 12, min=-149)
+    at = (least[:, None] + (torch.rand(len(top), 128, generator=g, device="cuda") * (top - least + 1)[:, None]).long()).clamp(max=top[:, None])
+    x = ((1 + torch.rand(len(top), 128, generator=g, device="cuda", dtype=torch.float64)) * _powers(at)).float()
+    x *= torch.randint(0, 2, x.shape, generator=g, device="cuda") * 2 - 1
+    x[:, 0] = _powers(top).float()
+    x[x.abs() >= _powers(top[:, None] + 1).float()] = 0        # rounded up out of the block's exponent
+    x[:, 1::5] = 0
+    p = torch.zeros(n, device="cuda")
+    state = pk.head_adamw_state(p, 8)
+    pk.head_adamw([p], [x.reshape(-1)], [state], 1, 1e-3, 0.0, 0.0, decay=0.0, seed=3)   # m = x; squares of such are zero
+    s = torch.clamp(top + 127, min=7)
+    assert torch.equal(state.m_scale.long(), s)
+    code = state.m.long().reshape(-1, 128)
+    e, d = code >> 3 & 15, code & 7
+    unit = _powers(s - 134)[:, None]
+    have = torch.where(e > 0, (8 + d) * _powers(e - 10), d * 2.0 ** -9) * unit * torch.where(code > 127, -1.0, 1.0)
+    want = x.double()
+    step = torch.maximum(2.0 ** -3 * want.abs(), 2.0 ** -9 * unit)
+    assert (code[x == 0] & 127 == 0).all()
+    assert ((have - want).abs() <= step).all()
+    # right on average: each value's rounding has at most half a step's standard deviation
+    off, room = (have - want).sum(1), 6 * 0.5 * (step ** 2).sum(1).sqrt()
+    assert (off.abs() <= room).all()
+    (m, v), = pk.head_adamw_values([state], [p])
+    assert (v == 0).all() and torch.equal(m.double().reshape(-1, 128), have.bfloat16().double()) and torch.isfinite(p).all()
+
+
+@pytest.mark.gpu
+def test_adamw_8_bit_states_without_gradients_come_to_zero():
+    """m of vectors that get no gradient any more: down through the smallest numbers to zero, not to a value that stays."""
+    import torch
+    p, state = torch.zeros(256, device="cuda"), pk.head_adamw_state(torch.zeros(256, device="cuda"), 8)
+    pk.head_adamw([p], [torch.linspace(-1, 1, 256, device="cuda") * 1e-30], [state], 1, 1e-3, seed=1)
+    none = torch.zeros(256, device="cuda")
+    for step in range(2, 700):                           # 0.9^700 * 1e-31 is far below 2^-149
+        pk.head_adamw([p], [none], [state], step, 1e-3, seed=1)
+    assert (state.m & 127 == 0).all() and (state.m_scale == 0).all()
