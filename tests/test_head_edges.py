@@ -207,3 +207,130 @@ def test_adamw_8_bit_states_without_gradients_come_to_zero():
     for step in range(2, 700):                           # 0.9^700 * 1e-31 is far below 2^-149
         pk.head_adamw([p], [none], [state], step, 1e-3, seed=1)
     assert (state.m & 127 == 0).all() and (state.m_scale == 0).all()
+
+
+def _embed_case(seed, n, t, each, dim, dtype):
+    """Ids with -1, ids past all vectors, vector 0 of nobody but row 7, whole rows without a vector; and their sums in float64."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    ids = torch.randint(0, each, (n, t), generator=g, device="cuda", dtype=torch.int32)
+    some = torch.rand(n, t, generator=g, device="cuda")
+    ids[some < 0.15] = -1
+    ids[some > 0.95] = 2 ** 31 - 1
+    ids[[0, n // 2, n - 1]] = -3
+    ids[:, 0][ids[:, 0] == 0] = 1
+    ids[7, 0] = 0
+    offsets = torch.arange(t, device="cuda") * each
+    vectors = t * each
+    table = torch.randn(vectors, dim, generator=g, device="cuda").to(dtype)
+    at = ids.long() + offsets
+    here = (ids >= 0) & (at < vectors)
+    return ids, offsets, table, torch.where(here, at, vectors)
+
+
+def _sums(at, values, n):
+    """Sums of the rows of `values` that go to each of n places, in float64 on the host; what goes to place n is dropped."""
+    import torch
+    at, values = at.cpu().numpy(), values.cpu().numpy()
+    return torch.from_numpy(np.stack([np.bincount(at, v, n + 1)[:n] for v in values.T], 1)).cuda()
+
+
+# Rows, ids, vectors of each id, dim: what the kernel for many rows with many ids takes (16 ids, 4,096 rows times the groups of a wavefront), with rows
+# that end inside a group's four, ids that are no multiple of a group's lanes, and vectors longer than a group reads at once.
+SWEEP = [(16_389, 17, 40, 64), (32_771, 17, 40, 64), (8_195, 33, 25, 128), (16_391, 16, 25, 128), (4_099, 16, 60, 520), (4_097, 70, 9, 1032), (65_541, 20, 30, 16),
+         (65_543, 131, 3, 32), (65_537, 65, 3, 24)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,t,each,dim", SWEEP)
+def test_embed_of_many_rows_with_many_ids(n, t, each, dim, dtype):
+    import torch
+    ids, offsets, table, at = _embed_case(n + t, n, t, each, dim, getattr(torch, dtype))
+    table[0] = float("nan")                              # what an id without a vector may read
+    scale = 0.37
+    wide = torch.cat([table.double(), torch.zeros(1, dim, dtype=torch.float64, device="cuda")])
+    want, size = (torch.zeros(n, dim, dtype=torch.float64, device="cuda") for _ in range(2))
+    for k in range(t):
+        want += wide[at[:, k]]
+        size += wide[at[:, k]].abs()
+    other = torch.arange(n, device="cuda") != 7
+    room = torch.full((n, t + 3), -1, dtype=torch.int32, device="cuda")
+    room[:, :t] = ids
+    room[:, t:] = 0                                      # behind a row's ids: read by nobody
+    for i in (ids, room[:, :t]):
+        got = pk.head_embed(table, i, offsets, scale)
+        assert torch.isnan(got[7]).all()
+        last = 2.0 ** -8 if dtype == "bfloat16" else U
+        _within(got[other], scale * want[other], scale * ((t + 2) * U * size + last * want.abs())[other])
+        assert (got[[0, n // 2, n - 1]] == 0).all()
+    assert torch.equal(got[other], pk.head_embed(table, ids, offsets, scale)[other])
+    plain = pk.head_embed(table, (ids.long() + offsets).clamp(-1, 2 ** 31 - 1).int().where(ids >= 0, -1), None, scale)
+    assert torch.equal(plain[other], got[other])         # the same vectors without offsets
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,vectors", [(2 ** 20 - 1, 500), (2 ** 20, 500), (2 ** 20 + 1, 70_000), (2_100_003, 3), (4_300_001, 1_100_000)])
+def test_embed_gradient_of_very_many_lookups(n, vectors):
+    """One id a row at 2^20 pairs, where a lane of the sort takes 16, and up to 526 tiles of those; chunks of 32 to 128 pairs."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.randint(0, vectors, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[torch.rand(n, generator=g, device="cuda") < 0.3] = vectors - 1
+    ids[torch.rand(n, generator=g, device="cuda") < 0.1] = -1
+    grad = torch.randint(-3, 4, (n, 4), generator=g, device="cuda").float()     # sums of small whole numbers are exact
+    want = _sums(torch.where(ids < 0, vectors, ids.long()), grad.double(), vectors)
+    got = pk.head_embed_grad(grad, ids, vectors)
+    assert torch.equal(got.double(), want)
+    assert torch.equal(got, pk.head_embed_grad(grad, ids, vectors))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,t,each,dim", [(8_195, 128, 700, 31), (16_389, 70, 2000, 64), (67_203, 64, 40, 8)])
+def test_embed_gradient_of_many_rows_with_many_ids(n, t, each, dim, dtype):
+    import torch
+    ids, offsets, table, at = _embed_case(n, n, t, each, dim, getattr(torch, dtype))
+    vectors = t * each
+    grad = torch.randn(n, dim, device="cuda").to(table.dtype)
+    grad[n // 2] = float("nan")                          # a row without a vector
+    row = torch.arange(n, device="cuda")[:, None].expand(n, t).reshape(-1)
+    at = at.reshape(-1)
+    want, size = _sums(at, grad[row].double(), vectors), _sums(at, grad[row].double().abs(), vectors)
+    count = _sums(at, torch.ones(n * t, 1, dtype=torch.float64, device="cuda"), vectors)
+    got = pk.head_embed_grad(grad, ids, vectors, offsets, 0.37)
+    last = 2.0 ** -8 if dtype == "bfloat16" else U
+    _within(got, 0.37 * want, 0.37 * ((count + 2) * U * size + last * want.abs()))
+    assert (got[count[:, 0] == 0] == 0).all()
+    assert torch.equal(got, pk.head_embed_grad(grad, ids, vectors, offsets, 0.37))
+
+
+@pytest.mark.gpu
+def test_cross_entropy_in_several_pieces_of_the_classes_in_bfloat16():
+    """So many rows that p of all classes is larger than a piece: pieces' parts of grad_hidden, scaled by grad_loss's largest magnitude, add up."""
+    import torch
+    n, dim, classes = 270_001, 24, 2_100                 # three pieces, of 1024 classes and less
+    h, w, b, t = _classes(3, n, dim, classes, torch.bfloat16)
+    _, lse = pk.head_cross_entropy(h, w, t, b)
+    gl = torch.rand(n, device="cuda") * 3e-6
+    got_h, got_w, got_b = pk.head_cross_entropy_grad(gl, h, w, t, lse, b)
+    w64, want_w, size_w, want_b, size_b = w.double(), 0, 0, 0, 0
+    for lo in range(0, n, 30_000):
+        h64, t64, l64 = h[lo:lo + 30_000].double(), t[lo:lo + 30_000].long(), lse[lo:lo + 30_000].double()
+        has = (t64 >= 0) & (t64 < classes)
+        g = (gl[lo:lo + 30_000].double() * has)[:, None]
+        logits = h64 @ w64.T + b.double()
+        size = h64.abs() @ w64.abs().T + b.double().abs()
+        p = torch.exp(logits - l64[:, None])
+        off = g * (2 * p * (4 * (dim + 2) * U * size + 2 * U * (l64.abs()[:, None] + logits.abs()) + 8 * U) + 4 * U)
+        row = torch.nonzero(has)[:, 0]
+        p[row, t64[row]] -= 1
+        p *= g
+        want_b, size_b = want_b + p.sum(0), size_b + (off + (n + 8) * U * p.abs()).sum(0)
+        off += 2.0 ** -8 * p.abs()
+        want = p @ w64
+        _within(got_h[lo:lo + 30_000], want, off @ w64.abs() * 1.01 + 4 * (classes + 8) * U * (p.abs() @ w64.abs()) + 2.0 ** -8 * 1.01 * want.abs(), "grad_hidden")
+        want_w = want_w + p.T @ h64
+        size_w = size_w + off.T @ h64.abs() * 1.01 + 4 * (n / 16 + 8) * U * (p.abs().T @ h64.abs())
+    _within(got_w, want_w, size_w + 2.0 ** -8 * 1.01 * want_w.abs(), "grad_weight")
+    _within(got_b, want_b, size_b, "grad_bias")
