@@ -4,11 +4,12 @@
 //
 // A CPython extension on torch's C++ interface.  It is given the addresses of the library's entry points (bind) and knows nothing
 // else of the library but head.h.  What it does not take (anything but plain contiguous tensors of the current device that fit
-// each other, active torch function or dispatch modes) it declines with None, and the caller goes the general way, whose
+// each other and of which autograd wants no record, active torch function or dispatch modes) it declines with None, and the caller goes the general way, whose
 // checks raise the errors; an entry point's error code is returned as an int.
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
@@ -46,11 +47,19 @@ PyObject *declined() { Py_RETURN_NONE; }
 bool modes() { return at::impl::PythonTorchFunctionTLS::stack_len() > 0 || c10::impl::TorchDispatchModeTLS::any_modes_set(); }
 
 // A plain contiguous device tensor; null otherwise.
-const at::Tensor *tensor(PyObject *o)
+const at::Tensor *plain(PyObject *o)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !t.is_conj() && !t.is_neg() && t.is_contiguous() ? &t : nullptr;
+}
+
+// One of which autograd wants no record: no gradient, no tangent.
+const at::Tensor *tensor(PyObject *o)
+{
+    const at::Tensor *t = plain(o);
+    if (!t || !t->unsafeGetTensorImpl()->autograd_meta()) return t;
+    return (t->requires_grad() && at::GradMode::is_enabled()) || t->_fw_grad(0).defined() ? nullptr : t;
 }
 
 bool of_current_device(const at::Tensor &t) { return t.get_device() == c10::hip::current_device(); }
@@ -268,7 +277,7 @@ PyObject *cross_entropy_grad(PyObject *, PyObject *const *args, Py_ssize_t n)
 // Address of n adjacent values; null: not those.
 void *values_at(PyObject *o, const at::Tensor &like, at::ScalarType type, int64_t n)
 {
-    const at::Tensor *t = tensor(o);
+    const at::Tensor *t = plain(o);
     return t && t->scalar_type() == type && t->device() == like.device() && t->numel() == n ? t->data_ptr() : nullptr;
 }
 
@@ -310,7 +319,7 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     rule.rate = numbers[0], rule.beta1 = numbers[1], rule.beta2 = numbers[2], rule.eps = numbers[3], rule.decay = numbers[4];
     rule.seed = static_cast<uint32_t>(PyLong_AsUnsignedLongLongMask(args[10]));
     if (PyErr_Occurred()) return nullptr;
-    const at::Tensor *first = tensor(PyList_GET_ITEM(args[0], 0)), *grad = tensor(PyList_GET_ITEM(args[1], 0));
+    const at::Tensor *first = plain(PyList_GET_ITEM(args[0], 0)), *grad = plain(PyList_GET_ITEM(args[1], 0));
     PyObject *state = PyList_GET_ITEM(args[2], 0);
     if (!first || !grad || !of_current_device(*first) || !PyTuple_Check(state)) return declined();
     const Py_ssize_t kind = PyTuple_GET_SIZE(state);
@@ -321,7 +330,7 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     std::vector<head_adamw_tensor> tensors(n);
     for (Py_ssize_t i = 0; i < n; ++i) {
         head_adamw_tensor &t = tensors[i];
-        const at::Tensor *p = tensor(PyList_GET_ITEM(args[0], i));
+        const at::Tensor *p = plain(PyList_GET_ITEM(args[0], i));
         if (!p || p->numel() == 0) return declined();
         t.n = p->numel();
         t.param = static_cast<float *>(values_at(PyList_GET_ITEM(args[0], i), *first, at::kFloat, t.n));
@@ -344,13 +353,13 @@ PyObject *adamw_values(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     if (n_args != 2 || !PyList_CheckExact(args[0]) || modes()) return declined();
     const Py_ssize_t n = PyList_GET_SIZE(args[0]);
     if (n == 0 || n > HEAD_MAX_TENSORS || !is_list(args[1], n)) return declined();
-    const at::Tensor *first = tensor(PyList_GET_ITEM(args[1], 0));
+    const at::Tensor *first = plain(PyList_GET_ITEM(args[1], 0));
     if (!first || !of_current_device(*first)) return declined();
     std::vector<head_adamw_tensor> tensors(n);
     std::vector<at::Tensor> m(n), v(n);
     std::vector<void *> to_m(n), to_v(n);
     for (Py_ssize_t i = 0; i < n; ++i) {
-        const at::Tensor *p = tensor(PyList_GET_ITEM(args[1], i));
+        const at::Tensor *p = plain(PyList_GET_ITEM(args[1], i));
         if (!p || p->numel() == 0 || p->device() != first->device()) return declined();
         tensors[i].n = p->numel();
         if (!state_of(PyList_GET_ITEM(args[0], i), *first, 4, tensors[i])) return declined();

@@ -5,6 +5,10 @@ All tensors of a call are on one device, the current one.  A 2-D tensor may have
 its rows' elements are adjacent.  Results are new tensors (of the stream's pool) unless the call says that it updates
 its arguments.  `stream`: the torch stream to work on, the current one by default; a tensor that belongs to another stream
 is kept from being reused until this one is done with it, but the streams are the caller's to order.
+
+Autograd records none of the calls: a gradient is a call of its own (`*_grad`).  So that none is lost without a word, tensors that require a
+gradient are refused unless recording is off (torch.no_grad(), an autograd Function's methods), and tensors with a tangent always; head_adamw, like any
+optimizer's step, takes its tensors either way.
 """
 from __future__ import annotations
 
@@ -141,6 +145,11 @@ def _tensor(t, what: str, dtype=None, shape=None, like=None):
         raise ValueError(f"{what} must be {dtype}, not {t.dtype}")
     if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
         raise ValueError(f"{what} must have shape {list(shape)}, not {list(t.shape)}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which this call does not record: make it under torch.no_grad(), and take the gradient "
+                         "from the operator's own call for it")
+    if t.is_floating_point() and torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{what} has a tangent, which this call does not carry on")
     if t.is_contiguous() or (t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
         return t
     raise ValueError(f"{what} must be contiguous" + (" along its rows, which must not overlap" if t.dim() == 2 else ""))

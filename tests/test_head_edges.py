@@ -334,3 +334,37 @@ def test_cross_entropy_in_several_pieces_of_the_classes_in_bfloat16():
         size_w = size_w + off.T @ h64.abs() * 1.01 + 4 * (n / 16 + 8) * U * (p.abs().T @ h64.abs())
     _within(got_w, want_w, size_w + 2.0 ** -8 * 1.01 * want_w.abs(), "grad_weight")
     _within(got_b, want_b, size_b, "grad_bias")
+
+
+@pytest.mark.gpu
+def test_what_would_lose_a_gradient_is_refused():
+    """The operators record nothing for autograd: a tensor that requires a gradient is refused where torch would record one, and so is a tangent."""
+    import torch
+    x, w, b = torch.randn(4, 8, device="cuda"), torch.ones(8, device="cuda"), torch.zeros(8, device="cuda")
+    ids, t = torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    k, one = torch.randn(5, 8, device="cuda"), torch.ones(4, device="cuda")
+    y, mean, rstd = pk.head_layer_norm(x, w, b)
+    loss, lse = pk.head_cross_entropy(x, k, t)
+    calls = {pk.head_embed: ((k, ids), 1), pk.head_embed_grad: ((x, ids, 5), 1), pk.head_layer_norm: ((x, w, b), 3),
+             pk.head_layer_norm_grad: ((x, x.clone(), w, mean, rstd), 5), pk.head_cross_entropy: ((x, k, t, torch.zeros(5, device="cuda")), 4),
+             pk.head_cross_entropy_grad: ((one, x, k, t, lse, torch.zeros(5, device="cuda")), 6)}
+    other = torch.cuda.Stream()
+    for call, (args, some) in calls.items():
+        for i in range(some):
+            if not args[i].is_floating_point():
+                continue
+            asks = args[i].detach().clone().requires_grad_()
+            with_it = (*args[:i], asks, *args[i + 1:])
+            for stream in (None, other):
+                with pytest.raises(ValueError, match="gradient"):
+                    call(*with_it, stream=stream)
+            with torch.no_grad():
+                call(*with_it)
+            with torch.autograd.forward_ad.dual_level():
+                dual = torch.autograd.forward_ad.make_dual(args[i].detach(), torch.ones_like(args[i]))
+                with pytest.raises(ValueError, match="tangent"):
+                    call(*args[:i], dual, *args[i + 1:])
+    # an optimizer's step is no part of the graph
+    p = x.clone().requires_grad_()
+    pk.head_adamw([p], [x], [pk.head_adamw_state(p)], 1, 1e-3)
+    torch.cuda.synchronize()
