@@ -281,6 +281,13 @@ void *values_at(PyObject *o, const at::Tensor &like, at::ScalarType type, int64_
     return t && t->scalar_type() == type && t->device() == like.device() && t->numel() == n ? t->data_ptr() : nullptr;
 }
 
+// Before values are written: what autograd has kept of a tensor is out of date.
+void written(PyObject *o)
+{
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The states of a parameter: (m, v) or (m, m_scale, v, v_scale).
 bool state_of(PyObject *o, const at::Tensor &like, Py_ssize_t kind, head_adamw_tensor &t)
 {
@@ -338,6 +345,12 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n_args)
         if (!t.param || !t.grad || !state_of(PyList_GET_ITEM(args[2], i), *first, kind, t)) return declined();
         PyObject *copy = args[3] == Py_None ? Py_None : PyList_GET_ITEM(args[3], i);
         if (copy != Py_None && !(t.copy = values_at(copy, *first, at::kBFloat16, t.n))) return declined();
+    }
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        written(PyList_GET_ITEM(args[0], i));
+        PyObject *states = PyList_GET_ITEM(args[2], i);
+        for (Py_ssize_t k = 0; k < kind; ++k) written(PyTuple_GET_ITEM(states, k));
+        if (args[3] != Py_None && PyList_GET_ITEM(args[3], i) != Py_None) written(PyList_GET_ITEM(args[3], i));
     }
     void *stream = stream_of(*first);
     const int rc = without_gil([&] { return entry.adamw(&rule, tensors.data(), static_cast<int32_t>(n), stream); });

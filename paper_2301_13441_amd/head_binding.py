@@ -449,6 +449,8 @@ def head_adamw(params, grads, states, step: int, rate: float, beta1: float = 0.9
     rule = _AdamwRule(grad_dtype, 32 if kind == 2 else 8, step, rate, beta1, beta2, eps, decay, seed & 0xFFFFFFFF)
     used = [] if stream is None else [*params, *grads, *(t for s in states for t in s), *(copies or [])]
     with _on(stream, first, used) as s:
+        written = [*params, *(t for s in states for t in s), *(c for c in copies or [] if c is not None)]
+        torch.autograd.graph.increment_version([t for t in written if not t.is_inference()])  # what autograd has kept of them is out of date
         _check(_lib().head_adamw(rule, rows, n, s), "head_adamw")
 
 

@@ -368,3 +368,22 @@ def test_what_would_lose_a_gradient_is_refused():
     p = x.clone().requires_grad_()
     pk.head_adamw([p], [x], [pk.head_adamw_state(p)], 1, 1e-3)
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_adamw_tells_autograd_that_it_wrote():
+    """What a graph has kept of a parameter is out of date after a step, and its backward pass says so."""
+    import torch
+    for stream in (None, torch.cuda.Stream()):
+        p, g = torch.ones(8, device="cuda", requires_grad=True), torch.ones(8, device="cuda")
+        copy, state = torch.empty(8, dtype=torch.bfloat16, device="cuda"), pk.head_adamw_state(p.detach())
+        loss = (p * p).sum()
+        torch.cuda.synchronize()
+        pk.head_adamw([p], [g], [state], 1, 1e-3, copies=[copy], stream=stream)
+        torch.cuda.synchronize()
+        assert all(t._version > 0 for t in (p, copy, *state)) and g._version == 0
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():                         # such tensors have no version
+        p = torch.ones(8, device="cuda")
+        pk.head_adamw([p], [torch.ones(8, device="cuda")], [pk.head_adamw_state(p)], 1, 1e-3)
