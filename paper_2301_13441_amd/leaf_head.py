@@ -91,12 +91,15 @@ class LeafHead:
 
     def predict(self, leaves, linear=None):
         """(probabilities, labels) of the rows.  linear: what linear() gave, kept over calls; by default it is made anew."""
+        import torch
+        if self.n_classes == 1:  # a linear model of one output has a threshold and no softmax
+            n = leaves.shape[0]
+            return torch.ones(n, 1, device=self.bias.device), torch.zeros(n, dtype=torch.int32, device=self.bias.device)
         made = linear is None
         linear = self.linear() if made else linear
         try:
             return linear.predict(self._hidden(leaves)[1].float())
         finally:
             if made:
-                import torch
                 torch.cuda.current_stream().synchronize()  # the weights go with the handle
                 linear.close()

@@ -387,3 +387,17 @@ def test_adamw_tells_autograd_that_it_wrote():
     with torch.inference_mode():                         # such tensors have no version
         p = torch.ones(8, device="cuda")
         pk.head_adamw([p], [torch.ones(8, device="cuda")], [pk.head_adamw_state(p)], 1, 1e-3)
+
+
+@pytest.mark.gpu
+def test_a_head_of_one_class_gives_it_every_row():
+    import torch
+    head = pk.LeafHead([0, 5, 9], n_classes=1, dim=8, seed=2)
+    head.bias.fill_(3.0)                                 # whatever its logit
+    leaves = torch.tensor([[1, 2], [4, -1], [0, 3]], dtype=torch.int32, device="cuda")
+    assert head.train_step(leaves, torch.zeros(3, dtype=torch.int32, device="cuda"), 1e-3).item() == 0
+    two = pk.LeafHead([0, 5, 9], n_classes=2, dim=8, seed=2).predict(leaves)
+    for probabilities, labels in (head.predict(leaves), head.predict(leaves[:0])):
+        n = len(labels)
+        assert probabilities.shape == (n, 1) and (probabilities == 1).all() and labels.shape == (n,) and (labels == 0).all()
+        assert probabilities.dtype == two[0].dtype and labels.dtype == two[1].dtype and probabilities.device == two[0].device
