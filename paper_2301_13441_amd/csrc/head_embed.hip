@@ -6,8 +6,8 @@
 // Forward: a vector of `dim` values is read by a group of lanes, a piece of up to 16 bytes each; groups that share a row
 // (a wavefront's, or a workgroup's where rows are few) take its ids in turn and add up their sums at the end.
 //
-// Backward: (vector, row) pairs, one for each id, are sorted by vector with a stable radix sort, 8 bits a pass: counts of
-// each digit by tile, sums over the tiles, then each tile moves its pairs to their places.  The sorted list is cut into
+// Backward: (vector, row) pairs, one for each id, are sorted by vector with a stable radix sort, up to 10 bits a pass: counts
+// of each digit by tile, sums over the tiles, then each tile moves its pairs to their places.  The sorted list is cut into
 // chunks of equal length whatever vectors they hold, so that a vector that every row has costs no more than others; a group
 // of lanes adds up a chunk, run after run of equal vectors.  A run inside a chunk is a vector's gradient.  Of runs that cross
 // chunks the parts go to the workspace, and a second kernel adds up the parts of each.  No atomics on values: the order
@@ -129,10 +129,13 @@ __global__ __launch_bounds__(1024) void embed_kernel(int64_t n_rows, int dim, Id
     }
 }
 
-// Many rows with many ids: a group of G lanes takes ROWS rows at once, all groups go through the ids in the same order, and so
-// few of them are launched that all are resident: what is read at a time is the vectors of a few ids (trees), which an L2
-// holds, and not the whole table (33 MB of leaves).  The G lanes read G ids of a row at once, and each gets every one of them from its neighbours.
-// Bound by the L2s: 103,069 rows of 128 ids, 128 bfloat16, 171 us, 17 TB/s.  Two rows of a group 201 us, eight 244, a wavefront for each row 381.
+// Many rows with many ids: a group of G lanes takes ROWS rows at once, and all groups go through the ids in the same order: what those that
+// run at the same time read is the vectors of a few ids (trees) rather than of the whole table (33 MB of leaves).  The G lanes read G ids of a row at
+// once, and each gets every one of them from its neighbours.
+// Bound by what goes from the caches to registers: 103,069 rows of 128 ids, 128 bfloat16, 171 us, 17 TB/s.  Two rows of a group 201 us, eight 244, a
+// wavefront for each row 365 to 390.  A launch of no more workgroups than are resident takes as long (a million such rows 2.0 ms either way).
+// Rounds are of G ids, there or not, so that ids are at least half of one: 20 ids, 256 float32 (G = 64), 110,000 rows take 217 us here and 203 to 218 in
+// the general kernel, 4,500 rows 21 and 15; 40 ids 254 and 371, and 23 and 24.
 template <class T, int V, int G, int ROWS>
 __global__ __launch_bounds__(THREADS) void sweep_kernel(int64_t n_rows, int dim, Ids s, const T *table, uint32_t stride_bytes, float scale,
                                                         T *out)
@@ -551,7 +554,7 @@ hipError_t embed(const head_ids &ids, int64_t dim, const T *table, int64_t table
         const int lanes = power_at_least(ceil_div(dim, V()), 64), in_wave = 64 / lanes;
         constexpr int ROWS = 4;
         if constexpr (V() * sizeof(T) == 16)
-            if (lanes >= 4 && ids.n_ids >= 16 && ids.n_rows >= int64_t{1024} * ROWS * in_wave && table_stride * sizeof(T) <= UINT32_MAX)
+            if (lanes >= 4 && ids.n_ids >= std::max(16, lanes / 2) && ids.n_rows >= int64_t{1024} * ROWS * in_wave && table_stride * sizeof(T) <= UINT32_MAX)
                 return by_lanes(lanes, [&](auto G) {
                     const dim3 grid(static_cast<uint32_t>(std::min(ceil_div(ids.n_rows, ROWS * (THREADS / G())), MAX_GRID)),
                                     static_cast<uint32_t>(ceil_div(dim, G() * V())));

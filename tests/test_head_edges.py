@@ -235,9 +235,10 @@ def _sums(at, values, n):
     return torch.from_numpy(np.stack([np.bincount(at, v, n + 1)[:n] for v in values.T], 1)).cuda()
 
 
-# Rows, ids, vectors of each id, dim: what the kernel for many rows with many ids takes (16 ids, 4,096 rows times the groups of a wavefront), with rows
+# Rows, ids, vectors of each id, dim: what the kernel for many rows with many ids takes (16 ids and half as many as a group has lanes, 4,096 rows times
+# the groups of a wavefront) and, at 16 ids of 520 values, just does not, with rows
 # that end inside a group's four, ids that are no multiple of a group's lanes, and vectors longer than a group reads at once.
-SWEEP = [(16_389, 17, 40, 64), (32_771, 17, 40, 64), (8_195, 33, 25, 128), (16_391, 16, 25, 128), (4_099, 16, 60, 520), (4_097, 70, 9, 1032), (65_541, 20, 30, 16),
+SWEEP = [(16_389, 17, 40, 64), (32_771, 17, 40, 64), (8_195, 33, 25, 128), (16_391, 16, 25, 128), (4_099, 16, 60, 520), (4_099, 33, 30, 520), (4_097, 70, 9, 1032), (65_541, 20, 30, 16),
          (65_543, 131, 3, 32), (65_537, 65, 3, 24)]
 
 
