@@ -41,7 +41,7 @@ struct Batch {
     int32_t count;
 };
 struct Numbers {
-    float beta1, rest1, beta2, rest2, keep, rate, root, eps;  // rest: 1 - beta; keep: 1 - rate decay; rate, root: with the corrections
+    float beta1, rest1, beta2, rest2, decay, rate, root, eps;  // rest: 1 - beta; decay: times the rate; rate, root: with the corrections
 };
 
 __host__ __device__ inline uint32_t hash(uint32_t x)  // a multiply and xor-shift finaliser: every bit depends on every other
@@ -201,8 +201,9 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const Batch b, const Num
             m.v[i] = c.beta1 * m.v[i] + c.rest1 * x;
             v.v[i] = c.beta2 * v.v[i] + c.rest2 * x * x;
             root[i] = sqrtf(v.v[i]);
-            // the quotient to two roundings, of a number that is small next to p
-            p.v[i] = p.v[i] * c.keep - c.rate * m.v[i] * __builtin_amdgcn_rcpf(root[i] * c.root + c.eps);
+            // The quotient to two roundings, of a number that is small next to p.  Decay and step are one difference to p: 1 - rate decay would
+            // itself be rounded, to 1 where rates are small.
+            p.v[i] -= c.decay * p.v[i] + c.rate * m.v[i] * __builtin_amdgcn_rcpf(root[i] * c.root + c.eps);
             copy.v[i] = narrow<bf16>(p.v[i]);
         }
         put(t.param + at, p, some, wide);
@@ -286,7 +287,7 @@ hipError_t launch_adamw(const head_adamw_rule &rule, const head_adamw_tensor *te
 {
     const double step = static_cast<double>(rule.step);
     const Numbers c{static_cast<float>(rule.beta1), static_cast<float>(1 - rule.beta1), static_cast<float>(rule.beta2),
-                    static_cast<float>(1 - rule.beta2), static_cast<float>(1 - rule.rate * rule.decay),
+                    static_cast<float>(1 - rule.beta2), static_cast<float>(rule.rate * rule.decay),
                     static_cast<float>(rule.rate / (1 - std::pow(rule.beta1, step))),
                     static_cast<float>(1 / std::sqrt(1 - std::pow(rule.beta2, step))), static_cast<float>(rule.eps)};
     const uint32_t key = hash(rule.seed + 0x9E3779B9u * static_cast<uint32_t>(rule.step));

@@ -402,3 +402,38 @@ def test_a_head_of_one_class_gives_it_every_row():
         n = len(labels)
         assert probabilities.shape == (n, 1) and (probabilities == 1).all() and labels.shape == (n,) and (labels == 0).all()
         assert probabilities.dtype == two[0].dtype and labels.dtype == two[1].dtype and probabilities.device == two[0].device
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_decays_at_small_rates(bits):
+    """rate * decay far below a float32 rounding of 1: lost in each step alone, it has to show on average over steps whose updates round
+    either way.  The same gradients with and without decay, whose difference is decay's."""
+    import torch
+    n, steps, rate, decay = 1 << 18, 400, 2e-6, 0.01
+    ends = []
+    for d in (0.0, decay):
+        g = torch.Generator(device="cuda").manual_seed(5)
+        p = 1 + torch.rand(n, generator=g, device="cuda") * 0.9
+        state = pk.head_adamw_state(p, bits)
+        for step in range(1, steps + 1):
+            pk.head_adamw([p], [torch.randn(n, generator=g, device="cuda")], [state], step, rate, decay=d, seed=1)
+        ends.append(p.double())
+    fallen = ((ends[0] - ends[1]) / ends[0]).mean().item()
+    # each step's rounding is off by 2^-24 of p at most, in either direction: standard error below 2^-24 * sqrt(2 * steps / n)
+    assert abs(fallen - steps * rate * decay) < 6 * U * (2 * steps / n) ** 0.5 + 0.01 * steps * rate * decay
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_rounds_a_parameter_once(bits):
+    """A parameter next to which its step is small is the exact result, rounded once."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(6)
+    p = torch.randn(100_003, generator=g, device="cuda")
+    p64, x = p.double(), torch.randn(len(p), generator=g, device="cuda")
+    rate, beta1, beta2, eps, decay = 1e-3, 0.9, 0.999, 1e-8, 0.05
+    pk.head_adamw([p], [x], [pk.head_adamw_state(p, bits)], 1, rate, beta1, beta2, eps, decay)
+    step = rate * x.double() / (x.double().abs() + eps)          # of the first step, whose corrections undo 1 - beta
+    want = p64 - (rate * decay * p64 + step)
+    _within(p, want, U * torch.maximum(want.abs(), p64.abs()) + 16 * U * (step.abs() + rate * decay * p64.abs()))
