@@ -150,7 +150,7 @@ def _tensor(t, what: str, dtype=None, shape=None, like=None):
                          "from the operator's own call for it")
     if t.is_floating_point() and torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
         raise ValueError(f"{what} has a tangent, which this call does not carry on")
-    if t.is_contiguous() or (t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
+    if t.is_contiguous() or (t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]):
         return t
     raise ValueError(f"{what} must be contiguous" + (" along its rows, which must not overlap" if t.dim() == 2 else ""))
 

@@ -437,3 +437,20 @@ def test_adamw_rounds_a_parameter_once(bits):
     step = rate * x.double() / (x.double().abs() + eps)          # of the first step, whose corrections undo 1 - beta
     want = p64 - (rate * decay * p64 + step)
     _within(p, want, U * torch.maximum(want.abs(), p64.abs()) + 16 * U * (step.abs() + rate * decay * p64.abs()))
+
+
+@pytest.mark.gpu
+def test_rows_of_one_element_may_lie_any_way():
+    """A column of a matrix, by whatever steps: a row's only element is adjacent to itself."""
+    import torch
+    whole = torch.randn(6, 32, device="cuda")
+    ids = torch.arange(6 * 32, dtype=torch.int32, device="cuda").reshape(6, 32) % 5
+    w, table = torch.ones(1, device="cuda"), torch.randn(5, 24, device="cuda")
+    x, i = whole[:, 3::8][:, :1], ids[:, 3::8][:, :1]
+    assert x.stride() == (32, 8) and not x.is_contiguous()
+    for got, want in zip(pk.head_layer_norm(x, w), pk.head_layer_norm(x.contiguous(), w)):
+        assert torch.equal(got, want)
+    assert torch.equal(pk.head_embed(table, i), pk.head_embed(table, i.contiguous()))
+    assert torch.equal(pk.head_embed(table[:, 3::8][:, :1], i), pk.head_embed(table[:, 3:4].contiguous(), i.contiguous()))
+    with pytest.raises(ValueError, match="overlap"):
+        pk.head_layer_norm(whole[:1, :1].expand(6, 1), w)
