@@ -118,7 +118,8 @@ typedef struct head_classes {
 } head_classes;
 
 /* Bytes of workspace (16-byte aligned) of the two calls below; negative HEAD_E* on error.  Of the pointers and strides in
- * `c` only the alignment counts, and whether there is a bias. */
+ * `c` only the alignment counts.  The gradients' grows with the rows: it has room for 1,024 classes of all of them, or for fewer where
+ * there are fewer. */
 int64_t head_cross_entropy_bytes(const head_classes *c);
 int64_t head_cross_entropy_grad_bytes(const head_classes *c);
 

@@ -312,7 +312,7 @@ struct Model {
 // ---- forward
 
 // Rows of C are classes and its columns rows of the batch, so that a lane has the values of one row in its registers.  16,384 x 65,536 logits
-// over 512 bfloat16: 1.27 ms, 865 TFLOP/s; bound by LDS and matrix core in turn, and by the exponentials at a tile's end, 15 vector
+// over 512 bfloat16: 1.23 to 1.32 ms, 833 to 894 TFLOP/s; bound by LDS and matrix core in turn, and by the exponentials at a tile's end, 15 vector
 // instructions for each logit in all.  4,099 x 20,011 over 128 float32: 260 us, 81 TFLOP/s.
 template <class T, class S>
 __global__ __launch_bounds__(S::THREADS, 2) void lse_kernel(Model<T> m, uint32_t row_tiles, uint32_t class_tiles, float2 *parts, float *target_logit)
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256) void lse_join_kernel(int64_t n_rows, int64_t n
 // by its largest magnitude (`scale`) first, and the results are multiplied by it: values are near -1 then, which roundings of
 // many rows, of either sign, are right for on average, and not all of one factor times that (in a mean loss 1 / n_rows, say).
 // A row without a target has logits of -inf here, so that p is 0 whatever it holds, and no bit in `has_target`, by which the products leave it out.
-// 16,384 x 32,768 bfloat16: 730 us, of which the stores alone take about half.
+// 16,384 x 32,768 bfloat16: 732 us, of which the stores alone take about half.
 template <class T, class S, bool TWO>
 __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const float *lse, const float *grad_loss, int64_t first_class,
                                                        uint32_t row_tiles, uint32_t class_tiles, T *p, int64_t stride, int64_t plane,
@@ -556,7 +556,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void p_kernel(Model<T> m, const floa
 // float32, added to what is there where `add` says so; or (out) the one part is the result.
 // TWO: A has two planes, whose products are added.  Where A lies along memory its rows are the batch's, elsewhere the sum goes over those.
 // scale: of the results, or null.  p of 16,384 rows and 32,768
-// classes, 512 columns, bfloat16: 711 us for hidden's gradient, 630 for weight's, 773 and 872 TFLOP/s; 4,099 x 20,011, 128 columns, float32: 231 and 237 us, 91 and 89, the matrix core busy for 78 %.
+// classes, 512 columns, bfloat16: 706 us for hidden's gradient, 636 for weight's, 778 and 864 TFLOP/s; 4,099 x 20,011, 128 columns, float32:
+// 230 and 238 us, 91 and 88, the matrix core busy for 78 %.
 template <class T, class S, bool A_ALONG, bool TWO>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Operand<T> a, Operand<T> b, int64_t dim, uint32_t row_tiles,
                                                              uint32_t column_tiles, uint32_t splits, int64_t split_depth, int64_t plane,
@@ -710,7 +711,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *from, int64_t stride
 
 // A workgroup's tile.  Small: 4 wavefronts and 128 x 128, of which a CU has two.  Large: 8 wavefronts and 256 x 256, where bfloat16
 // products have enough of them: half the traffic to LDS and a third less from it for as many products (16,384 x 65,536 logits over 512
-// values: 1.32 ms, against 1.58).  float32 products are bound by the matrix core and gain nothing (4,099 x 20,011 logits over 128: 257 us, against 255).
+// values: 1.23 to 1.32 ms, against 1.58).  float32 products are bound by the matrix core and gain nothing (4,099 x 20,011 logits over 128: 257 us, against 255).
 // Of fewer than 256 rows or classes it would be empty in part, and its one plane of p would have few of them to be right on average over: 1 row, 70,000
 // classes and 64 values take 72 us a step in Small, against 100; 66,001 rows, 10 classes and 512 values 150, against 179; but 255 rows, 66,000
 // classes and 512 values 250, with two planes, against 227 with one.

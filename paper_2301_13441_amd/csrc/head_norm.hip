@@ -21,7 +21,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_GRID = 1 << 22;       // workgroups of the forward pass: 2^30 threads, a grid's axis has room for 2^32
-// A y of so many bytes is no more in the 32 MB of the L2s when it is read: its stores are non-temporal (515,345 x 90 float32: 90 us, 4.1 TB/s,
+// A y of so many bytes is no more in the 32 MB of the L2s when it is read: its stores are non-temporal (515,345 x 90 float32: 89 us, 4.2 TB/s,
 // against 107).  The backward pass, which reads twice what it writes, gains nothing (295 us, against 296).
 constexpr int64_t PAST_BYTES = int64_t{64} << 20;
 constexpr int MAX_WORKGROUPS = 768;   // of the backward pass, three for each of 256 CUs: rows of its workspace
@@ -53,8 +53,8 @@ __device__ __forceinline__ int column(int i)
     return (i * LANES + static_cast<int>(threadIdx.x % LANES)) * V;
 }
 
-// A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.  515,345 rows of 90 float32: 92
-// us, 4.0 TB/s; one row at a time 195, eight 118 (both with ordinary stores, as 107).
+// A team takes ROWS rows at once where a lane has few values of each: their loads are on their way together.  515,345 rows of 90 float32: 89
+// us, 4.2 TB/s; one row at a time 195, eight 118 (both with ordinary stores, as 107).
 template <class T, int V, int LANES, int N, int ROWS, bool PAST>
 __global__ __launch_bounds__(THREADS) void norm_kernel(int64_t n_rows, int dim, const T *x, int64_t x_stride, const float *weight,
                                                        const float *bias, float eps, T *y, float *mean, float *rstd)
