@@ -42,11 +42,11 @@ enum {
 /* Documented limits (HEAD_ELIMIT): */
 #define HEAD_MAX_DIM 16384           /* dim */
 #define HEAD_MAX_ROWS 1000000000     /* n_rows */
-#define HEAD_MAX_VECTORS 1000000000  /* n_vectors, n_classes */
+#define HEAD_MAX_VECTORS 1000000000  /* n_vectors, n_classes, n_outputs */
 #define HEAD_MAX_IDS 2147483647      /* n_ids */
 #define HEAD_MAX_TOKENS 2147483647   /* n_rows * n_ids, of head_embed_grad */
-#define HEAD_MAX_LOGITS (INT64_C(1) << 44) /* n_rows * n_classes */
-#define HEAD_MAX_TENSORS 1000000     /* tensors of one head_adamw call */
+#define HEAD_MAX_LOGITS (INT64_C(1) << 44) /* n_rows * n_classes, n_rows * n_outputs */
+#define HEAD_MAX_TENSORS 1000000     /* tensors of one head_adamw or head_clip call */
 #define HEAD_BLOCK 128               /* values that share a scale byte in the 8-bit states */
 
 /*
@@ -138,6 +138,61 @@ int head_cross_entropy_grad(const head_classes *c, const float *lse, const float
                             void *grad_weight, float *grad_bias, void *workspace, void *stream);
 
 /*
+ * A dense layer and its batch: z[r][k] = sum_d x[r][d] * weight[k][d] + bias[k].  x [n_rows][dim] and weight of dtype, bias float32
+ * or NULL (zeros).  head_linear: weight is [n_outputs][dim], and an activation follows.  head_gated: weight is [2 * n_outputs][dim]
+ * and bias [2 * n_outputs]; the first n_outputs columns of z are gates, the others values, and each value is multiplied by the
+ * activation of its gate.
+ *
+ * HEAD_GELU is x times the normal distribution's integral up to x, HEAD_SILU x / (1 + exp(-x)); the slope of HEAD_RELU at 0 is 0.
+ * For bfloat16 values activations and slopes are right to 2^-13, relative to the activation and to 1, which is small next to their results'
+ * rounding.
+ */
+enum { HEAD_IDENTITY = 0, HEAD_RELU = 1, HEAD_GELU = 2, HEAD_SILU = 3 };
+
+typedef struct head_layer {
+    int32_t dtype;
+    int32_t activation;
+    int64_t n_rows;
+    int64_t dim;
+    int64_t n_outputs;
+    const void *x;
+    int64_t x_stride;
+    const void *weight;
+    int64_t weight_stride;
+    const float *bias; /* not read by the gradients */
+} head_layer;
+
+/* Bytes of workspace (16-byte aligned) of the four calls below; negative HEAD_E* on error.  Of the pointers and strides in `l` only
+ * the alignment counts.  The gradients' holds the gradient of z, and grows with the rows. */
+int64_t head_linear_bytes(const head_layer *l);
+int64_t head_linear_grad_bytes(const head_layer *l);
+int64_t head_gated_bytes(const head_layer *l);
+int64_t head_gated_grad_bytes(const head_layer *l);
+
+/*
+ * y = residual + scale * activation(z); residual [n_rows][n_outputs] of dtype or NULL (zeros), y [n_rows][n_outputs] of dtype; z, of
+ * the same shape and type, or NULL (not wanted): what the gradients need where there is an activation.  Sums, z, activation and y's terms
+ * are float32, y and z are rounded from those.
+ */
+int head_linear(const head_layer *l, const void *residual, int64_t residual_stride, float scale, void *y, void *z, void *workspace,
+                void *stream);
+
+/*
+ * The gradients from grad [n_rows][n_outputs] (of y): grad_x [n_rows][dim] and grad_weight [n_outputs][dim] of dtype, grad_bias
+ * [n_outputs] float32 or NULL (not wanted).  That of the residual is grad itself.  z is what head_linear gave; with HEAD_IDENTITY it
+ * is not read and may be NULL.  In bfloat16 the gradient of z is rounded before it is multiplied, as z was before.
+ */
+int head_linear_grad(const head_layer *l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, float scale,
+                     void *grad_x, void *grad_weight, float *grad_bias, void *workspace, void *stream);
+
+/* y = activation(gates) * values, [n_rows][n_outputs] of dtype; z [n_rows][2 * n_outputs] of dtype or NULL (not wanted). */
+int head_gated(const head_layer *l, void *y, void *z, void *workspace, void *stream);
+
+/* The gradients, likewise: grad [n_rows][n_outputs], grad_weight [2 * n_outputs][dim], grad_bias [2 * n_outputs]. */
+int head_gated_grad(const head_layer *l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, void *grad_x,
+                    void *grad_weight, float *grad_bias, void *workspace, void *stream);
+
+/*
  * One AdamW step over all tensors.  For every value, with step >= 1 counting from the first one:
  *     m = beta1 * m + (1 - beta1) * g;  v = beta2 * v + (1 - beta2) * g * g
  *     param -= rate * decay * param + rate / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
@@ -175,6 +230,25 @@ int head_adamw(const head_adamw_rule *rule, const head_adamw_tensor *tensors, in
  * only m, v, m_scale, v_scale and n are used; out_m[i] and out_v[i] ([n] bfloat16) are HOST arrays of device pointers.
  */
 int head_adamw_values(const head_adamw_tensor *tensors, void *const *out_m, void *const *out_v, int32_t n_tensors, void *stream);
+
+/*
+ * The 2-norm of the values of all tensors together, and every value times min(1, max_norm / norm), in float32, rounded to its type.  Squares are
+ * added in float64: no finite values make the norm overflow before it is rounded to float32, or vanish.  A norm that is NaN makes
+ * every value NaN; with an infinite one finite values become 0 and infinite ones NaN.  max_norm > 0; INFINITY: no limit (what is not
+ * finite stays as it is).  grad and out, of dtype, may be the same memory, which is then not written where the factor is 1; out NULL in all
+ * tensors: only the norm is wanted.  The list is HOST memory, borrowed for the call.
+ */
+typedef struct head_clip_tensor {
+    const void *grad;
+    void *out;
+    int64_t n;
+    int32_t dtype;
+} head_clip_tensor;
+
+/* Bytes of workspace (16-byte aligned) head_clip needs; negative HEAD_E* on error.  Of the tensors only n counts. */
+int64_t head_clip_bytes(const head_clip_tensor *tensors, int32_t n_tensors);
+
+int head_clip(const head_clip_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, void *workspace, void *stream);
 
 const char *head_strerror(int code);
 

@@ -10,12 +10,14 @@ from .binding import (Forest, ForestError, forest_load, forest_pack, lib_path, l
                       OUT_SCORES, OUT_LABELS, OUT_BOTH)
 
 from .linear_binding import Linear, LinearError, linear_load
-from .head_binding import (HeadError, head_adamw, head_adamw_state, head_adamw_values, head_cross_entropy,
-                           head_cross_entropy_grad, head_embed, head_embed_grad, head_layer_norm, head_layer_norm_grad)
+from .head_binding import (HeadError, head_adamw, head_adamw_state, head_adamw_values, head_clip, head_cross_entropy,
+                           head_cross_entropy_grad, head_embed, head_embed_grad, head_gated, head_gated_grad, head_layer_norm,
+                           head_layer_norm_grad, head_linear, head_linear_grad)
 from .leaf_head import LeafHead
 
 __all__ = ["Linear", "LinearError", "linear_load", "Forest", "ForestError", "forest_load", "forest_pack", "lib_path", "load_library",
            "AGG_SUM", "AGG_MEAN", "TRANSFORM_NONE", "TRANSFORM_SIGMOID", "TRANSFORM_SOFTMAX",
            "OUT_SCORES", "OUT_LABELS", "OUT_BOTH",
            "HeadError", "head_adamw", "head_adamw_state", "head_adamw_values", "head_cross_entropy", "head_cross_entropy_grad",
-           "head_embed", "head_embed_grad", "head_layer_norm", "head_layer_norm_grad", "LeafHead"]
+           "head_embed", "head_embed_grad", "head_layer_norm", "head_layer_norm_grad", "head_linear", "head_linear_grad",
+           "head_gated", "head_gated_grad", "head_clip", "LeafHead"]

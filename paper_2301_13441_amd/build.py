@@ -16,7 +16,8 @@ SOURCES = ["forest_pack.cpp", "forest_api_host.cpp", "forest_api.cpp", "forest_k
            "forest_kernels_rank.hip", "forest_kernels_ranklds.hip", "forest_kernels_rankbank.hip", "forest_kernels_split.hip",
            "forest_kernels_walk.hip", "forest_kernels_deep.hip", "forest_probe.hip",
            "linear_api.cpp", "linear_kernels.hip",
-           "head_api.cpp", "head_embed.hip", "head_norm.hip", "head_loss.hip", "head_adamw.hip"]
+           "head_api.cpp", "head_embed.hip", "head_norm.hip", "head_loss.hip", "head_linear.hip", "head_few.hip",
+           "head_adamw.hip", "head_clip.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

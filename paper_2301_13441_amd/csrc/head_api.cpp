@@ -69,6 +69,46 @@ int check_class_pointers(const head_classes &c)
     return HEAD_OK;
 }
 
+// A layer whose z has `halves` times n_outputs columns.
+int check_layer(const head_layer *l, int halves)
+{
+    if (!l || l->n_outputs < 1 || l->activation < HEAD_IDENTITY || l->activation > HEAD_SILU) return HEAD_EINVAL;
+    if (int rc = check_shape(l->dtype, l->n_rows, l->dim)) return rc;
+    if (l->n_outputs > HEAD_MAX_VECTORS / halves || (l->n_rows > 0 && l->n_outputs > HEAD_MAX_LOGITS / halves / l->n_rows)) return HEAD_ELIMIT;
+    return HEAD_OK;
+}
+
+int check_layer_pointers(const head_layer &l)
+{
+    const int e = value_bytes(l.dtype);
+    if (bad(l.weight, e) || bad_stride(l.weight_stride, l.dim) || misaligned(l.bias, 4)) return HEAD_EINVAL;
+    if (l.n_rows > 0 && (bad(l.x, e) || bad_stride(l.x_stride, l.dim))) return HEAD_EINVAL;
+    return HEAD_OK;
+}
+
+int check_layer_grad(const head_layer &l, int halves, bool has_z, int64_t bytes, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride,
+                     const void *grad_x, const void *grad_weight, const float *grad_bias, const void *workspace)
+{
+    if (int rc = check_layer_pointers(l)) return rc;
+    const int e = value_bytes(l.dtype);
+    if (bad(grad_weight, e) || misaligned(grad_bias, 4) || (bytes > 0 && bad(workspace, 16))) return HEAD_EINVAL;
+    if (l.n_rows == 0) return HEAD_OK;
+    if (bad(grad, e) || bad_stride(grad_stride, l.n_outputs) || bad(grad_x, e)) return HEAD_EINVAL;
+    if (has_z && (bad(z, e) || bad_stride(z_stride, halves * l.n_outputs))) return HEAD_EINVAL;
+    return HEAD_OK;
+}
+
+int check_clip(const head_clip_tensor *tensors, int32_t n_tensors)
+{
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return HEAD_EINVAL;
+    if (n_tensors > HEAD_MAX_TENSORS) return HEAD_ELIMIT;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        if (tensors[i].n < 0) return HEAD_EINVAL;
+        if (tensors[i].n > (int64_t{1} << 40)) return HEAD_ELIMIT;
+    }
+    return HEAD_OK;
+}
+
 int check_tensors(const head_adamw_tensor *tensors, int32_t n_tensors)
 {
     if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return HEAD_EINVAL;
@@ -185,6 +225,75 @@ int head_cross_entropy_grad(const head_classes *c, const float *lse, const float
                                           static_cast<hipStream_t>(stream)));
 }
 
+int64_t head_linear_bytes(const head_layer *l)
+{
+    if (int rc = check_layer(l, 1)) return rc;
+    return linear_bytes(*l);
+}
+
+int head_linear(const head_layer *l, const void *residual, int64_t residual_stride, float scale, void *y, void *z, void *workspace,
+                void *stream)
+{
+    const int64_t bytes = head_linear_bytes(l);
+    if (bytes < 0) return static_cast<int>(bytes);
+    if (int rc = check_layer_pointers(*l)) return rc;
+    if (l->n_rows == 0) return HEAD_OK;
+    const int e = value_bytes(l->dtype);
+    if (bad(y, e) || misaligned(z, e) || (bytes > 0 && bad(workspace, 16))) return HEAD_EINVAL;
+    if (residual && (misaligned(residual, e) || bad_stride(residual_stride, l->n_outputs))) return HEAD_EINVAL;
+    return done(launch_linear(*l, residual, residual_stride, scale, y, z, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int64_t head_linear_grad_bytes(const head_layer *l)
+{
+    if (int rc = check_layer(l, 1)) return rc;
+    return linear_grad_bytes(*l);
+}
+
+int head_linear_grad(const head_layer *l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, float scale,
+                     void *grad_x, void *grad_weight, float *grad_bias, void *workspace, void *stream)
+{
+    const int64_t bytes = head_linear_grad_bytes(l);
+    if (bytes < 0) return static_cast<int>(bytes);
+    if (int rc = check_layer_grad(*l, 1, l->activation != HEAD_IDENTITY, bytes, z, z_stride, grad, grad_stride, grad_x, grad_weight, grad_bias,
+                                  workspace))
+        return rc;
+    return done(launch_linear_grad(*l, z, z_stride, grad, grad_stride, scale, grad_x, grad_weight, grad_bias, workspace,
+                                   static_cast<hipStream_t>(stream)));
+}
+
+int64_t head_gated_bytes(const head_layer *l)
+{
+    if (int rc = check_layer(l, 2)) return rc;
+    return gated_bytes(*l);
+}
+
+int head_gated(const head_layer *l, void *y, void *z, void *workspace, void *stream)
+{
+    const int64_t bytes = head_gated_bytes(l);
+    if (bytes < 0) return static_cast<int>(bytes);
+    if (int rc = check_layer_pointers(*l)) return rc;
+    if (l->n_rows == 0) return HEAD_OK;
+    const int e = value_bytes(l->dtype);
+    if (bad(y, e) || misaligned(z, e) || (bytes > 0 && bad(workspace, 16))) return HEAD_EINVAL;
+    return done(launch_gated(*l, y, z, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int64_t head_gated_grad_bytes(const head_layer *l)
+{
+    if (int rc = check_layer(l, 2)) return rc;
+    return gated_grad_bytes(*l);
+}
+
+int head_gated_grad(const head_layer *l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, void *grad_x,
+                    void *grad_weight, float *grad_bias, void *workspace, void *stream)
+{
+    const int64_t bytes = head_gated_grad_bytes(l);
+    if (bytes < 0) return static_cast<int>(bytes);
+    if (int rc = check_layer_grad(*l, 2, true, bytes, z, z_stride, grad, grad_stride, grad_x, grad_weight, grad_bias, workspace)) return rc;
+    return done(launch_gated_grad(*l, z, z_stride, grad, grad_stride, grad_x, grad_weight, grad_bias, workspace, static_cast<hipStream_t>(stream)));
+}
+
 int head_adamw(const head_adamw_rule *rule, const head_adamw_tensor *tensors, int32_t n_tensors, void *stream)
 {
     if (!rule || !is_dtype(rule->grad_dtype) || (rule->bits != 32 && rule->bits != 8) || rule->step < 1) return HEAD_EINVAL;
@@ -211,6 +320,31 @@ int head_adamw_values(const head_adamw_tensor *tensors, void *const *out_m, void
         if (!t.m || !t.v || !t.m_scale || !t.v_scale || bad(out_m[i], 2) || bad(out_v[i], 2)) return HEAD_EINVAL;
     }
     return done(launch_adamw_values(tensors, out_m, out_v, n_tensors, static_cast<hipStream_t>(stream)));
+}
+
+int64_t head_clip_bytes(const head_clip_tensor *tensors, int32_t n_tensors)
+{
+    if (int rc = check_clip(tensors, n_tensors)) return rc;
+    return clip_bytes(tensors, n_tensors);
+}
+
+int head_clip(const head_clip_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, void *workspace, void *stream)
+{
+    const int64_t bytes = head_clip_bytes(tensors, n_tensors);
+    if (bytes < 0) return static_cast<int>(bytes);
+    if (!(max_norm > 0) || bad(norm, 4) || (bytes > 0 && bad(workspace, 16))) return HEAD_EINVAL;
+    int32_t outs = 0, some = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        const head_clip_tensor &t = tensors[i];
+        if (!is_dtype(t.dtype)) return HEAD_EINVAL;
+        if (t.n == 0) continue;
+        const int e = value_bytes(t.dtype);
+        if (bad(t.grad, e) || misaligned(t.out, e)) return HEAD_EINVAL;
+        ++some;
+        outs += t.out != nullptr;
+    }
+    if (outs != 0 && outs != some) return HEAD_EINVAL;
+    return done(launch_clip(tensors, n_tensors, max_norm, norm, workspace, static_cast<hipStream_t>(stream)));
 }
 
 const char *head_strerror(int code)

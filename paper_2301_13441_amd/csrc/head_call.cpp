@@ -18,7 +18,9 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
+#include <utility>
 #include <vector>
 
 #include "../../include/head.h"
@@ -39,6 +41,16 @@ struct Entries {
     decltype(&head_cross_entropy_grad) cross_entropy_grad;
     decltype(&head_adamw) adamw;
     decltype(&head_adamw_values) adamw_values;
+    decltype(&head_linear_bytes) linear_bytes;
+    decltype(&head_linear) linear;
+    decltype(&head_linear_grad_bytes) linear_grad_bytes;
+    decltype(&head_linear_grad) linear_grad;
+    decltype(&head_gated_bytes) gated_bytes;
+    decltype(&head_gated) gated;
+    decltype(&head_gated_grad_bytes) gated_grad_bytes;
+    decltype(&head_gated_grad) gated_grad;
+    decltype(&head_clip_bytes) clip_bytes;
+    decltype(&head_clip) clip;
 } entry;
 constexpr Py_ssize_t ENTRIES = sizeof(entry) / sizeof(void *);
 
@@ -274,6 +286,132 @@ PyObject *cross_entropy_grad(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// A layer's x, weight and bias (or None), and the layer they make; `halves`: of z's columns.
+bool layer_of(PyObject *x_object, PyObject *weight_object, PyObject *bias_object, PyObject *activation, int halves, const at::Tensor *&x,
+              const at::Tensor *&weight, head_layer &l)
+{
+    x = tensor(x_object);
+    weight = tensor(weight_object);
+    const at::Tensor *bias = bias_object == Py_None ? nullptr : tensor(bias_object);
+    if (!x || !weight || modes() || x->dim() != 2 || weight->dim() != 2 || dtype_of(*x) < 0 || !of_current_device(*x)) return false;
+    const int64_t rows = x->size(0), dim = x->size(1), columns = weight->size(0);
+    const long act = PyLong_AsLong(activation);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    if (!fits(weight, *x, x->scalar_type(), {columns, dim}) || columns % halves || act < HEAD_IDENTITY || act > HEAD_SILU ||
+        (bias_object != Py_None && !fits(bias, *x, at::kFloat, {columns})))
+        return false;
+    l = head_layer{dtype_of(*x), static_cast<int32_t>(act), rows, dim, columns / halves, x->data_ptr(), dim, weight->data_ptr(), dim,
+                   bias ? static_cast<const float *>(bias->data_ptr()) : nullptr};
+    return true;
+}
+
+void *data_of(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// y, or y and z.
+PyObject *results(int rc, const at::Tensor &y, const at::Tensor &z)
+{
+    if (rc) return PyLong_FromLong(rc);
+    return z.defined() ? tuple_of(y, z) : THPVariable_Wrap(y);
+}
+
+// linear(x, weight, bias, activation, residual, scale, keep)
+PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *x, *weight;
+    head_layer l;
+    if (n != 7 || !layer_of(args[0], args[1], args[2], args[3], 1, x, weight, l)) return declined();
+    const at::Tensor *residual = args[4] == Py_None ? nullptr : tensor(args[4]);
+    if (args[4] != Py_None && !fits(residual, *x, x->scalar_type(), {l.n_rows, l.n_outputs})) return declined();
+    const double scale = PyFloat_AsDouble(args[5]);
+    if (PyErr_Occurred()) return nullptr;
+    const int keep = PyObject_IsTrue(args[6]);
+    if (keep < 0) return nullptr;
+    const int64_t bytes = entry.linear_bytes(&l);
+    if (bytes < 0) return PyLong_FromLongLong(bytes);
+    const at::Tensor y = at::empty({l.n_rows, l.n_outputs}, x->options()), z = keep ? at::empty({l.n_rows, l.n_outputs}, x->options()) : at::Tensor(),
+                     work = bytes ? workspace(bytes, *x) : at::Tensor();
+    const void *from = residual ? residual->data_ptr() : nullptr;
+    void *to = y.data_ptr(), *to_z = data_of(z), *space = data_of(work), *stream = stream_of(*x);
+    const int rc =
+        without_gil([&] { return entry.linear(&l, from, l.n_outputs, static_cast<float>(scale), to, to_z, space, stream); });
+    return results(rc, y, z);
+    END_HANDLE_TH_ERRORS
+}
+
+// gated(x, weight, bias, activation, keep)
+PyObject *gated(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *x, *weight;
+    head_layer l;
+    if (n != 5 || !layer_of(args[0], args[1], args[2], args[3], 2, x, weight, l)) return declined();
+    const int keep = PyObject_IsTrue(args[4]);
+    if (keep < 0) return nullptr;
+    const int64_t bytes = entry.gated_bytes(&l);
+    if (bytes < 0) return PyLong_FromLongLong(bytes);
+    const at::Tensor y = at::empty({l.n_rows, l.n_outputs}, x->options()),
+                     z = keep ? at::empty({l.n_rows, 2 * l.n_outputs}, x->options()) : at::Tensor(), work = bytes ? workspace(bytes, *x) : at::Tensor();
+    void *to = y.data_ptr(), *to_z = data_of(z), *space = data_of(work), *stream = stream_of(*x);
+    const int rc = without_gil([&] { return entry.gated(&l, to, to_z, space, stream); });
+    return results(rc, y, z);
+    END_HANDLE_TH_ERRORS
+}
+
+// grad, z or None, and the results of a layer's gradient; launch(z, grad, to x, to weight, to bias or null, workspace, stream).
+template <class Launch>
+PyObject *layer_grad(PyObject *grad_object, PyObject *z_object, PyObject *bias_object, const at::Tensor &x, const at::Tensor &weight, const head_layer &l,
+                     bool reads_z, int64_t bytes, Launch launch)
+{
+    const at::Tensor *grad = tensor(grad_object), *z = z_object == Py_None ? nullptr : tensor(z_object);
+    const int bias = PyObject_IsTrue(bias_object);
+    if (bias < 0) return nullptr;
+    if (!fits(grad, x, x.scalar_type(), {l.n_rows, l.n_outputs})) return declined();
+    if (z_object != Py_None ? !fits(z, x, x.scalar_type(), {l.n_rows, weight.size(0)}) : reads_z) return declined();
+    if (bytes < 0) return PyLong_FromLongLong(bytes);
+    const at::Tensor gx = at::empty({l.n_rows, l.dim}, x.options()), gw = at::empty({weight.size(0), l.dim}, x.options()),
+                     gb = bias ? at::empty({weight.size(0)}, x.options().dtype(at::kFloat)) : at::Tensor(),
+                     work = bytes ? workspace(bytes, x) : at::Tensor();
+    const void *from_z = z ? z->data_ptr() : nullptr, *from = grad->data_ptr();
+    void *to_x = gx.data_ptr(), *to_weight = gw.data_ptr(), *space = data_of(work), *stream = stream_of(x);
+    float *to_bias = static_cast<float *>(data_of(gb));
+    const int rc = without_gil([&] { return launch(from_z, from, to_x, to_weight, to_bias, space, stream); });
+    return rc ? PyLong_FromLong(rc) : tuple_of(gx, gw, gb);
+}
+
+// linear_grad(grad, x, weight, z, activation, scale, bias)
+PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *x, *weight;
+    head_layer l;
+    if (n != 7 || !layer_of(args[1], args[2], Py_None, args[4], 1, x, weight, l)) return declined();
+    const double scale = PyFloat_AsDouble(args[5]);
+    if (PyErr_Occurred()) return nullptr;
+    return layer_grad(args[0], args[3], args[6], *x, *weight, l, l.activation != HEAD_IDENTITY, entry.linear_grad_bytes(&l),
+                      [&](const void *z, const void *grad, void *to_x, void *to_weight, float *to_bias, void *space, void *stream) {
+                          return entry.linear_grad(&l, z, l.n_outputs, grad, l.n_outputs, static_cast<float>(scale), to_x, to_weight, to_bias, space, stream);
+                      });
+    END_HANDLE_TH_ERRORS
+}
+
+// gated_grad(grad, x, weight, z, activation, bias)
+PyObject *gated_grad(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *x, *weight;
+    head_layer l;
+    if (n != 6 || !layer_of(args[1], args[2], Py_None, args[4], 2, x, weight, l)) return declined();
+    return layer_grad(args[0], args[3], args[5], *x, *weight, l, true, entry.gated_grad_bytes(&l),
+                      [&](const void *z, const void *grad, void *to_x, void *to_weight, float *to_bias, void *space, void *stream) {
+                          return entry.gated_grad(&l, z, 2 * l.n_outputs, grad, l.n_outputs, to_x, to_weight, to_bias, space, stream);
+                      });
+    END_HANDLE_TH_ERRORS
+}
+
 // Address of n adjacent values; null: not those.
 void *values_at(PyObject *o, const at::Tensor &like, at::ScalarType type, int64_t n)
 {
@@ -398,6 +536,68 @@ PyObject *adamw_values(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// clip(grads, max_norm, in_place): a list.  Returns (norm, a new list).
+PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    if (n_args != 3 || !PyList_CheckExact(args[0]) || modes()) return declined();
+    const Py_ssize_t n = PyList_GET_SIZE(args[0]);
+    if (n == 0 || n > HEAD_MAX_TENSORS) return declined();
+    const double max_norm = PyFloat_AsDouble(args[1]);
+    if (PyErr_Occurred()) return nullptr;
+    const int in_place = PyObject_IsTrue(args[2]);
+    if (in_place < 0) return nullptr;
+    if (!(max_norm > 0)) return declined();
+    const at::Tensor *first = tensor(PyList_GET_ITEM(args[0], 0));
+    if (!first || !of_current_device(*first)) return declined();
+    std::vector<head_clip_tensor> tensors(n);
+    std::vector<at::Tensor> out(n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor *t = tensor(PyList_GET_ITEM(args[0], i));
+        if (!t || dtype_of(*t) < 0 || t->device() != first->device() || t->numel() == 0) return declined();
+        tensors[i] = head_clip_tensor{t->data_ptr(), nullptr, t->numel(), dtype_of(*t)};
+    }
+    if (in_place) {  // the same memory twice is the general way's error
+        std::vector<std::pair<uintptr_t, uintptr_t>> ends(n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            const at::Tensor &t = THPVariable_Unpack(PyList_GET_ITEM(args[0], i));
+            const uintptr_t at = reinterpret_cast<uintptr_t>(tensors[i].grad);
+            ends[i] = {at, at + t.nbytes()};
+        }
+        std::sort(ends.begin(), ends.end());
+        for (Py_ssize_t i = 1; i < n; ++i)
+            if (ends[i - 1].second > ends[i].first) return declined();
+    }
+    const int64_t bytes = entry.clip_bytes(tensors.data(), static_cast<int32_t>(n));
+    if (bytes < 0) return PyLong_FromLongLong(bytes);
+    const at::Tensor norm = at::empty({}, first->options().dtype(at::kFloat)), work = workspace(bytes, *first);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor &t = THPVariable_Unpack(PyList_GET_ITEM(args[0], i));
+        if (in_place) written(PyList_GET_ITEM(args[0], i));
+        out[i] = in_place ? t : at::empty(t.sizes(), t.options());
+        tensors[i].out = out[i].data_ptr();
+    }
+    float *to = static_cast<float *>(norm.data_ptr());
+    void *space = work.data_ptr(), *stream = stream_of(*first);
+    const int rc = without_gil([&] { return entry.clip(tensors.data(), static_cast<int32_t>(n), max_norm, to, space, stream); });
+    if (rc) return PyLong_FromLong(rc);
+    PyObject *list = PyList_New(n);
+    for (Py_ssize_t i = 0; list && i < n; ++i) {
+        PyObject *one = in_place ? Py_NewRef(PyList_GET_ITEM(args[0], i)) : THPVariable_Wrap(out[i]);
+        if (!one) {
+            Py_DECREF(list);
+            return nullptr;
+        }
+        PyList_SET_ITEM(list, i, one);
+    }
+    PyObject *first_of_pair = list ? THPVariable_Wrap(norm) : nullptr;
+    PyObject *pair = first_of_pair ? PyTuple_Pack(2, first_of_pair, list) : nullptr;
+    Py_XDECREF(first_of_pair);
+    Py_XDECREF(list);
+    return pair;
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses of the entry points, in Entries' order)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -422,6 +622,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 PyMethodDef METHODS[] = {HEAD_METHOD(bind),          HEAD_METHOD(embed),         HEAD_METHOD(embed_grad),
                          HEAD_METHOD(layer_norm),    HEAD_METHOD(layer_norm_grad), HEAD_METHOD(cross_entropy),
                          HEAD_METHOD(cross_entropy_grad), HEAD_METHOD(adamw),    HEAD_METHOD(adamw_values),
+                         HEAD_METHOD(linear),        HEAD_METHOD(linear_grad),   HEAD_METHOD(gated),
+                         HEAD_METHOD(gated_grad),    HEAD_METHOD(clip),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef MODULE = {PyModuleDef_HEAD_INIT, "_head_call", nullptr, -1, METHODS, nullptr, nullptr, nullptr, nullptr};
 

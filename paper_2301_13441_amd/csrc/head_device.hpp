@@ -95,6 +95,21 @@ int64_t cross_entropy_grad_bytes(const head_classes &c);
 hipError_t launch_cross_entropy_grad(const head_classes &c, const float *lse, const float *grad_loss, void *grad_hidden,
                                      void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream);
 
+int64_t linear_bytes(const head_layer &l);
+int64_t linear_grad_bytes(const head_layer &l);
+int64_t gated_bytes(const head_layer &l);
+int64_t gated_grad_bytes(const head_layer &l);
+hipError_t launch_linear(const head_layer &l, const void *residual, int64_t residual_stride, float scale, void *y, void *z, void *workspace,
+                         hipStream_t stream);
+hipError_t launch_linear_grad(const head_layer &l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, float scale,
+                              void *grad_x, void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream);
+hipError_t launch_gated(const head_layer &l, void *y, void *z, void *workspace, hipStream_t stream);
+hipError_t launch_gated_grad(const head_layer &l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, void *grad_x,
+                             void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream);
+
+int64_t clip_bytes(const head_clip_tensor *tensors, int32_t n_tensors);
+hipError_t launch_clip(const head_clip_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, void *workspace, hipStream_t stream);
+
 hipError_t launch_adamw(const head_adamw_rule &rule, const head_adamw_tensor *tensors, int32_t n_tensors, hipStream_t stream);
 hipError_t launch_adamw_values(const head_adamw_tensor *tensors, void *const *out_m, void *const *out_v, int32_t n_tensors,
                                hipStream_t stream);

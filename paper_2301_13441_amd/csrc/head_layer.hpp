@@ -1,0 +1,86 @@
+// What the kernels of dense layers share (formulas: head.h): activations, their slopes, and what a layer's results go through.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "head_device.hpp"
+
+namespace head_impl {
+
+// f(the activation as a constant), so that loops are not full of choices.
+template <class F>
+__device__ __forceinline__ void with_activation(int32_t activation, F f)
+{
+    switch (activation) {
+        case HEAD_RELU: return f(std::integral_constant<int, HEAD_RELU>());
+        case HEAD_GELU: return f(std::integral_constant<int, HEAD_GELU>());
+        case HEAD_SILU: return f(std::integral_constant<int, HEAD_SILU>());
+        default: return f(std::integral_constant<int, HEAD_IDENTITY>());
+    }
+}
+
+// Value and slope of an activation at x, for results of type T.
+template <class T, int ACTIVATION>
+struct Activation {
+    float value, slope;
+
+    __device__ __forceinline__ explicit Activation(float x)
+    {
+        if constexpr (ACTIVATION == HEAD_IDENTITY) {
+            value = x;
+            slope = 1;
+        } else if constexpr (ACTIVATION == HEAD_RELU) {
+            value = x <= 0 ? 0 : x;  // NaN stays
+            slope = x > 0 ? 1 : 0;
+        } else if constexpr (ACTIVATION == HEAD_SILU) {
+            // value = x s, slope = s + x s (1 - s) with s = 1 / (1 + exp(-x))
+            float s;
+            if constexpr (sizeof(T) == 4) s = 1 / (1 + expf(-x));
+            else s = __builtin_amdgcn_rcpf(1 + __builtin_amdgcn_exp2f(x * -1.44269504088896341f));
+            value = x * s;
+            slope = s + value * (1 - s);
+        } else {
+            // value = x P, slope = P + x exp(-x^2 / 2) / sqrt(2 pi) with P(x) = erfc(-x / sqrt 2) / 2
+            float p, e;
+            if constexpr (sizeof(T) == 4) {
+                p = 0.5f * erfcf(x * -0.707106781186547524f);
+                e = expf(-0.5f * x * x);
+            } else {
+                // P(-a) = exp(-a^2 / 2) Q(1 / (1 + 0.375 a)) for a >= 0: a polynomial fitted (least squares of the relative difference, weighted
+                // until its extremes were even) to erfcx(a / sqrt 2) / 2 on [0, 14], 2^-14.9 off at most
+                const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.375f, 1.0f));
+                e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);
+                const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, -0.09064799f, 0.20029321f), 0.08355508f), 0.15773682f), 0.14906072f) * e;
+                p = x > 0 ? 1 - q : q;
+            }
+            value = x * p;
+            slope = fmaf(x * e, 0.398942280401432678f, p);
+        }
+    }
+};
+
+// Where a layer's results go.  Null: not there, not wanted.
+template <class T>
+struct End {
+    int32_t activation;
+    const float *bias;
+    const T *residual;
+    int64_t residual_stride;
+    float scale;
+    T *y, *z;
+    int64_t n_rows, outs;  // columns of y
+    bool wide;             // rows of residual, y and z are whole in pairs of values
+};
+
+// Layers of few rows, forward, have a kernel of their own (head_few.hip), without a workspace.
+constexpr int64_t FEW_ROWS = 64;
+inline bool is_few(const head_layer &l) { return l.n_rows <= FEW_ROWS; }
+
+template <class T, bool GATED>
+hipError_t launch_few(const head_layer &l, const End<T> &end, hipStream_t stream);
+
+}  // namespace head_impl

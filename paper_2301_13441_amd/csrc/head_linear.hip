@@ -1,0 +1,561 @@
+// Dense layers of the trainable head and their gradients, on gfx950 (formulas: head.h).
+//
+//     linear   z = x weight^T + bias,                            y = residual + scale act(z)
+//     gated    (gates | values) = z = x weight^T + bias,         y = act(gates) values
+//     gradients, with dz that of z:  grad_x = dz weight,  grad_weight = dz^T x,  grad_bias = sum over rows of dz
+//
+// Forward is one product whose tiles end in the activation: z goes to memory only where it is wanted.  A gated layer's tile has the same
+// columns of gates and of values, in the same lanes.  Backward dz is made in one pass over z and grad, with the sums of its
+// columns, and read by two products.  Products of few tiles are cut along the sum's axis; parts are added in a fixed order.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "head_layer.hpp"
+#include "head_product.hpp"
+
+namespace head_impl {
+namespace {
+
+// ---- forward
+
+// A lane's results of a tile, C = z before the bias, through activation and residual.
+template <class T, class S, bool GATED>
+__device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float (&bias)[S::NT], const End<T> &e, int64_t row0, int64_t column0)
+{
+    constexpr int N = GATED ? S::NT / 2 : S::NT;  // adjacent columns of y that a lane has
+    const int64_t first = row0 + S::row(0, 0), left = e.n_rows - first;
+    const int rows = static_cast<int>(std::min<int64_t>(S::M, left));
+    // of a wavefront's columns, a lane's first one of y
+    const int64_t column = GATED ? column0 / 2 + S::wave_n() * (S::NT * 16) + threadIdx.x % 32 * N : column0 + S::column(0);
+    T *y = e.y + first * e.outs + column;
+    T *z = e.z ? e.z + first * (GATED ? 2 : 1) * e.outs + column : nullptr;
+    const T *residual = !GATED && e.residual ? e.residual + first * e.residual_stride + column : nullptr;
+    const int columns = static_cast<int>(std::min<int64_t>(N, e.outs - column));
+    if (columns <= 0) return;
+    auto put = [&](T *to, const float (&v)[N]) {
+        Pack<T, N> p;
+#pragma unroll
+        for (int k = 0; k < N; ++k) p.v[k] = narrow<T>(v[k]);
+        if (e.wide) {
+            *reinterpret_cast<Pack<T, N> *>(to) = p;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (k < columns) to[k] = p.v[k];
+        }
+    };
+    with_activation(e.activation, [&](auto ACTIVATION) {
+        using Act = Activation<T, ACTIVATION()>;
+#pragma unroll
+        for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int down = mt * 32 + i / 4 * 8 + i % 4;
+                if (down >= rows) continue;
+                float v[N];
+                if constexpr (GATED) {
+                    float gate[N], value[N];
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        gate[k] = c[mt][2 * k][i] + bias[2 * k];
+                        value[k] = c[mt][2 * k + 1][i] + bias[2 * k + 1];
+                        v[k] = Act(gate[k]).value * value[k];
+                    }
+                    if (z) {
+                        put(z + down * 2 * e.outs, gate);
+                        put(z + down * 2 * e.outs + e.outs, value);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[k] = c[mt][k][i] + bias[k];
+                    if (z) put(z + down * e.outs, v);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[k] = e.scale * Act(v[k]).value;
+                    if (residual) {
+                        const T *from = residual + down * e.residual_stride;
+                        if (e.wide) {
+                            const Pack<T, N> r = *reinterpret_cast<const Pack<T, N> *>(from);
+#pragma unroll
+                            for (int k = 0; k < N; ++k) v[k] += widen(r.v[k]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < N; ++k) v[k] += k < columns ? widen(from[k]) : 0.0f;
+                        }
+                    }
+                }
+                put(y + down * e.outs, v);
+            }
+    });
+}
+
+template <class T, class S, bool GATED>
+__global__ __launch_bounds__(S::THREADS, 2) void layer_kernel(Operand<T> x, Operand<T> weight, End<T> e, uint32_t row_tiles, uint32_t column_tiles)
+{
+    extern __shared__ char lds[];
+    Products<T, S, true, true, GATED> products(x, weight, lds);
+    const uint32_t tiles = row_tiles * column_tiles;
+    uint32_t column_tile = 0, row_tile = 0;
+    auto aim = [&](uint32_t tile) {
+        if (tile >= tiles) return;
+        tile_of(tile, row_tiles, column_tiles, row_tile, column_tile);
+        products.aim(int64_t{S::M} * row_tile, int64_t{S::N} * column_tile, 0, x.depth, row_tile + column_tile);
+    };
+    aim(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * row_tile;
+        float bias[S::NT] = {};
+        if (e.bias) {
+#pragma unroll
+            for (int nt = 0; nt < S::NT; ++nt) {
+                int64_t k = column0 + S::column(nt);
+                bool there = k < e.outs;
+                if constexpr (GATED) {
+                    k = column0 / 2 + S::wave_n() * (S::NT * 16) + threadIdx.x % 32 * (S::NT / 2) + nt / 2;
+                    there = k < e.outs;
+                    k += nt % 2 * e.outs;
+                }
+                bias[nt] = there ? e.bias[k] : 0.0f;
+            }
+        }
+        Acc c[S::MT][S::NT];
+        products.clear(c);
+        products.run(c, [&] { aim(tile + gridDim.x); });
+        finish<T, S, GATED>(c, bias, e, row0, column0);
+    }
+}
+
+// The end of a layer whose product came in parts, [splits][n_rows][columns of z] float32: a lane for each value of y.
+template <class T, bool GATED>
+__global__ __launch_bounds__(256) void finish_kernel(const float *parts, int64_t splits, End<T> e)
+{
+    const int64_t columns = GATED ? 2 * e.outs : e.outs, n = e.n_rows * e.outs, all = e.n_rows * columns;
+    for (int64_t i = int64_t{256} * blockIdx.x + threadIdx.x; i < n; i += int64_t{256} * gridDim.x) {
+        const int64_t r = i / e.outs, k = i % e.outs, at = r * columns + k;
+        float a = 0, b = 0;
+#pragma unroll 4
+        for (int64_t s = 0; s < splits; ++s) {
+            a += parts[s * all + at];
+            if constexpr (GATED) b += parts[s * all + at + e.outs];
+        }
+        if (e.bias) {
+            a += e.bias[k];
+            if constexpr (GATED) b += e.bias[e.outs + k];
+        }
+        if (e.z) {
+            e.z[at] = narrow<T>(a);
+            if constexpr (GATED) e.z[at + e.outs] = narrow<T>(b);
+        }
+        with_activation(e.activation, [&](auto ACTIVATION) {
+            const float v = Activation<T, ACTIVATION()>(a).value;
+            if constexpr (GATED) e.y[i] = narrow<T>(v * b);
+            else e.y[i] = narrow<T>(e.scale * v + (e.residual ? widen(e.residual[r * e.residual_stride + k]) : 0.0f));
+        });
+    }
+}
+
+// ---- backward
+
+// dz of `rows` rows from row `rows` * blockIdx.y on, `stride` apart, and parts [gridDim.y][columns] of the sums of its columns, either if
+// wanted; zeros behind its columns up to `padded`.  `scale` is only that of the sums.
+template <class T>
+struct Slopes {
+    int32_t activation;
+    const T *z, *grad;
+    int64_t z_stride, grad_stride;
+    int64_t n_rows, outs, rows;
+    T *dz;
+    int64_t stride, padded;
+    float scale;
+    float *parts;
+};
+
+// LANES lanes side by side, of N columns each, 256 / LANES rows at a time.
+template <class T, bool GATED, int N, int LANES>
+__global__ __launch_bounds__(256) void slope_kernel(Slopes<T> s)
+{
+    constexpr int HIGH = 256 / LANES, H = GATED ? 2 : 1;
+    __shared__ float lds[HIGH][H][LANES * N];
+    const int x = threadIdx.x % LANES, y = threadIdx.x / LANES;
+    const int64_t column = (int64_t{LANES} * blockIdx.x + x) * N, columns = H * s.outs;
+    const int64_t row0 = s.rows * blockIdx.y, end = std::min(row0 + s.rows, s.n_rows);
+    float sums[H][N] = {};
+    if (column < s.outs) {
+        with_activation(s.activation, [&](auto ACTIVATION) {
+            constexpr bool READS = GATED || ACTIVATION() != HEAD_IDENTITY;
+#pragma unroll 2
+            for (int64_t row = row0 + y; row < end; row += HIGH) {
+                const Pack<T, N> g = *reinterpret_cast<const Pack<T, N> *>(s.grad + row * s.grad_stride + column);
+                Pack<T, N> z[H], out[H];
+                if constexpr (READS) {
+#pragma unroll
+                    for (int h = 0; h < H; ++h) z[h] = *reinterpret_cast<const Pack<T, N> *>(s.z + row * s.z_stride + h * s.outs + column);
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    float d[H];
+                    d[0] = widen(g.v[k]);
+                    if constexpr (READS) {
+                        const Activation<T, ACTIVATION()> a(widen(z[0].v[k]));
+                        if constexpr (GATED) {
+                            d[1] = d[0] * a.value;
+                            d[0] *= widen(z[1].v[k]);
+                        }
+                        if constexpr (ACTIVATION() == HEAD_RELU) d[0] = a.slope > 0 ? d[0] : 0;
+                        else d[0] *= a.slope;
+                    }
+#pragma unroll
+                    for (int h = 0; h < H; ++h) {
+                        sums[h][k] += d[h];
+                        out[h].v[k] = narrow<T>(d[h]);
+                    }
+                }
+                if (s.dz) {
+#pragma unroll
+                    for (int h = 0; h < H; ++h) *reinterpret_cast<Pack<T, N> *>(s.dz + row * s.stride + h * s.outs + column) = out[h];
+                }
+            }
+        });
+    }
+    if (N == 1 && s.dz && column < s.padded - columns)  // whole vectors have nothing behind them
+        for (int64_t row = row0 + y; row < end; row += HIGH) s.dz[row * s.stride + columns + column] = T(0);
+    if (!s.parts) return;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int k = 0; k < N; ++k) lds[y][h][x * N + k] = sums[h][k];
+    __syncthreads();
+    for (int i = threadIdx.x; i < H * LANES * N; i += 256) {
+        const int h = i / (LANES * N), k = i % (LANES * N);
+        const int64_t at = int64_t{LANES} * N * blockIdx.x + k;
+        float all = 0;
+#pragma unroll
+        for (int j = 0; j < HIGH; ++j) all += lds[j][h][k];
+        if (at < s.outs) s.parts[blockIdx.y * columns + h * s.outs + at] = s.scale * all;
+    }
+}
+
+// C = A B.  Each of `splits` parts of the sum's axis goes to a result of its own, [splits][rows][columns] float32; or (out) the one
+// part is the result.
+template <class T, class S, bool A_ALONG, bool B_ALONG>
+__global__ __launch_bounds__(S::THREADS, 2) void sum_kernel(Operand<T> a, Operand<T> b, int64_t columns, uint32_t row_tiles, uint32_t column_tiles,
+                                                            uint32_t splits, int64_t split_depth, float scale, float *parts, T *out)
+{
+    static_assert(!S::NEXT, "a lane's columns are 32 apart");
+    extern __shared__ char lds[];
+    Products<T, S, A_ALONG, B_ALONG> products(a, b, lds);
+    const uint32_t tiles = row_tiles * column_tiles * splits;
+    uint32_t column_tile = 0, row_tile = 0;
+    auto aim = [&](uint32_t tile) {
+        if (tile >= tiles) return;
+        tile_of(tile, row_tiles * splits, column_tiles, row_tile, column_tile);
+        const int64_t depth0 = row_tile / row_tiles * split_depth;
+        products.aim(int64_t{S::M} * (row_tile % row_tiles), int64_t{S::N} * column_tile, depth0, std::min(a.depth, depth0 + split_depth), 0);
+    };
+    aim(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * (row_tile % row_tiles), split = row_tile / row_tiles;
+        Acc c[S::MT][S::NT];
+        products.clear(c);
+        products.run(c, [&] { aim(tile + gridDim.x); });
+        const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
+        const int64_t at = (row0 + S::row(0, 0)) * columns + column0 + S::column(0);
+        auto each = [&](auto store) {
+#pragma unroll
+            for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int down = mt * 32 + i / 4 * 8 + i % 4;
+#pragma unroll
+                    for (int nt = 0; nt < S::NT; ++nt)
+                        if (down < rows && column0 + S::column(nt) < columns) store(down * columns + nt * 32, scale * c[mt][nt][i]);
+                }
+        };
+        if (out) {
+            T *to = out + at;
+            each([&](int64_t k, float v) { to[k] = narrow<T>(v); });
+        } else {
+            float *to = parts + split * a.rows * columns + at;
+            each([&](int64_t k, float v) { to[k] = v; });
+        }
+    }
+}
+
+// ---- what a call launches
+
+// A gated layer's tiles have two columns of z for each of y.
+template <class Size>
+struct GatedOf;
+template <>
+struct GatedOf<Tiny> { using Type = Shape<64, 128, 2, 2, false>; };
+template <>
+struct GatedOf<Small> { using Type = Shape<128, 128, 2, 2, false>; };
+template <>
+struct GatedOf<Large> { using Type = Shape<256, 256, 4, 2, false>; };
+
+enum { TINY, SMALL, LARGE };
+
+// How a product [rows][columns] over `depth` is cut.
+struct Cut {
+    int size;
+    int64_t row_tiles, column_tiles, splits, split_depth;
+    int64_t tiles() const { return row_tiles * column_tiles * splits; }
+};
+
+Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, bool gated = false)
+{
+    const int64_t step = STEP / value_bytes(dtype);
+    auto tiles = [&](int64_t tile) { return ceil_div(rows, tile) * ceil_div(columns, tile); };
+    Cut c{};
+    const int64_t most = std::max<int64_t>(1, depth / (16 * step));  // parts of a large tile's sum that are long enough
+    if (dtype == HEAD_BF16 && std::min(rows, columns) > 128 && tiles(Large::TILE) * std::min<int64_t>(most, 4) >= Large::RESIDENT) c.size = LARGE;
+    else if (std::min(rows, columns) > 64 && tiles(Small::TILE) >= Small::RESIDENT / 2) c.size = SMALL;
+    else c.size = TINY;
+    const int64_t tile = c.size == LARGE ? 256 : c.size == SMALL ? 128 : 64, resident = c.size == LARGE ? 256 : 512;
+    c.row_tiles = ceil_div(rows, tile);
+    c.column_tiles = ceil_div(columns, gated && c.size == TINY ? 128 : tile);
+    c.splits = splits_of(c.row_tiles * c.column_tiles, resident, depth, step);
+    c.split_depth = round_up(ceil_div(depth, c.splits), step);
+    c.splits = std::max<int64_t>(1, ceil_div(depth, c.split_depth));
+    return c;
+}
+
+// The parts of a call's workspace, in bytes from its start.
+struct Space {
+    int64_t bytes = 0;
+    int64_t part(int64_t n)
+    {
+        const int64_t at = bytes;
+        bytes += round_up(n, 256);
+        return at;
+    }
+};
+
+struct Plan : Space {
+    int64_t packed;                  // values of a packed row of x and weight
+    int64_t x = -1, weight = -1;     // packed operands; -1: used where they are
+    Cut forward, to_x, to_weight;
+    int64_t parts = -1, weight_parts = -1;
+    int64_t stride, padded;          // values of a row of dz, and how many are zero or its own
+    int64_t dz = -1, bias_rows, bias_chunks, bias_parts = -1;
+};
+
+bool whole(int32_t dtype, const void *at, int64_t stride, int64_t n)
+{
+    const int e = value_bytes(dtype);
+    return (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(n * e)) % 16 == 0;
+}
+
+void plan_operands(const head_layer &l, int64_t columns, Plan &p)
+{
+    const int e = value_bytes(l.dtype);
+    p.packed = round_up(l.dim, 16 / e);
+    if (!whole(l.dtype, l.x, l.x_stride, l.dim)) p.x = p.part(l.n_rows * p.packed * e);
+    if (!whole(l.dtype, l.weight, l.weight_stride, l.dim)) p.weight = p.part(columns * p.packed * e);
+}
+
+Plan plan_forward(const head_layer &l, bool gated)
+{
+    Plan p;
+    const int64_t columns = gated ? 2 * l.n_outputs : l.n_outputs;
+    if (l.n_rows == 0 || is_few(l)) return p;
+    plan_operands(l, columns, p);
+    p.forward = cut_of(l.dtype, l.n_rows, columns, l.dim, gated);
+    if (p.forward.splits > 1) p.parts = p.part(p.forward.splits * l.n_rows * columns * 4);
+    return p;
+}
+
+Plan plan_backward(const head_layer &l, bool gated)
+{
+    Plan p;
+    const int e = value_bytes(l.dtype);
+    const int64_t columns = gated ? 2 * l.n_outputs : l.n_outputs;
+    if (l.n_rows == 0) return p;
+    plan_operands(l, columns, p);
+    // Rows a power of two apart would lie in few of the memory's channels: a row more than its values by 256 bytes goes through all.
+    p.padded = round_up(columns, 16 / e);
+    p.stride = p.padded + 256 / e;
+    p.dz = p.part(l.n_rows * p.stride * e);
+    p.bias_chunks = std::min<int64_t>(ceil_div(l.n_rows, 16), std::min<int64_t>(8192, std::max<int64_t>(1, (int64_t{1} << 20) / columns)));
+    p.bias_rows = ceil_div(l.n_rows, p.bias_chunks);
+    p.bias_chunks = ceil_div(l.n_rows, p.bias_rows);
+    p.bias_parts = p.part(p.bias_chunks * columns * 4);
+    p.to_x = cut_of(l.dtype, l.n_rows, l.dim, columns);
+    p.to_weight = cut_of(l.dtype, columns, l.dim, l.n_rows);
+    if (p.to_x.splits > 1) p.parts = p.part(p.to_x.splits * l.n_rows * l.dim * 4);
+    if (p.to_weight.splits > 1) p.weight_parts = p.part(p.to_weight.splits * columns * l.dim * 4);
+    return p;
+}
+
+template <class S, auto *KERNEL, class... Args>
+hipError_t launch_tiles(int64_t tiles, int64_t resident, hipStream_t stream, Args... args)
+{
+    constexpr size_t BYTES = 2 * (S::M + S::N) * STEP;
+    if (const hipError_t e = allow_lds<KERNEL>(BYTES)) return e;
+    hipLaunchKernelGGL(KERNEL, grid_of(tiles, resident), dim3(S::THREADS), BYTES, stream, args...);
+    return hipGetLastError();
+}
+
+// f(the size as a type); float32 products have no large tiles.
+template <class T, class F>
+hipError_t with_size(int size, F f)
+{
+    if constexpr (sizeof(T) == 2)
+        if (size == LARGE) return f(Large());
+    return size == SMALL ? f(Small()) : f(Tiny());
+}
+
+// x, or weight, packed if it has to be.
+template <class T>
+Operand<T> operand(const void *at, int64_t stride, int64_t rows, int64_t dim, int64_t packed, int64_t packed_at, char *workspace, hipStream_t stream)
+{
+    const T *from = static_cast<const T *>(at);
+    if (packed_at < 0) return Operand<T>{from, stride, rows, dim};
+    T *to = reinterpret_cast<T *>(workspace + packed_at);
+    hipLaunchKernelGGL((pack_kernel<T>), grid_of(ceil_div(rows * packed, 256)), dim3(256), 0, stream, from, stride, rows, dim, to, packed);
+    return Operand<T>{to, packed, rows, packed};
+}
+
+template <class T, bool A_ALONG, bool B_ALONG>
+hipError_t launch_sum(const Cut &c, const Operand<T> &a, const Operand<T> &b, int64_t columns, float scale, float *parts, T *out, hipStream_t stream)
+{
+    return with_size<T>(c.size, [&](auto size) {
+        using Size = decltype(size);
+        using S = typename Size::template Of<false>;
+        return launch_tiles<S, sum_kernel<T, S, A_ALONG, B_ALONG>>(c.tiles(), Size::RESIDENT, stream, a, b, columns, static_cast<uint32_t>(c.row_tiles),
+                                                                   static_cast<uint32_t>(c.column_tiles), static_cast<uint32_t>(c.splits), c.split_depth,
+                                                                   scale, parts, out);
+    });
+}
+
+template <class T, bool GATED>
+hipError_t forward(const head_layer &l, const void *residual, int64_t residual_stride, float scale, void *y, void *z, char *workspace,
+                   hipStream_t stream)
+{
+    const int64_t columns = (GATED ? 2 : 1) * l.n_outputs;
+    End<T> end{l.activation, l.bias, static_cast<const T *>(residual), residual ? residual_stride : 0, scale, static_cast<T *>(y), static_cast<T *>(z),
+               l.n_rows, l.n_outputs, false};
+    if (is_few(l)) return launch_few<T, GATED>(l, end, stream);
+    const Plan p = plan_forward(l, GATED);
+    const Operand<T> x = operand<T>(l.x, l.x_stride, l.n_rows, l.dim, p.packed, p.x, workspace, stream);
+    const Operand<T> weight = operand<T>(l.weight, l.weight_stride, columns, l.dim, p.packed, p.weight, workspace, stream);
+    if (const hipError_t e = hipGetLastError()) return e;
+    const Cut &c = p.forward;
+    if (c.splits > 1) {
+        float *parts = reinterpret_cast<float *>(workspace + p.parts);
+        Cut sum = c;
+        if (GATED && c.size == TINY) sum.column_tiles = ceil_div(columns, Tiny::TILE);
+        if (const hipError_t e = launch_sum<T, true, true>(sum, x, weight, columns, 1.0f, parts, nullptr, stream)) return e;
+        hipLaunchKernelGGL((finish_kernel<T, GATED>), grid_of(ceil_div(l.n_rows * l.n_outputs, 256)), dim3(256), 0, stream, parts, c.splits, end);
+        return hipGetLastError();
+    }
+    const uint64_t bits = address(y) | address(z) | address(residual) | static_cast<uint64_t>((l.n_outputs | end.residual_stride) * sizeof(T));
+    end.wide = bits % (2 * sizeof(T)) == 0;
+    return with_size<T>(c.size, [&](auto size) {
+        using Size = decltype(size);
+        using S = std::conditional_t<GATED, typename GatedOf<Size>::Type, typename Size::template Of<true>>;
+        return launch_tiles<S, layer_kernel<T, S, GATED>>(c.tiles(), Size::RESIDENT, stream, x, weight, end, static_cast<uint32_t>(c.row_tiles),
+                                                          static_cast<uint32_t>(c.column_tiles));
+    });
+}
+
+template <class T, bool GATED>
+void launch_slopes(const Slopes<T> &s, int64_t chunks, bool wide, hipStream_t stream)
+{
+    constexpr int V = 16 / sizeof(T);
+    auto run = [&](auto n, auto lanes) {
+        hipLaunchKernelGGL((slope_kernel<T, GATED, n(), lanes()>), dim3(static_cast<uint32_t>(ceil_div(s.outs, n() * lanes())), static_cast<uint32_t>(chunks)),
+                           dim3(256), 0, stream, s);
+    };
+    using std::integral_constant;
+    const int64_t lanes = wide ? ceil_div(s.outs, V) : s.outs;
+    if (wide) {
+        if (lanes > 16) run(integral_constant<int, V>(), integral_constant<int, 64>());
+        else if (lanes > 4) run(integral_constant<int, V>(), integral_constant<int, 16>());
+        else run(integral_constant<int, V>(), integral_constant<int, 4>());
+    } else {
+        if (lanes > 16) run(integral_constant<int, 1>(), integral_constant<int, 64>());
+        else run(integral_constant<int, 1>(), integral_constant<int, 16>());
+    }
+}
+
+template <class T, bool GATED>
+hipError_t backward(const head_layer &l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, float scale, void *grad_x,
+                    void *grad_weight, float *grad_bias, char *workspace, hipStream_t stream)
+{
+    const int64_t columns = (GATED ? 2 : 1) * l.n_outputs;
+    T *to_x = static_cast<T *>(grad_x), *to_weight = static_cast<T *>(grad_weight);
+    if (l.n_rows == 0) {
+        hipLaunchKernelGGL((zero_kernel<T>), grid_of(ceil_div(columns * l.dim, 256)), dim3(256), 0, stream, to_weight, columns * l.dim);
+        if (grad_bias) hipLaunchKernelGGL((zero_kernel<float>), grid_of(ceil_div(columns, 256)), dim3(256), 0, stream, grad_bias, columns);
+        return hipGetLastError();
+    }
+    const Plan p = plan_backward(l, GATED);
+    const Operand<T> x = operand<T>(l.x, l.x_stride, l.n_rows, l.dim, p.packed, p.x, workspace, stream);
+    const Operand<T> weight = operand<T>(l.weight, l.weight_stride, columns, l.dim, p.packed, p.weight, workspace, stream);
+    // Without an activation dz is grad itself, where products can read it.
+    const bool reads = GATED || l.activation != HEAD_IDENTITY;
+    const bool makes = reads || !whole(l.dtype, grad, grad_stride, l.n_outputs);
+    const T *dz = static_cast<const T *>(grad);
+    int64_t stride = grad_stride;
+    if (makes || grad_bias) {
+        Slopes<T> s{l.activation, static_cast<const T *>(z), dz, z_stride, grad_stride, l.n_rows, l.n_outputs, p.bias_rows,
+                    makes ? reinterpret_cast<T *>(workspace + p.dz) : nullptr, p.stride, p.padded, scale,
+                    grad_bias ? reinterpret_cast<float *>(workspace + p.bias_parts) : nullptr};
+        const bool wide = whole(l.dtype, grad, grad_stride, l.n_outputs) && (!reads || whole(l.dtype, z, z_stride, l.n_outputs));
+        launch_slopes<T, GATED>(s, p.bias_chunks, wide, stream);
+        if (grad_bias) add_parts<float>(s.parts, p.bias_chunks, columns, grad_bias, stream);
+        if (makes) dz = s.dz, stride = p.stride;
+    }
+    if (const hipError_t e = hipGetLastError()) return e;
+    float *parts = p.parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + p.parts);
+    float *weight_parts = p.weight_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + p.weight_parts);
+    // The sum over dz's columns goes by whole vectors: behind them are zeros, and zeros are taken for the weights that would be there.
+    if (const hipError_t e = launch_sum<T, true, false>(p.to_x, Operand<T>{dz, stride, l.n_rows, columns}, Operand<T>{weight.at, weight.stride, weight.depth, columns},
+                                                        l.dim, scale, parts, parts ? nullptr : to_x, stream))
+        return e;
+    if (parts) add_parts(parts, p.to_x.splits, l.n_rows * l.dim, to_x, stream);
+    if (const hipError_t e = launch_sum<T, false, false>(p.to_weight, Operand<T>{dz, stride, columns, l.n_rows}, Operand<T>{x.at, x.stride, x.depth, l.n_rows}, l.dim,
+                                                         scale, weight_parts, weight_parts ? nullptr : to_weight, stream))
+        return e;
+    if (weight_parts) add_parts(weight_parts, p.to_weight.splits, columns * l.dim, to_weight, stream);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t linear_bytes(const head_layer &l) { return plan_forward(l, false).bytes; }
+int64_t gated_bytes(const head_layer &l) { return plan_forward(l, true).bytes; }
+int64_t linear_grad_bytes(const head_layer &l) { return plan_backward(l, false).bytes; }
+int64_t gated_grad_bytes(const head_layer &l) { return plan_backward(l, true).bytes; }
+
+hipError_t launch_linear(const head_layer &l, const void *residual, int64_t residual_stride, float scale, void *y, void *z, void *workspace,
+                         hipStream_t stream)
+{
+    auto *call = l.dtype == HEAD_F32 ? forward<float, false> : forward<bf16, false>;
+    return call(l, residual, residual_stride, scale, y, z, static_cast<char *>(workspace), stream);
+}
+
+hipError_t launch_gated(const head_layer &l, void *y, void *z, void *workspace, hipStream_t stream)
+{
+    auto *call = l.dtype == HEAD_F32 ? forward<float, true> : forward<bf16, true>;
+    return call(l, nullptr, 0, 1.0f, y, z, static_cast<char *>(workspace), stream);
+}
+
+hipError_t launch_linear_grad(const head_layer &l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, float scale,
+                              void *grad_x, void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream)
+{
+    auto *call = l.dtype == HEAD_F32 ? backward<float, false> : backward<bf16, false>;
+    return call(l, z, z_stride, grad, grad_stride, scale, grad_x, grad_weight, grad_bias, static_cast<char *>(workspace), stream);
+}
+
+hipError_t launch_gated_grad(const head_layer &l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, void *grad_x,
+                             void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream)
+{
+    auto *call = l.dtype == HEAD_F32 ? backward<float, true> : backward<bf16, true>;
+    return call(l, z, z_stride, grad, grad_stride, 1.0f, grad_x, grad_weight, grad_bias, static_cast<char *>(workspace), stream);
+}
+
+}  // namespace head_impl

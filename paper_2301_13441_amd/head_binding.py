@@ -25,7 +25,10 @@ _f32, _f64 = ctypes.c_float, ctypes.c_double
 
 HEAD_EXPORTS = ["head_embed", "head_embed_grad_bytes", "head_embed_grad", "head_layer_norm", "head_layer_norm_grad_bytes",
                 "head_layer_norm_grad", "head_cross_entropy_bytes", "head_cross_entropy_grad_bytes", "head_cross_entropy",
-                "head_cross_entropy_grad", "head_adamw", "head_adamw_values", "head_strerror"]
+                "head_cross_entropy_grad", "head_adamw", "head_adamw_values", "head_linear_bytes", "head_linear", "head_linear_grad_bytes",
+                "head_linear_grad", "head_gated_bytes", "head_gated", "head_gated_grad_bytes", "head_gated_grad", "head_clip_bytes",
+                "head_clip", "head_strerror"]
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}  # HEAD_IDENTITY, HEAD_RELU, HEAD_GELU, HEAD_SILU
 BLOCK = 128  # HEAD_BLOCK
 
 
@@ -47,6 +50,15 @@ class _AdamwRule(ctypes.Structure):
                 ("eps", _f64), ("decay", _f64), ("seed", _u32)]
 
 
+class _Layer(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("activation", _i32), ("n_rows", _i64), ("dim", _i64), ("n_outputs", _i64), ("x", _p), ("x_stride", _i64),
+                ("weight", _p), ("weight_stride", _i64), ("bias", _p)]
+
+
+class _ClipTensor(ctypes.Structure):
+    _fields_ = [("grad", _p), ("out", _p), ("n", _i64), ("dtype", _i32)]
+
+
 class HeadError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: {code} ({_lib().head_strerror(int(code)).decode()})")
@@ -61,7 +73,7 @@ def _lib():
     if _ready is not None:
         return _ready
     lib = load_library()
-    ids, classes = ctypes.POINTER(_Ids), ctypes.POINTER(_Classes)
+    ids, classes, layer, clips = (ctypes.POINTER(t) for t in (_Ids, _Classes, _Layer, _ClipTensor))
     for name, result, *args in (
             ("head_embed", _i32, ids, _i32, _i64, _p, _i64, _f32, _p, _p),
             ("head_embed_grad_bytes", _i64, ids, _i32, _i64),
@@ -75,6 +87,16 @@ def _lib():
             ("head_cross_entropy_grad", _i32, classes, _p, _p, _p, _p, _p, _p, _p),
             ("head_adamw", _i32, ctypes.POINTER(_AdamwRule), ctypes.POINTER(_AdamwTensor), _i32, _p),
             ("head_adamw_values", _i32, ctypes.POINTER(_AdamwTensor), ctypes.POINTER(_p), ctypes.POINTER(_p), _i32, _p),
+            ("head_linear_bytes", _i64, layer),
+            ("head_linear", _i32, layer, _p, _i64, _f32, _p, _p, _p, _p),
+            ("head_linear_grad_bytes", _i64, layer),
+            ("head_linear_grad", _i32, layer, _p, _i64, _p, _i64, _f32, _p, _p, _p, _p, _p),
+            ("head_gated_bytes", _i64, layer),
+            ("head_gated", _i32, layer, _p, _p, _p, _p),
+            ("head_gated_grad_bytes", _i64, layer),
+            ("head_gated_grad", _i32, layer, _p, _i64, _p, _i64, _p, _p, _p, _p, _p),
+            ("head_clip_bytes", _i64, clips, _i32),
+            ("head_clip", _i32, clips, _i32, _f64, _p, _p, _p),
             ("head_strerror", ctypes.c_char_p, _i32)):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = result, args
@@ -103,7 +125,9 @@ def _native():
             _head_call.bind(*(entry_point(getattr(lib, name)) for name in (
                 "head_embed", "head_embed_grad_bytes", "head_embed_grad", "head_layer_norm", "head_layer_norm_grad_bytes",
                 "head_layer_norm_grad", "head_cross_entropy_bytes", "head_cross_entropy", "head_cross_entropy_grad_bytes",
-                "head_cross_entropy_grad", "head_adamw", "head_adamw_values")))
+                "head_cross_entropy_grad", "head_adamw", "head_adamw_values", "head_linear_bytes", "head_linear", "head_linear_grad_bytes",
+                "head_linear_grad", "head_gated_bytes", "head_gated", "head_gated_grad_bytes", "head_gated_grad", "head_clip_bytes",
+                "head_clip")))
             _calls = _head_call
         except ImportError as exc:
             warnings.warn(f"the native calls of the head cannot be imported ({exc}): calls take some microseconds more; "
@@ -482,3 +506,161 @@ def head_adamw_values(states, params, stream=None):
             at_m[k], at_v[k] = m.data_ptr(), v.data_ptr()
         _check(_lib().head_adamw_values(rows, at_m, at_v, n, s), "head_adamw_values")
     return out
+
+
+def _activation(name) -> int:
+    try:
+        return ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"activation must be one of {list(ACTIVATIONS)}, not {name!r}") from None
+
+
+def _layer(x, weight, bias, activation: int, halves: int):
+    import torch
+    _tensor(x, "x", shape=(None, None))
+    dtype = _dtype(x, "x")
+    _tensor(weight, "weight", x.dtype, (None, x.shape[1]), x)
+    if weight.shape[0] % halves:
+        raise ValueError(f"weight must have as many rows of gates as of values, not {weight.shape[0]} in all")
+    if bias is not None:
+        _tensor(bias, "bias", torch.float32, (weight.shape[0],), x)
+    return _Layer(dtype, activation, x.shape[0], x.shape[1], weight.shape[0] // halves, x.data_ptr(), _stride(x), weight.data_ptr(),
+                  _stride(weight), _at(bias))
+
+
+def head_linear(x, weight, bias=None, activation: Optional[str] = None, residual=None, scale: float = 1.0, keep: bool = False, stream=None):
+    """y = residual + scale * activation(z) with z = x weight^T + bias.
+
+    x: [n_rows, dim] float32 or bfloat16, weight: [n_outputs, dim] of the same type, bias: float32 [n_outputs] or None.  activation:
+    None, "relu", "gelu" (x times the normal distribution's integral up to x) or "silu".  residual: [n_rows, n_outputs] of the same type, or
+    None.  Returns y, [n_rows, n_outputs] of the same type, and with keep (y, z): z, which the gradients of a layer with an
+    activation need.
+    """
+    act = _activation(activation)
+    if stream is None:
+        got = _native().linear(x, weight, bias, act, residual, scale, keep)
+        if got is not None:
+            return _done(got, "head_linear")
+    import torch
+    layer = _layer(x, weight, bias, act, 1)
+    shape = (layer.n_rows, layer.n_outputs)
+    if residual is not None:
+        _tensor(residual, "residual", x.dtype, shape, x)
+    nbytes = _check(_lib().head_linear_bytes(layer), "head_linear")
+    with _on(stream, x, (x, weight, bias, residual)) as s:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        z = torch.empty(shape, dtype=x.dtype, device=x.device) if keep else None
+        work = _workspace(nbytes, x)
+        _check(_lib().head_linear(layer, _at(residual), 0 if residual is None else _stride(residual), scale, y.data_ptr(), _at(z), _at(work), s),
+               "head_linear")
+    return (y, z) if keep else y
+
+
+def _layer_grad(what, call, nbytes, layer, halves, grad, x, weight, z, bias, stream):
+    """The checks, outputs and workspace of a layer's gradient; call(z and its stride, grad and its stride, outputs, workspace, stream)."""
+    import torch
+    _tensor(grad, "grad", x.dtype, (layer.n_rows, layer.n_outputs), x)
+    if z is not None:
+        _tensor(z, "z", x.dtype, (layer.n_rows, weight.shape[0]), x)
+    elif halves == 2 or layer.activation:
+        raise ValueError("z is what the layer gave with keep=True, and is needed where there is an activation")
+    nbytes = _check(nbytes(layer), what)
+    with _on(stream, x, (grad, x, weight, z)) as s:
+        grad_x = torch.empty((layer.n_rows, layer.dim), dtype=x.dtype, device=x.device)
+        grad_weight = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
+        grad_bias = torch.empty(weight.shape[0], dtype=torch.float32, device=x.device) if bias else None
+        work = _workspace(nbytes, x)
+        _check(call(_at(z), 0 if z is None else _stride(z), grad.data_ptr(), _stride(grad), grad_x.data_ptr(), grad_weight.data_ptr(),
+                    _at(grad_bias), _at(work), s), what)
+    return grad_x, grad_weight, grad_bias
+
+
+def head_linear_grad(grad, x, weight, z=None, activation: Optional[str] = None, scale: float = 1.0, bias: bool = True, stream=None):
+    """The gradients of head_linear from grad, that of y.  z: what head_linear gave with keep=True; without an activation it is not needed.
+    Returns (grad_x, grad_weight, grad_bias): the first two like x and weight, grad_bias float32 [n_outputs], or None without `bias`.  The
+    residual's gradient is grad itself."""
+    act = _activation(activation)
+    if stream is None:
+        got = _native().linear_grad(grad, x, weight, z, act, scale, bias)
+        if got is not None:
+            return _done(got, "head_linear_grad")
+    layer = _layer(x, weight, None, act, 1)
+
+    def call(z_at, z_stride, grad_at, grad_stride, *rest):
+        return _lib().head_linear_grad(layer, z_at, z_stride, grad_at, grad_stride, scale, *rest)
+    return _layer_grad("head_linear_grad", call, _lib().head_linear_grad_bytes, layer, 1, grad, x, weight, z, bias, stream)
+
+
+def head_gated(x, weight, bias=None, activation: Optional[str] = "silu", keep: bool = False, stream=None):
+    """y = activation(gates) * values, where z = x weight^T + bias is the gates, its first half of columns, and the values.
+
+    x: [n_rows, dim] float32 or bfloat16, weight: [2 * n_outputs, dim] of the same type, bias: float32 [2 * n_outputs] or None, activation: as
+    in head_linear.  Returns y, [n_rows, n_outputs] of the same type, and with keep (y, z): z, [n_rows, 2 * n_outputs], which
+    the gradients need.
+    """
+    act = _activation(activation)
+    if stream is None:
+        got = _native().gated(x, weight, bias, act, keep)
+        if got is not None:
+            return _done(got, "head_gated")
+    import torch
+    layer = _layer(x, weight, bias, act, 2)
+    nbytes = _check(_lib().head_gated_bytes(layer), "head_gated")
+    with _on(stream, x, (x, weight, bias)) as s:
+        y = torch.empty((layer.n_rows, layer.n_outputs), dtype=x.dtype, device=x.device)
+        z = torch.empty((layer.n_rows, weight.shape[0]), dtype=x.dtype, device=x.device) if keep else None
+        work = _workspace(nbytes, x)
+        _check(_lib().head_gated(layer, y.data_ptr(), _at(z), _at(work), s), "head_gated")
+    return (y, z) if keep else y
+
+
+def head_gated_grad(grad, x, weight, z, activation: Optional[str] = "silu", bias: bool = True, stream=None):
+    """The gradients of head_gated from grad, that of y, and z, which head_gated gave with keep=True.  Returns (grad_x, grad_weight, grad_bias):
+    the first two like x and weight, grad_bias float32 [2 * n_outputs], or None without `bias`."""
+    act = _activation(activation)
+    if stream is None:
+        got = _native().gated_grad(grad, x, weight, z, act, bias)
+        if got is not None:
+            return _done(got, "head_gated_grad")
+    layer = _layer(x, weight, None, act, 2)
+
+    def call(*args):
+        return _lib().head_gated_grad(layer, *args)
+    return _layer_grad("head_gated_grad", call, _lib().head_gated_grad_bytes, layer, 2, grad, x, weight, z, bias, stream)
+
+
+def head_clip(grads, max_norm: float, in_place: bool = False, stream=None):
+    """The 2-norm of all tensors' values together, and the tensors times min(1, max_norm / norm).
+
+    grads: contiguous float32 and bfloat16 tensors of any shape, a list.  max_norm: above 0; math.inf for no limit.  Returns (norm, clipped): norm a
+    float32 tensor of no dimensions, clipped a list of new tensors like grads, or with in_place of grads themselves, whose values are
+    replaced: they must not overlap.  A NaN among the values makes the norm and, unless there is no limit, all of them NaN.
+    """
+    if stream is None:
+        got = _native().clip(grads, max_norm, in_place)
+        if got is not None:
+            return _done(got, "head_clip")
+    import torch
+    grads = list(grads)
+    if not grads:
+        raise ValueError("there are no tensors")
+    if not max_norm > 0:
+        raise ValueError(f"max_norm must be above 0, not {max_norm}")
+    for k, t in enumerate(grads):
+        _tensor(t, f"grads[{k}]", like=grads[0] if k else None)
+        _dtype(t, f"grads[{k}]")
+        if not t.is_contiguous():
+            raise ValueError(f"grads[{k}] must be contiguous")
+    if in_place:
+        ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in grads if t.numel())
+        if any(end > begin for (_, end), (begin, _) in zip(ends, ends[1:])):
+            raise ValueError("tensors that are replaced must not overlap")
+    with _on(stream, grads[0], grads) as s:
+        norm = torch.empty((), dtype=torch.float32, device=grads[0].device)
+        out = grads if in_place else [torch.empty_like(t, memory_format=torch.contiguous_format) for t in grads]
+        tensors = (_ClipTensor * len(grads))(*(_ClipTensor(t.data_ptr(), o.data_ptr(), t.numel(), _dtype(t, "grads")) for t, o in zip(grads, out)))
+        work = _workspace(_check(_lib().head_clip_bytes(tensors, len(grads)), "head_clip"), grads[0])
+        if in_place:
+            torch.autograd.graph.increment_version([t for t in grads if not t.is_inference()])  # what autograd has kept of them is out of date
+        _check(_lib().head_clip(tensors, len(grads), max_norm, norm.data_ptr(), _at(work), s), "head_clip")
+    return norm, list(out)
