@@ -247,6 +247,7 @@ int head_linear(const head_layer *l, const void *residual, int64_t residual_stri
 int64_t head_linear_grad_bytes(const head_layer *l)
 {
     if (int rc = check_layer(l, 1)) return rc;
+    if (l->n_outputs > HEAD_MAX_OUTPUTS) return HEAD_ELIMIT;
     return linear_grad_bytes(*l);
 }
 
@@ -282,6 +283,7 @@ int head_gated(const head_layer *l, void *y, void *z, void *workspace, void *str
 int64_t head_gated_grad_bytes(const head_layer *l)
 {
     if (int rc = check_layer(l, 2)) return rc;
+    if (l->n_outputs > HEAD_MAX_OUTPUTS) return HEAD_ELIMIT;
     return gated_grad_bytes(*l);
 }
 

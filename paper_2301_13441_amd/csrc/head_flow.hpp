@@ -1,0 +1,264 @@
+// The products of head_linear.hip, on gfx950: the shapes and the layout in LDS of head_product.hpp, with the matrix core fed across the steps of
+// the sum and across tiles.
+//
+// A step's tiles of A and B are loaded STAGES steps ahead, into the stage of LDS that a step has just left.  A wavefront reads the next 32
+// bytes of the sum's axis while the matrix core works on the last ones, over the end of a step too: the barrier, the loads that it
+// lets go and the next step's first reads come before a step's last instructions of the matrix core, so that it has work meanwhile.
+//
+// Loads go through buffer descriptors, whose bounds give zeros past the last row and past the end of a sum that lies across memory, and by which a
+// lane has one 32-bit offset for all its loads of an operand.
+#pragma once
+
+#include "head_product.hpp"
+
+namespace head_impl {
+namespace {
+
+constexpr int64_t FLOW_STRIDE = (1 << 21) + 256;  // bytes of a row's step, at most: offsets in a tile, of up to 256 rows, stay far below 2^31
+
+// Tiles of ROWS x 128 bytes of an operand: layout in LDS and meaning of the parameters as in Tile.
+template <class T, int STEP, bool ALONG, int ROWS, int THREADS, int NT, bool PAIRS, int FRAGMENTS>
+struct FlowTile {
+    static constexpr int VALUES = 16 / sizeof(T), DEPTH = STEP / sizeof(T), BYTES = ROWS * STEP, LOADS = BYTES / (THREADS * 16), WAVES = THREADS / 64;
+    static constexpr int SLOTS = ALONG ? STEP / 16 : ROWS / VALUES;  // chunks of a row of the tile
+    static constexpr int EACH = 64 / SLOTS;                          // rows that a wavefront loads at a time
+    static constexpr int ADDRESSES = ALONG ? STEP / 32 : FRAGMENTS;
+    static_assert(LOADS > 0, "every lane has a chunk of a step");
+
+    static __device__ __forceinline__ int key(int r)
+    {
+        if constexpr (ALONG) return r / (256 / STEP) % SLOTS;
+        if constexpr (sizeof(T) == 4) return r / 4 % 2 * 8;
+        return ROWS >= 128 ? r % 4 * 4 : r / 2 % 2 * 4;
+    }
+
+    uint32_t lane_offset;  // bytes from the tile's first value to this lane's first chunk
+    int lane_at;           // its index of the sum in the tile, where that lies along memory
+    uint32_t address[ADDRESSES];  // of this lane's reads in a half of LDS
+    const char *base, *base1;  // of the tile, at the step to load; base1: of its rows in the other half of the operand's
+    int64_t bytes, bytes1;     // from there to the operand's end
+    int64_t left;              // of the sum
+
+    // Row of memory, from the tile's first, of a row of an ALONG tile.  A lane's share of r and a load's have no bits in common, and go
+    // through this one by one.
+    static __device__ __forceinline__ int row_of(int r)
+    {
+        const int in = r % (NT * 32);
+        if constexpr (PAIRS) return (r - in) / 2 + in % 32 * (NT / 2) + in / 64;
+        return r - in + in % 32 * NT + in / 32;
+    }
+
+    __device__ __forceinline__ void begin(int64_t stride, int first_row)
+    {
+        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = wave * EACH + lane / (64 / EACH);
+        if constexpr (ALONG) {
+            lane_at = ((lane % SLOTS) ^ key(r)) * VALUES;
+            lane_offset = static_cast<uint32_t>(row_of(r) * static_cast<int>(stride * sizeof(T)) + lane_at * static_cast<int>(sizeof(T)));
+#pragma unroll
+            for (int kk = 0; kk < ADDRESSES; ++kk) {
+                const int row = first_row + threadIdx.x % 32, chunk = 2 * kk + lane / 32;
+                address[kk] = row * STEP + ((chunk ^ key(row)) * 16);
+            }
+        } else {
+            lane_at = 0;
+            lane_offset = static_cast<uint32_t>(r * static_cast<int>(stride * sizeof(T)) + ((lane % SLOTS) ^ key(r)) * 16);
+#pragma unroll
+            for (int f = 0; f < ADDRESSES; ++f) {
+                const int row = first_row + f * 32;
+                if constexpr (sizeof(T) == 2) {
+                    const int i = threadIdx.x % 16, depth = lane / 32 * VALUES + i / 4, in = row + threadIdx.x % 32 / 16 * 16 + i % 4 * 4;
+                    address[f] = depth * (ROWS * 2) + (in / VALUES ^ key(depth)) * 16 + in % VALUES * 2;
+                } else {
+                    // a chunk's values are of four indexes, which the key has in common
+                    const int r32 = row + threadIdx.x % 32, depth = lane / 32 * VALUES;
+                    address[f] = depth * (ROWS * 4) + (r32 / VALUES ^ key(depth)) * 16 + r32 % VALUES * 4;
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void aim(const Operand<T> &o, int64_t row0, int64_t from)
+    {
+        const int64_t row_bytes = o.stride * static_cast<int64_t>(sizeof(T));
+        left = o.depth - from;
+        if constexpr (ALONG) {
+            const int64_t end = round_to_chunk(o.depth) * static_cast<int64_t>(sizeof(T));  // of a row
+            const int64_t rows = PAIRS ? o.rows / 2 : o.rows, first = PAIRS ? row0 / 2 : row0;
+            base = reinterpret_cast<const char *>(o.at + from) + first * row_bytes;
+            bytes = (rows - 1 - first) * row_bytes + end - from * static_cast<int64_t>(sizeof(T));
+            if constexpr (PAIRS) {
+                base1 = base + rows * row_bytes;
+                bytes1 = bytes;
+            }
+        } else {
+            base = reinterpret_cast<const char *>(o.at + row0) + from * row_bytes;
+            bytes = (left - 1) * row_bytes + (round_to_chunk(o.rows) - row0) * static_cast<int64_t>(sizeof(T));
+        }
+    }
+    static __device__ __forceinline__ int64_t round_to_chunk(int64_t n) { return (n + VALUES - 1) / VALUES * VALUES; }
+
+    // The step that base is at, to LDS, and on to the next one.
+    __device__ __forceinline__ void load(const Operand<T> &o, char *lds)
+    {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host's pass knows no descriptors
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const int row_bytes = static_cast<int>(o.stride * sizeof(T));
+        auto records = [](int64_t n) { return static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(n, INT32_MAX))); };
+        auto descriptor = [&](const char *at, int64_t n) {
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, records(n), 0x00020000);  // no stride: bytes; 32-bit format
+        };
+        const auto all = descriptor(base, bytes);
+        uint32_t offset = lane_offset;
+        if constexpr (ALONG) {
+            if (left < DEPTH) offset = lane_at < left ? lane_offset : 0x80000000u;  // past any end, with any row's offset too: zeros
+        }
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int r = j * WAVES * EACH;  // and this wavefront's EACH rows, which are in the lane's offset
+            const auto to = (LdsChunk)(lds + (j * WAVES + wave) * 1024);
+            if constexpr (PAIRS) {
+                // rows r + wave * EACH .. of the tile are of one half, the same one for all lanes
+                const bool other = (r + wave * EACH) / 32 % 2;
+                const auto half = other ? descriptor(base1, bytes1) : all;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(half, to, 16, offset + static_cast<uint32_t>(row_of(r) * row_bytes), 0, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(all, to, 16, offset + static_cast<uint32_t>((ALONG ? row_of(r) : r) * row_bytes), 0, 0, 0);
+            }
+        }
+        const int64_t ahead = ALONG ? int64_t{STEP} : int64_t{DEPTH} * row_bytes;
+        base += ahead;
+        bytes -= ahead;
+        if constexpr (PAIRS) {
+            base1 += ahead;
+            bytes1 -= ahead;
+        }
+        left -= DEPTH;
+#endif
+    }
+
+    // Fragment f of 32 rows, of the kk-th 32 bytes of the sum's axis.
+    __device__ __forceinline__ Chunk read(const char *lds, int f, int kk) const
+    {
+        if constexpr (ALONG) {
+            return *reinterpret_cast<const Chunk *>(lds + address[kk] + f * 32 * STEP);
+        } else if constexpr (sizeof(T) == 2) {
+            Half h[2];
+            h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalf)(lds + address[f] + kk * 2 * VALUES * ROWS * 2));
+            h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalf)(lds + address[f] + (kk * 2 * VALUES + 4) * ROWS * 2));
+            return *reinterpret_cast<Chunk *>(h);
+        } else {
+            Chunk p;
+#pragma unroll
+            for (int j = 0; j < VALUES; ++j)
+                p[j] = *reinterpret_cast<const float *>(lds + address[f] + (kk * 2 * VALUES + j) * ROWS * 4);
+            return p;
+        }
+    }
+};
+
+// The products of a workgroup's tiles, one after the other.  next() aims at the next tile to load (aim), or does nothing where there is none.
+template <class T, class S, int STEP, int STAGES, bool A_ALONG, bool B_ALONG, bool PAIRS = false>
+struct Flow {
+    using A = FlowTile<T, STEP, A_ALONG, S::M, S::THREADS, 1, false, S::MT>;
+    using B = FlowTile<T, STEP, B_ALONG, S::N, S::THREADS, S::NEXT || PAIRS ? S::NT : 1, PAIRS, S::NT>;
+    static_assert(B_ALONG || !(S::NEXT || PAIRS), "rows of a tile that lies across stay in order");
+    static_assert(!PAIRS || S::NT % 2 == 0, "a wavefront's columns are as many of each half");
+    static constexpr int STAGE = A::BYTES + B::BYTES, BYTES = STAGES * STAGE;
+    static constexpr int KK = STEP / 32, DEPTH = A::DEPTH;
+    static constexpr int LATER = (STAGES - 2) * (A::LOADS + B::LOADS);  // loads behind those of the next stage
+
+    const Operand<T> &a, &b;
+    char *lds;
+    A ta;
+    B tb;
+    int steps = 0;  // left to load of the tile that is aimed at
+    int stage = 0;  // where the step is that the matrix core is at
+    Chunk x[2][S::MT], y[2][S::NT];
+
+    __device__ __forceinline__ Flow(const Operand<T> &a_, const Operand<T> &b_, char *lds_) : a(a_), b(b_), lds(lds_)
+    {
+        ta.begin(a.stride, S::wave_m() * (S::MT * 32));
+        tb.begin(b.stride, S::wave_n() * (S::NT * 32));
+    }
+
+    static __device__ __forceinline__ int steps_of(int64_t from, int64_t to) { return static_cast<int>((to - from + DEPTH - 1) / DEPTH); }
+
+    // A tile whose sum goes over [from, to).
+    __device__ __forceinline__ void aim(int64_t row0, int64_t column0, int64_t from, int64_t to)
+    {
+        steps = steps_of(from, to);
+        ta.aim(a, row0, from);
+        tb.aim(b, column0, from);
+    }
+
+    template <class Next>
+    __device__ __forceinline__ void load(int to, Next next)
+    {
+        if (steps == 0) next();
+        if (steps == 0) return;
+        ta.load(a, lds + to * STAGE);
+        tb.load(b, lds + to * STAGE + A::BYTES);
+        --steps;
+    }
+
+    __device__ __forceinline__ void read(int kk)
+    {
+        const char *at = lds + stage * STAGE;
+#pragma unroll
+        for (int mt = 0; mt < S::MT; ++mt) x[kk % 2][mt] = ta.read(at, mt, kk);
+#pragma unroll
+        for (int nt = 0; nt < S::NT; ++nt) y[kk % 2][nt] = tb.read(at + A::BYTES, nt, kk);
+    }
+
+    // The next stage is there, for all wavefronts, and nobody reads what they have read any more.
+    __device__ __forceinline__ void meet() const
+    {
+        if (steps == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // at the end there are no later loads
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+
+    // Once, before the first tile.
+    template <class Next>
+    __device__ __forceinline__ void begin(Next next)
+    {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) load(s, next);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read(0);
+    }
+
+    // The next tile's sum, of `count` steps, into c.
+    template <class Next>
+    __device__ __forceinline__ void run(Acc (&c)[S::MT][S::NT], int count, Next next)
+    {
+#pragma unroll
+        for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < S::NT; ++nt) c[mt][nt] = Acc{};
+        for (; count > 0; --count) {
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if (kk + 1 < KK) {
+                    read(kk + 1);
+                } else {
+                    meet();
+                    load(stage, next);
+                    stage = stage + 1 < STAGES ? stage + 1 : 0;
+                    read(0);
+                }
+#pragma unroll
+                for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+                    for (int nt = 0; nt < S::NT; ++nt) multiply(x[kk % 2][mt], y[kk % 2][nt], c[mt][nt], T());
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+};
+
+}  // namespace
+}  // namespace head_impl

@@ -73,7 +73,7 @@ struct End {
     float scale;
     T *y, *z;
     int64_t n_rows, outs;  // columns of y
-    bool wide;             // rows of residual, y and z are whole in pairs of values
+    bool wide;             // rows of residual, y and z are whole in what a lane stores of them, and short
 };
 
 // Layers of few rows, forward, have a kernel of their own (head_few.hip), without a workspace.

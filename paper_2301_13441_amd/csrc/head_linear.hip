@@ -13,33 +13,40 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "head_flow.hpp"
 #include "head_layer.hpp"
-#include "head_product.hpp"
 
 namespace head_impl {
 namespace {
 
 // ---- forward
 
-// A lane's results of a tile, C = z before the bias, through activation and residual.
-template <class T, class S, bool GATED>
+// A lane's results of a tile, C = z before the bias, through activation and residual.  FULL: all rows and columns of the tile are there,
+// rows are whole in what a lane stores at a time, and short enough that four of them are an offset of 32 bits.
+template <class T, class S, bool GATED, bool FULL>
 __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float (&bias)[S::NT], const End<T> &e, int64_t row0, int64_t column0)
 {
     constexpr int N = GATED ? S::NT / 2 : S::NT;  // adjacent columns of y that a lane has
-    const int64_t first = row0 + S::row(0, 0), left = e.n_rows - first;
-    const int rows = static_cast<int>(std::min<int64_t>(S::M, left));
-    // of a wavefront's columns, a lane's first one of y
-    const int64_t column = GATED ? column0 / 2 + S::wave_n() * (S::NT * 16) + threadIdx.x % 32 * N : column0 + S::column(0);
-    T *y = e.y + first * e.outs + column;
-    T *z = e.z ? e.z + first * (GATED ? 2 : 1) * e.outs + column : nullptr;
-    const T *residual = !GATED && e.residual ? e.residual + first * e.residual_stride + column : nullptr;
-    const int columns = static_cast<int>(std::min<int64_t>(N, e.outs - column));
-    if (columns <= 0) return;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wave_m = wave / S::WAVES_N, wave_n = wave % S::WAVES_N;
+    // Addresses are a wavefront's, which a scalar holds, and a lane's offset from there.
+    const int64_t first = row0 + wave_m * (S::MT * 32), column1 = (GATED ? column0 / 2 : column0) + wave_n * (N * 32);
+    const int down0 = lane / 32 * 4, across = lane % 32 * N;
+    const int rows = static_cast<int>(std::min<int64_t>(S::M, e.n_rows - first)) - down0;
+    const int columns = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(N, e.outs - column1 - across)));
+    if (!FULL && columns == 0) return;
+    using Offset = std::conditional_t<FULL, uint32_t, int64_t>;  // in values
+    const int64_t z_columns = GATED ? 2 * e.outs : e.outs;
+    const Offset in_y = static_cast<Offset>(down0 * e.outs + across), in_z = static_cast<Offset>(down0 * z_columns + across),
+                 in_residual = static_cast<Offset>(down0 * e.residual_stride + across);
+    T *y = e.y + first * e.outs + column1;
+    T *z = e.z ? e.z + first * z_columns + column1 : nullptr;
+    const T *residual = !GATED && e.residual ? e.residual + first * e.residual_stride + column1 : nullptr;
     auto put = [&](T *to, const float (&v)[N]) {
         Pack<T, N> p;
 #pragma unroll
         for (int k = 0; k < N; ++k) p.v[k] = narrow<T>(v[k]);
-        if (e.wide) {
+        if (FULL) {
             *reinterpret_cast<Pack<T, N> *>(to) = p;
         } else {
 #pragma unroll
@@ -54,7 +61,7 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int down = mt * 32 + i / 4 * 8 + i % 4;
-                if (down >= rows) continue;
+                if (!FULL && down >= rows) continue;
                 float v[N];
                 if constexpr (GATED) {
                     float gate[N], value[N];
@@ -65,18 +72,18 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
                         v[k] = Act(gate[k]).value * value[k];
                     }
                     if (z) {
-                        put(z + down * 2 * e.outs, gate);
-                        put(z + down * 2 * e.outs + e.outs, value);
+                        put(z + down * z_columns + in_z, gate);
+                        put(z + (down * z_columns + e.outs) + in_z, value);
                     }
                 } else {
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = c[mt][k][i] + bias[k];
-                    if (z) put(z + down * e.outs, v);
+                    if (z) put(z + down * z_columns + in_z, v);
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = e.scale * Act(v[k]).value;
                     if (residual) {
-                        const T *from = residual + down * e.residual_stride;
-                        if (e.wide) {
+                        const T *from = residual + down * e.residual_stride + in_residual;
+                        if (FULL) {
                             const Pack<T, N> r = *reinterpret_cast<const Pack<T, N> *>(from);
 #pragma unroll
                             for (int k = 0; k < N; ++k) v[k] += widen(r.v[k]);
@@ -86,7 +93,7 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
                         }
                     }
                 }
-                put(y + down * e.outs, v);
+                put(y + down * e.outs + in_y, v);
             }
     });
 }
@@ -95,35 +102,35 @@ template <class T, class S, bool GATED>
 __global__ __launch_bounds__(S::THREADS, 2) void layer_kernel(Operand<T> x, Operand<T> weight, End<T> e, uint32_t row_tiles, uint32_t column_tiles)
 {
     extern __shared__ char lds[];
-    Products<T, S, true, true, GATED> products(x, weight, lds);
+    Flow<T, S, STEP, 2, true, true, GATED> flow(x, weight, lds);
     const uint32_t tiles = row_tiles * column_tiles;
-    uint32_t column_tile = 0, row_tile = 0;
-    auto aim = [&](uint32_t tile) {
-        if (tile >= tiles) return;
-        tile_of(tile, row_tiles, column_tiles, row_tile, column_tile);
-        products.aim(int64_t{S::M} * row_tile, int64_t{S::N} * column_tile, 0, x.depth, row_tile + column_tile);
+    uint32_t ahead = blockIdx.x;
+    auto next = [&] {
+        if (ahead >= tiles) return;
+        uint32_t row_tile, column_tile;
+        tile_of(ahead, row_tiles, column_tiles, row_tile, column_tile);
+        flow.aim(int64_t{S::M} * row_tile, int64_t{S::N} * column_tile, 0, x.depth);
+        ahead += gridDim.x;
     };
-    aim(blockIdx.x);
+    flow.begin(next);
     for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        uint32_t row_tile, column_tile;
+        tile_of(tile, row_tiles, column_tiles, row_tile, column_tile);
         const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * row_tile;
+        Acc c[S::MT][S::NT];
+        flow.run(c, flow.steps_of(0, x.depth), next);
         float bias[S::NT] = {};
         if (e.bias) {
 #pragma unroll
             for (int nt = 0; nt < S::NT; ++nt) {
-                int64_t k = column0 + S::column(nt);
-                bool there = k < e.outs;
-                if constexpr (GATED) {
-                    k = column0 / 2 + S::wave_n() * (S::NT * 16) + threadIdx.x % 32 * (S::NT / 2) + nt / 2;
-                    there = k < e.outs;
-                    k += nt % 2 * e.outs;
-                }
-                bias[nt] = there ? e.bias[k] : 0.0f;
+                constexpr int N = GATED ? S::NT / 2 : S::NT;
+                const int64_t k = (GATED ? column0 / 2 : column0) + S::wave_n() * (N * 32) + threadIdx.x % 32 * N + (GATED ? nt / 2 : nt);
+                bias[nt] = k < e.outs ? e.bias[GATED ? k + nt % 2 * e.outs : k] : 0.0f;
             }
         }
-        Acc c[S::MT][S::NT];
-        products.clear(c);
-        products.run(c, [&] { aim(tile + gridDim.x); });
-        finish<T, S, GATED>(c, bias, e, row0, column0);
+        const int64_t all_columns = GATED ? 2 * e.outs : e.outs;
+        if (e.wide && row0 + S::M <= e.n_rows && column0 + S::N <= all_columns) finish<T, S, GATED, true>(c, bias, e, row0, column0);
+        else finish<T, S, GATED, false>(c, bias, e, row0, column0);
     }
 }
 
@@ -245,21 +252,29 @@ __global__ __launch_bounds__(S::THREADS, 2) void sum_kernel(Operand<T> a, Operan
 {
     static_assert(!S::NEXT, "a lane's columns are 32 apart");
     extern __shared__ char lds[];
-    Products<T, S, A_ALONG, B_ALONG> products(a, b, lds);
+    Flow<T, S, STEP, 2, A_ALONG, B_ALONG> flow(a, b, lds);
     const uint32_t tiles = row_tiles * column_tiles * splits;
-    uint32_t column_tile = 0, row_tile = 0;
-    auto aim = [&](uint32_t tile) {
-        if (tile >= tiles) return;
+    uint32_t ahead = blockIdx.x;
+    auto place = [&](uint32_t tile, int64_t &row0, int64_t &column0, int64_t &split) {
+        uint32_t row_tile, column_tile;
         tile_of(tile, row_tiles * splits, column_tiles, row_tile, column_tile);
-        const int64_t depth0 = row_tile / row_tiles * split_depth;
-        products.aim(int64_t{S::M} * (row_tile % row_tiles), int64_t{S::N} * column_tile, depth0, std::min(a.depth, depth0 + split_depth), 0);
+        row0 = int64_t{S::M} * (row_tile % row_tiles);
+        column0 = int64_t{S::N} * column_tile;
+        split = row_tile / row_tiles;
     };
-    aim(blockIdx.x);
+    auto next = [&] {
+        if (ahead >= tiles) return;
+        int64_t row0, column0, split;
+        place(ahead, row0, column0, split);
+        flow.aim(row0, column0, split * split_depth, std::min(a.depth, (split + 1) * split_depth));
+        ahead += gridDim.x;
+    };
+    flow.begin(next);
     for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * (row_tile % row_tiles), split = row_tile / row_tiles;
+        int64_t row0, column0, split;
+        place(tile, row0, column0, split);
         Acc c[S::MT][S::NT];
-        products.clear(c);
-        products.run(c, [&] { aim(tile + gridDim.x); });
+        flow.run(c, flow.steps_of(split * split_depth, std::min(a.depth, (split + 1) * split_depth)), next);
         const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
         const int64_t at = (row0 + S::row(0, 0)) * columns + column0 + S::column(0);
         auto each = [&](auto store) {
@@ -294,6 +309,12 @@ template <>
 struct GatedOf<Small> { using Type = Shape<128, 128, 2, 2, false>; };
 template <>
 struct GatedOf<Large> { using Type = Shape<256, 256, 4, 2, false>; };
+
+// A linear layer's: a lane has as many adjacent columns of y as its wavefront has 32 of them.
+template <class Size>
+struct LinearOf { using Type = typename Size::template Of<true>; };
+template <>
+struct LinearOf<Large> { using Type = Shape<256, 256, 4, 2, true>; };
 
 enum { TINY, SMALL, LARGE };
 
@@ -345,7 +366,7 @@ struct Plan : Space {
 bool whole(int32_t dtype, const void *at, int64_t stride, int64_t n)
 {
     const int e = value_bytes(dtype);
-    return (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(n * e)) % 16 == 0;
+    return stride * e <= FLOW_STRIDE && (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(n * e)) % 16 == 0;
 }
 
 void plan_operands(const head_layer &l, int64_t columns, Plan &p)
@@ -451,11 +472,14 @@ hipError_t forward(const head_layer &l, const void *residual, int64_t residual_s
         hipLaunchKernelGGL((finish_kernel<T, GATED>), grid_of(ceil_div(l.n_rows * l.n_outputs, 256)), dim3(256), 0, stream, parts, c.splits, end);
         return hipGetLastError();
     }
-    const uint64_t bits = address(y) | address(z) | address(residual) | static_cast<uint64_t>((l.n_outputs | end.residual_stride) * sizeof(T));
-    end.wide = bits % (2 * sizeof(T)) == 0;
+    auto rows_whole = [&](int bytes) {  // in pieces of that many, and four of them in 32 bits of offset
+        const uint64_t bits = address(y) | address(z) | address(residual) | static_cast<uint64_t>((l.n_outputs | end.residual_stride) * sizeof(T));
+        return bits % bytes == 0 && std::max(2 * l.n_outputs, end.residual_stride) <= int64_t{1} << 26;
+    };
     return with_size<T>(c.size, [&](auto size) {
         using Size = decltype(size);
-        using S = std::conditional_t<GATED, typename GatedOf<Size>::Type, typename Size::template Of<true>>;
+        using S = typename std::conditional_t<GATED, GatedOf<Size>, LinearOf<Size>>::Type;
+        end.wide = rows_whole((GATED ? S::NT / 2 : S::NT) * static_cast<int>(sizeof(T)));
         return launch_tiles<S, layer_kernel<T, S, GATED>>(c.tiles(), Size::RESIDENT, stream, x, weight, end, static_cast<uint32_t>(c.row_tiles),
                                                           static_cast<uint32_t>(c.column_tiles));
     });

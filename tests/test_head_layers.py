@@ -123,6 +123,8 @@ def test_layers_refuse_bad_arguments_before_any_device_call():
             assert f(_layer(**far)) == -7, far
     for f in (gated, gated_grad):
         assert f(_layer(outs=500_000_001)) == -7
+    for f in (linear_grad, gated_grad):
+        assert f(_layer(outs=262_145)) == -7
     for f in (linear, gated):
         assert f(_layer(), y=None) == f(_layer(), y=66) == f(_layer(), z=66) == f(_layer(n=100, xs=9), work=None) == f(_layer(n=100, xs=9), work=72) == -1
         assert f(_layer(n=0, x=None), y=None, work=None) == 0
@@ -278,7 +280,7 @@ def test_gated_gradient(n, dim, outs, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,dim,outs", [(4100, 64, 4200), (300, 40, 60_001), (8300, 2100, 300), (2048, 2100, 2056)])
+@pytest.mark.parametrize("n,dim,outs", [(4100, 64, 4200), (300, 40, 60_001), (70, 24, 262_144), (8300, 2100, 300), (2048, 2100, 2056)])
 def test_layers_in_large_tiles(n, dim, outs):
     """bfloat16, sampled rows and columns of products that fill the device."""
     import torch
