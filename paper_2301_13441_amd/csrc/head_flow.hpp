@@ -5,6 +5,12 @@
 // bytes of the sum's axis while the matrix core works on the last ones, over the end of a step too: the barrier, the loads that it
 // lets go and the next step's first reads come before a step's last instructions of the matrix core, so that it has work meanwhile.
 //
+// Products of float32 values go to the matrix core as products of bfloat16 ones, for which its rate is sixteen times that for float32: a value is
+// the sum of three of 8 bits each, exactly, and of the nine products of two values' parts the three smallest, together below 2^-25 of the
+// whole, are left out, which is half of what a float32 product is rounded by.  The parts are made of what a wavefront has read, 11 vector
+// instructions for two values.  bfloat16 has nothing below 2^-133, so values below 2^-109 lose bits.  Infinite values, and the few that round to
+// one, have no such parts: a sum that is not finite in the end is made again, with float32 instructions (again).
+//
 // Loads go through buffer descriptors, whose bounds give zeros past the last row and past the end of a sum that lies across memory, and by which a
 // lane has one 32-bit offset for all its loads of an operand.
 #pragma once
@@ -156,6 +162,33 @@ struct FlowTile {
     }
 };
 
+// The three parts of 8 float32 values: x = high + middle + low, each to nearest of what is left.
+struct Parts {
+    Chunk high, middle, low;
+
+    __device__ __forceinline__ Parts(Chunk x0, Chunk x1)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a = i < 2 ? x0[i * 2] : x1[i * 2 - 4], b = i < 2 ? x0[i * 2 + 1] : x1[i * 2 - 3];
+            high[i] = of_two(a, b);
+            middle[i] = of_two(a, b);
+            low[i] = of_two(a, b);
+        }
+    }
+
+    // Two values as bfloat16 ones in a word, and what they leave in their place.
+    static __device__ __forceinline__ float of_two(float &a, float &b)
+    {
+        using Two = __bf16 __attribute__((ext_vector_type(2)));
+        using Pair = float __attribute__((ext_vector_type(2)));
+        const uint32_t word = __builtin_bit_cast(uint32_t, __builtin_convertvector((Pair{a, b}), Two));
+        a -= __uint_as_float(word << 16);
+        b -= __uint_as_float(word & 0xFFFF0000u);
+        return __uint_as_float(word);
+    }
+};
+
 // The products of a workgroup's tiles, one after the other.  next() aims at the next tile to load (aim), or does nothing where there is none.
 template <class T, class S, int STEP, int STAGES, bool A_ALONG, bool B_ALONG, bool PAIRS = false>
 struct Flow {
@@ -164,7 +197,9 @@ struct Flow {
     static_assert(B_ALONG || !(S::NEXT || PAIRS), "rows of a tile that lies across stay in order");
     static_assert(!PAIRS || S::NT % 2 == 0, "a wavefront's columns are as many of each half");
     static constexpr int STAGE = A::BYTES + B::BYTES, BYTES = STAGES * STAGE;
-    static constexpr int KK = STEP / 32, DEPTH = A::DEPTH;
+    static constexpr int GROUP = sizeof(T) == 4 ? 2 : 1;  // times 32 bytes of the sum's axis that go to the matrix core at once
+    static constexpr int GROUPS = STEP / 32 / GROUP, DEPTH = A::DEPTH;
+    static_assert(GROUPS % 2 == 0, "a step begins in the same registers");
     static constexpr int LATER = (STAGES - 2) * (A::LOADS + B::LOADS);  // loads behind those of the next stage
 
     const Operand<T> &a, &b;
@@ -173,7 +208,7 @@ struct Flow {
     B tb;
     int steps = 0;  // left to load of the tile that is aimed at
     int stage = 0;  // where the step is that the matrix core is at
-    Chunk x[2][S::MT], y[2][S::NT];
+    Chunk x[2][GROUP][S::MT], y[2][GROUP][S::NT];
 
     __device__ __forceinline__ Flow(const Operand<T> &a_, const Operand<T> &b_, char *lds_) : a(a_), b(b_), lds(lds_)
     {
@@ -201,13 +236,91 @@ struct Flow {
         --steps;
     }
 
-    __device__ __forceinline__ void read(int kk)
+    __device__ __forceinline__ void read(int g)
     {
         const char *at = lds + stage * STAGE;
 #pragma unroll
-        for (int mt = 0; mt < S::MT; ++mt) x[kk % 2][mt] = ta.read(at, mt, kk);
+        for (int k = 0; k < GROUP; ++k) {
 #pragma unroll
-        for (int nt = 0; nt < S::NT; ++nt) y[kk % 2][nt] = tb.read(at + A::BYTES, nt, kk);
+            for (int mt = 0; mt < S::MT; ++mt) x[g % 2][k][mt] = ta.read(at, mt, g * GROUP + k);
+#pragma unroll
+            for (int nt = 0; nt < S::NT; ++nt) y[g % 2][k][nt] = tb.read(at + A::BYTES, nt, g * GROUP + k);
+        }
+    }
+
+    __device__ __forceinline__ void multiply_group(Acc (&c)[S::MT][S::NT], int g)
+    {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < S::NT; ++nt) multiply(x[g % 2][0][mt], y[g % 2][0][nt], c[mt][nt], bf16());
+        } else {
+            Chunk high[S::NT], middle[S::NT], low[S::NT];
+#pragma unroll
+            for (int nt = 0; nt < S::NT; ++nt) {
+                const Parts p(y[g % 2][0][nt], y[g % 2][1][nt]);
+                high[nt] = p.high, middle[nt] = p.middle, low[nt] = p.low;
+            }
+#pragma unroll
+            for (int mt = 0; mt < S::MT; ++mt) {
+                const Parts p(x[g % 2][0][mt], x[g % 2][1][mt]);
+                auto add = [&](const Chunk &a, const Chunk (&b)[S::NT]) {
+#pragma unroll
+                    for (int nt = 0; nt < S::NT; ++nt) multiply(a, b[nt], c[mt][nt], bf16());
+                };
+                add(p.low, high);
+                add(p.high, low);
+                add(p.middle, middle);
+                add(p.middle, high);
+                add(p.high, middle);
+                add(p.high, high);
+            }
+        }
+    }
+
+    // float32 sums that are not finite, by float32 instructions, straight from memory.  Others stay as they are, whatever is in other rows.
+    __device__ __forceinline__ void again(Acc (&c)[S::MT][S::NT], int64_t row0, int64_t column0, int64_t from, int64_t to) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            float none = 0;  // or NaN
+#pragma unroll
+            for (int mt = 0; mt < S::MT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < S::NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) none = fmaf(c[mt][nt][i], 0.0f, none);
+            if (!__any(none != none)) return;
+            const int lane = threadIdx.x % 32, later = threadIdx.x % 64 / 32;
+            const T *pb[S::NT];
+#pragma unroll
+            for (int nt = 0; nt < S::NT; ++nt) {
+                const int64_t wave0 = S::wave_n() * (S::NT * 32);
+                int64_t row;
+                if constexpr (PAIRS) row = nt % 2 * (b.rows / 2) + std::min<int64_t>((column0 + wave0) / 2 + lane * (S::NT / 2) + nt / 2, b.rows / 2 - 1);
+                else row = std::min<int64_t>(column0 + wave0 + (S::NEXT ? lane * S::NT + nt : nt * 32 + lane), b.rows - 1);
+                pb[nt] = b.at + row * (B_ALONG ? b.stride : 1);
+            }
+#pragma unroll
+            for (int mt = 0; mt < S::MT; ++mt) {
+                const int64_t row = std::min<int64_t>(row0 + S::wave_m() * (S::MT * 32) + mt * 32 + lane, a.rows - 1);
+                const T *pa = a.at + row * (A_ALONG ? a.stride : 1);
+                Acc d[S::NT];
+#pragma unroll
+                for (int nt = 0; nt < S::NT; ++nt) d[nt] = Acc{};
+                for (int64_t k0 = from; k0 < to; k0 += 2) {
+                    const int64_t k = k0 + later;
+                    const float u = k < to ? pa[k * (A_ALONG ? 1 : a.stride)] : 0.0f;
+#pragma unroll
+                    for (int nt = 0; nt < S::NT; ++nt)
+                        d[nt] = __builtin_amdgcn_mfma_f32_32x32x2f32(u, k < to ? pb[nt][k * (B_ALONG ? 1 : b.stride)] : 0.0f, d[nt], 0, 0, 0);
+                }
+#pragma unroll
+                for (int nt = 0; nt < S::NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) c[mt][nt][i] = fabsf(c[mt][nt][i]) < INFINITY ? c[mt][nt][i] : d[nt][i];
+            }
+        }
     }
 
     // The next stage is there, for all wavefronts, and nobody reads what they have read any more.
@@ -241,19 +354,16 @@ struct Flow {
             for (int nt = 0; nt < S::NT; ++nt) c[mt][nt] = Acc{};
         for (; count > 0; --count) {
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                if (kk + 1 < KK) {
-                    read(kk + 1);
+            for (int g = 0; g < GROUPS; ++g) {
+                if (g + 1 < GROUPS) {
+                    read(g + 1);
                 } else {
                     meet();
                     load(stage, next);
                     stage = stage + 1 < STAGES ? stage + 1 : 0;
                     read(0);
                 }
-#pragma unroll
-                for (int mt = 0; mt < S::MT; ++mt)
-#pragma unroll
-                    for (int nt = 0; nt < S::NT; ++nt) multiply(x[kk % 2][mt], y[kk % 2][nt], c[mt][nt], T());
+                multiply_group(c, g);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }

@@ -119,6 +119,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void layer_kernel(Operand<T> x, Oper
         const int64_t column0 = int64_t{S::N} * column_tile, row0 = int64_t{S::M} * row_tile;
         Acc c[S::MT][S::NT];
         flow.run(c, flow.steps_of(0, x.depth), next);
+        flow.again(c, row0, column0, 0, x.depth);
         float bias[S::NT] = {};
         if (e.bias) {
 #pragma unroll
@@ -274,7 +275,9 @@ __global__ __launch_bounds__(S::THREADS, 2) void sum_kernel(Operand<T> a, Operan
         int64_t row0, column0, split;
         place(tile, row0, column0, split);
         Acc c[S::MT][S::NT];
-        flow.run(c, flow.steps_of(split * split_depth, std::min(a.depth, (split + 1) * split_depth)), next);
+        const int64_t from = split * split_depth, to = std::min(a.depth, from + split_depth);
+        flow.run(c, flow.steps_of(from, to), next);
+        flow.again(c, row0, column0, from, to);
         const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
         const int64_t at = (row0 + S::row(0, 0)) * columns + column0 + S::column(0);
         auto each = [&](auto store) {
