@@ -1,7 +1,7 @@
 // The products of head_linear.hip, on gfx950: the shapes and the layout in LDS of head_product.hpp, with the matrix core fed across the steps of
 // the sum and across tiles.
 //
-// A step's tiles of A and B are loaded STAGES steps ahead, into the stage of LDS that a step has just left.  A wavefront reads the next 32
+// A step's tiles of A and B are loaded two steps ahead, into the half of LDS that a step has just left.  A wavefront reads the next 32
 // bytes of the sum's axis while the matrix core works on the last ones, over the end of a step too: the barrier, the loads that it
 // lets go and the next step's first reads come before a step's last instructions of the matrix core, so that it has work meanwhile.
 //
@@ -11,7 +11,7 @@
 // instructions for two values.  bfloat16 has nothing below 2^-133, so values below 2^-109 lose bits.  Infinite values, and the few that round to
 // one, have no such parts: a sum that is not finite in the end is made again, with float32 instructions (again).
 //
-// Loads go through buffer descriptors, whose bounds give zeros past the last row and past the end of a sum that lies across memory, and by which a
+// Loads go through buffer descriptors, of 16 bytes that begin at any word of 4, whose bounds give zeros past the last row and past the end of a sum that lies across memory, and by which a
 // lane has one 32-bit offset for all its loads of an operand.
 #pragma once
 
@@ -23,7 +23,7 @@ namespace {
 constexpr int64_t FLOW_STRIDE = (1 << 21) + 256;  // bytes of a row's step, at most: offsets in a tile, of up to 256 rows, stay far below 2^31
 
 // Tiles of ROWS x 128 bytes of an operand: layout in LDS and meaning of the parameters as in Tile.
-template <class T, int STEP, bool ALONG, int ROWS, int THREADS, int NT, bool PAIRS, int FRAGMENTS>
+template <class T, bool ALONG, int ROWS, int THREADS, int NT, bool PAIRS, int FRAGMENTS>
 struct FlowTile {
     static constexpr int VALUES = 16 / sizeof(T), DEPTH = STEP / sizeof(T), BYTES = ROWS * STEP, LOADS = BYTES / (THREADS * 16), WAVES = THREADS / 64;
     static constexpr int SLOTS = ALONG ? STEP / 16 : ROWS / VALUES;  // chunks of a row of the tile
@@ -88,7 +88,7 @@ struct FlowTile {
         const int64_t row_bytes = o.stride * static_cast<int64_t>(sizeof(T));
         left = o.depth - from;
         if constexpr (ALONG) {
-            const int64_t end = round_to_chunk(o.depth) * static_cast<int64_t>(sizeof(T));  // of a row
+            const int64_t end = whole_words(o.depth);  // of a row
             const int64_t rows = PAIRS ? o.rows / 2 : o.rows, first = PAIRS ? row0 / 2 : row0;
             base = reinterpret_cast<const char *>(o.at + from) + first * row_bytes;
             bytes = (rows - 1 - first) * row_bytes + end - from * static_cast<int64_t>(sizeof(T));
@@ -98,10 +98,27 @@ struct FlowTile {
             }
         } else {
             base = reinterpret_cast<const char *>(o.at + row0) + from * row_bytes;
-            bytes = (left - 1) * row_bytes + (round_to_chunk(o.rows) - row0) * static_cast<int64_t>(sizeof(T));
+            bytes = (left - 1) * row_bytes + whole_words(o.rows) - row0 * static_cast<int64_t>(sizeof(T));
         }
     }
-    static __device__ __forceinline__ int64_t round_to_chunk(int64_t n) { return (n + VALUES - 1) / VALUES * VALUES; }
+    // Bytes of n values, in the words of 4 by which bounds are checked.
+    static __device__ __forceinline__ int64_t whole_words(int64_t n) { return (n * static_cast<int64_t>(sizeof(T)) + 3) / 4 * 4; }
+
+    // Values that the last step loaded has of the sum, where they end inside a chunk; else 0.
+    __device__ __forceinline__ int torn() const { return ALONG && left < 0 && left % VALUES ? static_cast<int>(left + DEPTH) : 0; }
+
+    // Zeros in what this lane loaded of such a step from behind the sum's end, which are other values of the operand.
+    __device__ __forceinline__ void mend(char *lds, int there) const
+    {
+        if (lane_at >= there || lane_at + VALUES <= there) return;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            T *chunk = reinterpret_cast<T *>(lds + (j * WAVES + static_cast<int>(threadIdx.x / 64)) * 1024 + threadIdx.x % 64 * 16);
+#pragma unroll
+            for (int k = 1; k < VALUES; ++k)
+                if (lane_at + k >= there) chunk[k] = T(0);
+        }
+    }
 
     // The step that base is at, to LDS, and on to the next one.
     __device__ __forceinline__ void load(const Operand<T> &o, char *lds)
@@ -190,17 +207,16 @@ struct Parts {
 };
 
 // The products of a workgroup's tiles, one after the other.  next() aims at the next tile to load (aim), or does nothing where there is none.
-template <class T, class S, int STEP, int STAGES, bool A_ALONG, bool B_ALONG, bool PAIRS = false>
+template <class T, class S, bool A_ALONG, bool B_ALONG, bool PAIRS = false>
 struct Flow {
-    using A = FlowTile<T, STEP, A_ALONG, S::M, S::THREADS, 1, false, S::MT>;
-    using B = FlowTile<T, STEP, B_ALONG, S::N, S::THREADS, S::NEXT || PAIRS ? S::NT : 1, PAIRS, S::NT>;
+    using A = FlowTile<T, A_ALONG, S::M, S::THREADS, 1, false, S::MT>;
+    using B = FlowTile<T, B_ALONG, S::N, S::THREADS, S::NEXT || PAIRS ? S::NT : 1, PAIRS, S::NT>;
     static_assert(B_ALONG || !(S::NEXT || PAIRS), "rows of a tile that lies across stay in order");
     static_assert(!PAIRS || S::NT % 2 == 0, "a wavefront's columns are as many of each half");
-    static constexpr int STAGE = A::BYTES + B::BYTES, BYTES = STAGES * STAGE;
+    static constexpr int STAGE = A::BYTES + B::BYTES;  // of LDS, which holds two
     static constexpr int GROUP = sizeof(T) == 4 ? 2 : 1;  // times 32 bytes of the sum's axis that go to the matrix core at once
     static constexpr int GROUPS = STEP / 32 / GROUP, DEPTH = A::DEPTH;
     static_assert(GROUPS % 2 == 0, "a step begins in the same registers");
-    static constexpr int LATER = (STAGES - 2) * (A::LOADS + B::LOADS);  // loads behind those of the next stage
 
     const Operand<T> &a, &b;
     char *lds;
@@ -234,6 +250,14 @@ struct Flow {
         ta.load(a, lds + to * STAGE);
         tb.load(b, lds + to * STAGE + A::BYTES);
         --steps;
+    }
+
+    // Once the loads of stage `s`, a tile's last ones and those of ta and tb before now, are there.
+    __device__ __forceinline__ void mend(int s) const
+    {
+        if (ta.torn()) ta.mend(lds + s * STAGE, ta.torn());
+        if (tb.torn()) tb.mend(lds + s * STAGE + A::BYTES, tb.torn());
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 
     __device__ __forceinline__ void read(int g)
@@ -324,10 +348,10 @@ struct Flow {
     }
 
     // The next stage is there, for all wavefronts, and nobody reads what they have read any more.
-    __device__ __forceinline__ void meet() const
+    __device__ __forceinline__ void meet()
     {
-        if (steps == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // at the end there are no later loads
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (steps == 0) mend(stage ^ 1);  // a tile's last step was loaded last
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     }
@@ -336,9 +360,14 @@ struct Flow {
     template <class Next>
     __device__ __forceinline__ void begin(Next next)
     {
-#pragma unroll
-        for (int s = 0; s < STAGES; ++s) load(s, next);
+        load(0, next);
+        const int torn_a = ta.torn(), torn_b = tb.torn();
+        load(1, next);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (torn_a) ta.mend(lds, torn_a);
+        if (torn_b) tb.mend(lds + A::BYTES, torn_b);
+        if (steps == 0) mend(1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         read(0);
@@ -360,7 +389,7 @@ struct Flow {
                 } else {
                     meet();
                     load(stage, next);
-                    stage = stage + 1 < STAGES ? stage + 1 : 0;
+                    stage ^= 1;
                     read(0);
                 }
                 multiply_group(c, g);

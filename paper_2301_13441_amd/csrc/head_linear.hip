@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -102,7 +103,7 @@ template <class T, class S, bool GATED>
 __global__ __launch_bounds__(S::THREADS, 2) void layer_kernel(Operand<T> x, Operand<T> weight, End<T> e, uint32_t row_tiles, uint32_t column_tiles)
 {
     extern __shared__ char lds[];
-    Flow<T, S, STEP, 2, true, true, GATED> flow(x, weight, lds);
+    Flow<T, S, true, true, GATED> flow(x, weight, lds);
     const uint32_t tiles = row_tiles * column_tiles;
     uint32_t ahead = blockIdx.x;
     auto next = [&] {
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *parts, int64_t
 // ---- backward
 
 // dz of `rows` rows from row `rows` * blockIdx.y on, `stride` apart, and parts [gridDim.y][columns] of the sums of its columns, either if
-// wanted; zeros behind its columns up to `padded`.  `scale` is only that of the sums.
+// wanted.  `scale` is only that of the sums.
 template <class T>
 struct Slopes {
     int32_t activation;
@@ -175,7 +176,7 @@ struct Slopes {
     int64_t z_stride, grad_stride;
     int64_t n_rows, outs, rows;
     T *dz;
-    int64_t stride, padded;
+    int64_t stride;
     float scale;
     float *parts;
 };
@@ -227,8 +228,6 @@ __global__ __launch_bounds__(256) void slope_kernel(Slopes<T> s)
             }
         });
     }
-    if (N == 1 && s.dz && column < s.padded - columns)  // whole vectors have nothing behind them
-        for (int64_t row = row0 + y; row < end; row += HIGH) s.dz[row * s.stride + columns + column] = T(0);
     if (!s.parts) return;
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void sum_kernel(Operand<T> a, Operan
 {
     static_assert(!S::NEXT, "a lane's columns are 32 apart");
     extern __shared__ char lds[];
-    Flow<T, S, STEP, 2, A_ALONG, B_ALONG> flow(a, b, lds);
+    Flow<T, S, A_ALONG, B_ALONG> flow(a, b, lds);
     const uint32_t tiles = row_tiles * column_tiles * splits;
     uint32_t ahead = blockIdx.x;
     auto place = [&](uint32_t tile, int64_t &row0, int64_t &column0, int64_t &split) {
@@ -328,22 +327,37 @@ struct Cut {
     int64_t tiles() const { return row_tiles * column_tiles * splits; }
 };
 
+// What a product of that cut takes, in us, from times of sum_kernel and of the kernels that add parts over 20 shapes from 100 x 64 x 4096 to
+// 8192 x 2048 x 2048.  A workgroup's step takes longer where a CU has two of them, and a tile's end is its results' way to memory; a launch takes
+// 2.2; parts go to memory and back at 4.6 TB/s, in a launch of their own.  On those shapes the cut that this chooses is within 8 % of the fastest
+// one of all.
+double time_of(int32_t dtype, const Cut &c, int64_t rows, int64_t columns, int64_t depth)
+{
+    struct { double step, steps, end; } static const TIMES[2][3] = {{{0.73, 1.1, 2.0}, {1.54, 2.4, 4.0}, {9, 9, 9}}, {{0.39, 0.56, 1.4}, {0.62, 0.84, 3.5}, {1.4, 1.4, 7.4}}};
+    const auto &t = TIMES[dtype == HEAD_BF16][c.size];
+    const double step = STEP / value_bytes(dtype), steps = std::ceil(std::min(depth, c.split_depth) / step);
+    const double rounds = std::ceil(c.tiles() / (c.size == LARGE ? 256.0 : 512.0));
+    const double us = 2.2 + rounds * (steps * (c.tiles() > 256 ? t.steps : t.step) + t.end);
+    return c.splits > 1 ? us + 2.5 + static_cast<double>(c.splits) * rows * columns * 8 / 4.6e6 : us;
+}
+
 Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, bool gated = false)
 {
     const int64_t step = STEP / value_bytes(dtype);
-    auto tiles = [&](int64_t tile) { return ceil_div(rows, tile) * ceil_div(columns, tile); };
-    Cut c{};
-    const int64_t most = std::max<int64_t>(1, depth / (16 * step));  // parts of a large tile's sum that are long enough
-    if (dtype == HEAD_BF16 && std::min(rows, columns) > 128 && tiles(Large::TILE) * std::min<int64_t>(most, 4) >= Large::RESIDENT) c.size = LARGE;
-    else if (std::min(rows, columns) > 64 && tiles(Small::TILE) >= Small::RESIDENT / 2) c.size = SMALL;
-    else c.size = TINY;
-    const int64_t tile = c.size == LARGE ? 256 : c.size == SMALL ? 128 : 64, resident = c.size == LARGE ? 256 : 512;
-    c.row_tiles = ceil_div(rows, tile);
-    c.column_tiles = ceil_div(columns, gated && c.size == TINY ? 128 : tile);
-    c.splits = splits_of(c.row_tiles * c.column_tiles, resident, depth, step);
-    c.split_depth = round_up(ceil_div(depth, c.splits), step);
-    c.splits = std::max<int64_t>(1, ceil_div(depth, c.split_depth));
-    return c;
+    Cut best{};
+    double least = INFINITY;
+    for (int size = TINY; size <= (dtype == HEAD_BF16 ? LARGE : SMALL); ++size) {
+        const int64_t tile = 64 << size;
+        Cut c{size, ceil_div(rows, tile), ceil_div(columns, gated && size == TINY ? 128 : tile), 1, round_up(depth, step)};
+        for (int64_t splits = 1; splits <= 256; splits = splits & (splits - 1) ? splits / 3 * 4 : std::max(splits + 1, splits / 2 * 3)) {  // 1, 2, 3, 4, 6, 8, 12, ..
+            c.split_depth = round_up(ceil_div(depth, splits), step);
+            c.splits = std::max<int64_t>(1, ceil_div(depth, c.split_depth));
+            if (c.splits > 1 && (c.splits * rows * columns > int64_t{1} << 26 || c.tiles() > 1024)) break;
+            const double us = time_of(dtype, c, rows, columns, depth);
+            if (us < least) least = us, best = c;
+        }
+    }
+    return best;
 }
 
 // The parts of a call's workspace, in bytes from its start.
@@ -362,22 +376,29 @@ struct Plan : Space {
     int64_t x = -1, weight = -1;     // packed operands; -1: used where they are
     Cut forward, to_x, to_weight;
     int64_t parts = -1, weight_parts = -1;
-    int64_t stride, padded;          // values of a row of dz, and how many are zero or its own
+    int64_t stride;                  // values of a row of dz
     int64_t dz = -1, bias_rows, bias_chunks, bias_parts = -1;
 };
 
 bool whole(int32_t dtype, const void *at, int64_t stride, int64_t n)
 {
     const int e = value_bytes(dtype);
-    return stride * e <= FLOW_STRIDE && (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(n * e)) % 16 == 0;
+    return (address(at) | static_cast<uint64_t>(stride * e) | static_cast<uint64_t>(n * e)) % 16 == 0;
+}
+
+// Whether products read an operand where it is: rows begin at words of 4 bytes, not too far apart.
+bool readable(int32_t dtype, const void *at, int64_t stride)
+{
+    const int64_t bytes = stride * value_bytes(dtype);
+    return bytes <= FLOW_STRIDE && (address(at) | static_cast<uint64_t>(bytes)) % 4 == 0;
 }
 
 void plan_operands(const head_layer &l, int64_t columns, Plan &p)
 {
     const int e = value_bytes(l.dtype);
     p.packed = round_up(l.dim, 16 / e);
-    if (!whole(l.dtype, l.x, l.x_stride, l.dim)) p.x = p.part(l.n_rows * p.packed * e);
-    if (!whole(l.dtype, l.weight, l.weight_stride, l.dim)) p.weight = p.part(columns * p.packed * e);
+    if (!readable(l.dtype, l.x, l.x_stride)) p.x = p.part(l.n_rows * p.packed * e);
+    if (!readable(l.dtype, l.weight, l.weight_stride)) p.weight = p.part(columns * p.packed * e);
 }
 
 Plan plan_forward(const head_layer &l, bool gated)
@@ -399,8 +420,7 @@ Plan plan_backward(const head_layer &l, bool gated)
     if (l.n_rows == 0) return p;
     plan_operands(l, columns, p);
     // Rows a power of two apart would lie in few of the memory's channels: a row more than its values by 256 bytes goes through all.
-    p.padded = round_up(columns, 16 / e);
-    p.stride = p.padded + 256 / e;
+    p.stride = round_up(columns, 16 / e) + 256 / e;
     p.dz = p.part(l.n_rows * p.stride * e);
     p.bias_chunks = std::min<int64_t>(ceil_div(l.n_rows, 16), std::min<int64_t>(8192, std::max<int64_t>(1, (int64_t{1} << 20) / columns)));
     p.bias_rows = ceil_div(l.n_rows, p.bias_chunks);
@@ -439,7 +459,7 @@ Operand<T> operand(const void *at, int64_t stride, int64_t rows, int64_t dim, in
     if (packed_at < 0) return Operand<T>{from, stride, rows, dim};
     T *to = reinterpret_cast<T *>(workspace + packed_at);
     hipLaunchKernelGGL((pack_kernel<T>), grid_of(ceil_div(rows * packed, 256)), dim3(256), 0, stream, from, stride, rows, dim, to, packed);
-    return Operand<T>{to, packed, rows, packed};
+    return Operand<T>{to, packed, rows, dim};
 }
 
 template <class T, bool A_ALONG, bool B_ALONG>
@@ -524,12 +544,12 @@ hipError_t backward(const head_layer &l, const void *z, int64_t z_stride, const 
     const Operand<T> weight = operand<T>(l.weight, l.weight_stride, columns, l.dim, p.packed, p.weight, workspace, stream);
     // Without an activation dz is grad itself, where products can read it.
     const bool reads = GATED || l.activation != HEAD_IDENTITY;
-    const bool makes = reads || !whole(l.dtype, grad, grad_stride, l.n_outputs);
+    const bool makes = reads || !readable(l.dtype, grad, grad_stride);
     const T *dz = static_cast<const T *>(grad);
     int64_t stride = grad_stride;
     if (makes || grad_bias) {
         Slopes<T> s{l.activation, static_cast<const T *>(z), dz, z_stride, grad_stride, l.n_rows, l.n_outputs, p.bias_rows,
-                    makes ? reinterpret_cast<T *>(workspace + p.dz) : nullptr, p.stride, p.padded, scale,
+                    makes ? reinterpret_cast<T *>(workspace + p.dz) : nullptr, p.stride, scale,
                     grad_bias ? reinterpret_cast<float *>(workspace + p.bias_parts) : nullptr};
         const bool wide = whole(l.dtype, grad, grad_stride, l.n_outputs) && (!reads || whole(l.dtype, z, z_stride, l.n_outputs));
         launch_slopes<T, GATED>(s, p.bias_chunks, wide, stream);
@@ -539,7 +559,6 @@ hipError_t backward(const head_layer &l, const void *z, int64_t z_stride, const 
     if (const hipError_t e = hipGetLastError()) return e;
     float *parts = p.parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + p.parts);
     float *weight_parts = p.weight_parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + p.weight_parts);
-    // The sum over dz's columns goes by whole vectors: behind them are zeros, and zeros are taken for the weights that would be there.
     if (const hipError_t e = launch_sum<T, true, false>(p.to_x, Operand<T>{dz, stride, l.n_rows, columns}, Operand<T>{weight.at, weight.stride, weight.depth, columns},
                                                         l.dim, scale, parts, parts ? nullptr : to_x, stream))
         return e;
