@@ -318,6 +318,10 @@ struct LinearOf { using Type = typename Size::template Of<true>; };
 template <>
 struct LinearOf<Large> { using Type = Shape<256, 256, 4, 2, true>; };
 
+// Workgroups of a launch: as many as the device holds at a time.
+template <class Size>
+constexpr int64_t resident_of() { return std::is_same_v<Size, Tiny> ? 1024 : Size::RESIDENT; }
+
 enum { TINY, SMALL, LARGE };
 
 // How a product [rows][columns] over `depth` is cut.
@@ -327,17 +331,18 @@ struct Cut {
     int64_t tiles() const { return row_tiles * column_tiles * splits; }
 };
 
-// What a product of that cut takes, in us, from times of sum_kernel and of the kernels that add parts over 20 shapes from 100 x 64 x 4096 to
-// 8192 x 2048 x 2048.  A workgroup's step takes longer where a CU has two of them, and a tile's end is its results' way to memory; a launch takes
-// 2.2; parts go to memory and back at 4.6 TB/s, in a launch of their own.  On those shapes the cut that this chooses is within 8 % of the fastest
-// one of all.
+// What a product of that cut takes, in us, from times of sum_kernel and of the kernels that add parts over 26 shapes from 100 x 64 x 4096 to
+// 8192 x 1024 x 16384.  A workgroup's step takes `more` longer for each other workgroup that its CU has, and a tile's end is its results' way to
+// memory; a launch takes 2.2; parts go to memory and back at 4.6 TB/s, in a launch of their own.  On those shapes the cut that this chooses is within
+// 15 % of the fastest one of all.
 double time_of(int32_t dtype, const Cut &c, int64_t rows, int64_t columns, int64_t depth)
 {
-    struct { double step, steps, end; } static const TIMES[2][3] = {{{0.73, 1.1, 2.0}, {1.54, 2.4, 4.0}, {9, 9, 9}}, {{0.39, 0.56, 1.4}, {0.62, 0.84, 3.5}, {1.4, 1.4, 7.4}}};
+    struct { double step, more, end; } static const TIMES[2][3] = {{{0.73, 0.5, 2.0}, {1.54, 1.26, 4.0}, {}}, {{0.39, 0.157, 1.4}, {0.62, 0.33, 3.5}, {1.4, 0, 7.4}}};
     const auto &t = TIMES[dtype == HEAD_BF16][c.size];
     const double step = STEP / value_bytes(dtype), steps = std::ceil(std::min(depth, c.split_depth) / step);
-    const double rounds = std::ceil(c.tiles() / (c.size == LARGE ? 256.0 : 512.0));
-    const double us = 2.2 + rounds * (steps * (c.tiles() > 256 ? t.steps : t.step) + t.end);
+    const double resident = c.size == TINY ? resident_of<Tiny>() : c.size == SMALL ? resident_of<Small>() : resident_of<Large>();
+    const double tiles = c.tiles(), others = std::ceil(std::min(tiles, resident) / 256) - 1;
+    const double us = 2.2 + std::ceil(tiles / resident) * (steps * (t.step + t.more * others) + t.end);
     return c.splits > 1 ? us + 2.5 + static_cast<double>(c.splits) * rows * columns * 8 / 4.6e6 : us;
 }
 
@@ -352,7 +357,7 @@ Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, bool gat
         for (int64_t splits = 1; splits <= 256; splits = splits & (splits - 1) ? splits / 3 * 4 : std::max(splits + 1, splits / 2 * 3)) {  // 1, 2, 3, 4, 6, 8, 12, ..
             c.split_depth = round_up(ceil_div(depth, splits), step);
             c.splits = std::max<int64_t>(1, ceil_div(depth, c.split_depth));
-            if (c.splits > 1 && (c.splits * rows * columns > int64_t{1} << 26 || c.tiles() > 1024)) break;
+            if (c.splits > 1 && (c.splits * rows * columns > int64_t{1} << 26 || c.tiles() > 2048)) break;
             const double us = time_of(dtype, c, rows, columns, depth);
             if (us < least) least = us, best = c;
         }
@@ -468,7 +473,7 @@ hipError_t launch_sum(const Cut &c, const Operand<T> &a, const Operand<T> &b, in
     return with_size<T>(c.size, [&](auto size) {
         using Size = decltype(size);
         using S = typename Size::template Of<false>;
-        return launch_tiles<S, sum_kernel<T, S, A_ALONG, B_ALONG>>(c.tiles(), Size::RESIDENT, stream, a, b, columns, static_cast<uint32_t>(c.row_tiles),
+        return launch_tiles<S, sum_kernel<T, S, A_ALONG, B_ALONG>>(c.tiles(), resident_of<Size>(), stream, a, b, columns, static_cast<uint32_t>(c.row_tiles),
                                                                    static_cast<uint32_t>(c.column_tiles), static_cast<uint32_t>(c.splits), c.split_depth,
                                                                    scale, parts, out);
     });
@@ -503,7 +508,7 @@ hipError_t forward(const head_layer &l, const void *residual, int64_t residual_s
         using Size = decltype(size);
         using S = typename std::conditional_t<GATED, GatedOf<Size>, LinearOf<Size>>::Type;
         end.wide = rows_whole((GATED ? S::NT / 2 : S::NT) * static_cast<int>(sizeof(T)));
-        return launch_tiles<S, layer_kernel<T, S, GATED>>(c.tiles(), Size::RESIDENT, stream, x, weight, end, static_cast<uint32_t>(c.row_tiles),
+        return launch_tiles<S, layer_kernel<T, S, GATED>>(c.tiles(), resident_of<Size>(), stream, x, weight, end, static_cast<uint32_t>(c.row_tiles),
                                                           static_cast<uint32_t>(c.column_tiles));
     });
 }
