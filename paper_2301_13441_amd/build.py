@@ -78,7 +78,7 @@ def _build_extension(src: str, out: str, verbose: bool) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{d}" for d in include),
            os.path.join(CSRC, src), "-o", out, "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
-           "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+           "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)

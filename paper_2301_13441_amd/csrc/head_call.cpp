@@ -8,9 +8,11 @@
 // checks raise the errors; an entry point's error code is returned as an int.
 #include <Python.h>
 
+#include <ATen/EmptyTensor.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
@@ -88,6 +90,13 @@ bool fits(const at::Tensor *t, const at::Tensor &like, at::ScalarType type, at::
 }
 
 void *stream_of(const at::Tensor &like) { return c10::hip::getCurrentHIPStream(like.get_device()).stream(); }
+
+// A new contiguous tensor of the current device, as at::empty makes it, without the dispatcher's half microsecond.
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type)
+{
+    return at::Tensor(at::detail::empty_generic(sizes, c10::hip::HIPCachingAllocatorMasqueradingAsCUDA::get(),
+                                                c10::DispatchKeySet(c10::DispatchKey::CUDA), type, c10::nullopt));
+}
 
 at::Tensor workspace(int64_t bytes, const at::Tensor &like) { return at::empty({bytes}, like.options().dtype(at::kByte)); }
 
@@ -332,8 +341,8 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (keep < 0) return nullptr;
     const int64_t bytes = entry.linear_bytes(&l);
     if (bytes < 0) return PyLong_FromLongLong(bytes);
-    const at::Tensor y = at::empty({l.n_rows, l.n_outputs}, x->options()), z = keep ? at::empty({l.n_rows, l.n_outputs}, x->options()) : at::Tensor(),
-                     work = bytes ? workspace(bytes, *x) : at::Tensor();
+    const at::Tensor y = fresh({l.n_rows, l.n_outputs}, x->scalar_type()), z = keep ? fresh({l.n_rows, l.n_outputs}, x->scalar_type()) : at::Tensor(),
+                     work = bytes ? fresh({bytes}, at::kByte) : at::Tensor();
     const void *from = residual ? residual->data_ptr() : nullptr;
     void *to = y.data_ptr(), *to_z = data_of(z), *space = data_of(work), *stream = stream_of(*x);
     const int rc =
@@ -353,8 +362,8 @@ PyObject *gated(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (keep < 0) return nullptr;
     const int64_t bytes = entry.gated_bytes(&l);
     if (bytes < 0) return PyLong_FromLongLong(bytes);
-    const at::Tensor y = at::empty({l.n_rows, l.n_outputs}, x->options()),
-                     z = keep ? at::empty({l.n_rows, 2 * l.n_outputs}, x->options()) : at::Tensor(), work = bytes ? workspace(bytes, *x) : at::Tensor();
+    const at::Tensor y = fresh({l.n_rows, l.n_outputs}, x->scalar_type()),
+                     z = keep ? fresh({l.n_rows, 2 * l.n_outputs}, x->scalar_type()) : at::Tensor(), work = bytes ? fresh({bytes}, at::kByte) : at::Tensor();
     void *to = y.data_ptr(), *to_z = data_of(z), *space = data_of(work), *stream = stream_of(*x);
     const int rc = without_gil([&] { return entry.gated(&l, to, to_z, space, stream); });
     return results(rc, y, z);
@@ -372,9 +381,9 @@ PyObject *layer_grad(PyObject *grad_object, PyObject *z_object, PyObject *bias_o
     if (!fits(grad, x, x.scalar_type(), {l.n_rows, l.n_outputs})) return declined();
     if (z_object != Py_None ? !fits(z, x, x.scalar_type(), {l.n_rows, weight.size(0)}) : reads_z) return declined();
     if (bytes < 0) return PyLong_FromLongLong(bytes);
-    const at::Tensor gx = at::empty({l.n_rows, l.dim}, x.options()), gw = at::empty({weight.size(0), l.dim}, x.options()),
-                     gb = bias ? at::empty({weight.size(0)}, x.options().dtype(at::kFloat)) : at::Tensor(),
-                     work = bytes ? workspace(bytes, x) : at::Tensor();
+    const at::Tensor gx = fresh({l.n_rows, l.dim}, x.scalar_type()), gw = fresh({weight.size(0), l.dim}, x.scalar_type()),
+                     gb = bias ? fresh({weight.size(0)}, at::kFloat) : at::Tensor(),
+                     work = bytes ? fresh({bytes}, at::kByte) : at::Tensor();
     const void *from_z = z ? z->data_ptr() : nullptr, *from = grad->data_ptr();
     void *to_x = gx.data_ptr(), *to_weight = gw.data_ptr(), *space = data_of(work), *stream = stream_of(x);
     float *to_bias = static_cast<float *>(data_of(gb));
@@ -570,15 +579,15 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     }
     const int64_t bytes = entry.clip_bytes(tensors.data(), static_cast<int32_t>(n));
     if (bytes < 0) return PyLong_FromLongLong(bytes);
-    const at::Tensor norm = at::empty({}, first->options().dtype(at::kFloat)), work = workspace(bytes, *first);
+    const at::Tensor norm = fresh({}, at::kFloat), work = bytes ? fresh({bytes}, at::kByte) : at::Tensor();
     for (Py_ssize_t i = 0; i < n; ++i) {
         const at::Tensor &t = THPVariable_Unpack(PyList_GET_ITEM(args[0], i));
         if (in_place) written(PyList_GET_ITEM(args[0], i));
-        out[i] = in_place ? t : at::empty(t.sizes(), t.options());
+        out[i] = in_place ? t : fresh(t.sizes(), t.scalar_type());
         tensors[i].out = out[i].data_ptr();
     }
     float *to = static_cast<float *>(norm.data_ptr());
-    void *space = work.data_ptr(), *stream = stream_of(*first);
+    void *space = data_of(work), *stream = stream_of(*first);
     const int rc = without_gil([&] { return entry.clip(tensors.data(), static_cast<int32_t>(n), max_norm, to, space, stream); });
     if (rc) return PyLong_FromLong(rc);
     PyObject *list = PyList_New(n);

@@ -126,7 +126,9 @@ def test_layers_refuse_bad_arguments_before_any_device_call():
     for f in (linear_grad, gated_grad):
         assert f(_layer(outs=262_145)) == -7
     for f in (linear, gated):
-        assert f(_layer(), y=None) == f(_layer(), y=66) == f(_layer(), z=66) == f(_layer(n=100, xs=9), work=None) == f(_layer(n=100, xs=9), work=72) == -1
+        assert f(_layer(), y=None) == f(_layer(), y=66) == f(_layer(), z=66) == -1
+        odd = _layer(dtype=1, n=100, dim=7, xs=7, ws=7)  # rows at odd addresses, which are copied
+        assert f(odd, work=None) == f(odd, work=72) == -1
         assert f(_layer(n=0, x=None), y=None, work=None) == 0
     assert linear(_layer(), residual=66) == linear(_layer(), rs=4) == -1
     for f, zs in ((linear_grad, 5), (gated_grad, 10)):
@@ -138,7 +140,7 @@ def test_layers_refuse_bad_arguments_before_any_device_call():
     for name in ("linear", "gated"):
         assert getattr(lib, f"head_{name}_grad_bytes")(_layer()) > 0
         assert getattr(lib, f"head_{name}_bytes")(_layer(n=0)) == getattr(lib, f"head_{name}_grad_bytes")(_layer(n=0)) == 0
-        assert getattr(lib, f"head_{name}_bytes")(_layer(n=100, dim=7, xs=7, ws=7)) > 0
+        assert getattr(lib, f"head_{name}_bytes")(_layer(dtype=1, n=100, dim=7, xs=7, ws=7)) > 0
 
 
 def test_clip_refuses_bad_arguments_before_any_device_call():
@@ -149,12 +151,12 @@ def test_clip_refuses_bad_arguments_before_any_device_call():
         return lib.head_clip((hb._ClipTensor * len(rows))(*rows), count + len(more), limit, norm, work, None)
 
     for bad in (dict(grad=None), dict(grad=66), dict(out=66), dict(n=-1), dict(dtype=2), dict(count=-1), dict(limit=0.0), dict(limit=-1.0),
-                dict(limit=math.nan), dict(norm=None), dict(norm=66), dict(work=None), dict(work=72)):
+                dict(limit=math.nan), dict(norm=None), dict(norm=66), dict(n=10 ** 6, work=None), dict(n=10 ** 6, work=72)):
         assert call(**bad) == -1, bad
     assert call(more=[hb._ClipTensor(64, None, 10, 0)]) == -1  # some with a result and some without
     assert call(n=2 ** 40 + 1) == call(count=1_000_001) == -7
     assert lib.head_clip(None, 1, 1.0, 64, 64, None) == lib.head_clip_bytes(None, 1) == -1
-    assert lib.head_clip_bytes(None, 0) > 0  # there is a norm of nothing
+    assert lib.head_clip_bytes(None, 0) >= 0  # there is a norm of nothing
 
 
 def test_python_refuses_what_no_layer_is():
@@ -455,7 +457,8 @@ def _clip64(arrays, limit):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("shapes", [[(1,)], [(3,), (0,), (5, 7)], [(4096,), (4097,), (8191, 3)], [(k % 50 + 1,) for k in range(150)], [(300_001, 33), (10,)]])
+@pytest.mark.parametrize("shapes", [[(1,)], [(3,), (0,), (5, 7)], [(4096,), (4097,), (8191, 3)], [(k % 50 + 1,) for k in range(150)], [(40_960,)], [(40_000,), (961,)],
+                                    [(300_001, 33), (10,)]])
 def test_clip(shapes, in_place):
     import torch
     rng = np.random.default_rng(len(shapes))
@@ -469,7 +472,8 @@ def test_clip(shapes, in_place):
         before = [g.clone() for g in grads]
         norm, got = pk.head_clip(grads, limit, in_place=in_place)
         assert norm.shape == () and norm.dtype == torch.float32 and len(got) == len(grads)
-        assert abs(norm.item() - want_norm) <= 2 * U * want_norm
+        # 8 squares in float32 are off by 8 U of their sum at most (a product and seven sums), the root of the whole by half of that, and it is rounded
+        assert abs(norm.item() - want_norm) <= 5 * U * want_norm
         for g, o, b, w in zip(grads, got, before, want):
             assert o.dtype == g.dtype and o.shape == g.shape
             assert (o is g) == in_place and (in_place or torch.equal(g, b))
