@@ -47,8 +47,10 @@ __device__ __forceinline__ Chunk take(const T *row, int k, int dim)
     return c;
 }
 
+// parts (or null): where the sums over `each` steps from step `each` * blockIdx.y on go, [gridDim.y][n_rows][columns of z] float32.
 template <class T, bool GATED, bool WIDE, int MT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void few_kernel(const T *x, int64_t x_stride, const T *weight, int64_t weight_stride, int dim, End<T> e)
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(const T *x, int64_t x_stride, const T *weight, int64_t weight_stride, int dim, int each, End<T> e,
+                                                         float *parts)
 {
     constexpr int NT = GATED ? 2 : 1, V = 16 / sizeof(T), STEP = 4 * V, AHEAD = 4;
     __shared__ Sums lds[WAVES][NT][MT][64];
@@ -61,16 +63,21 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const T *x, int64_t x_s
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) b[mt] = x + std::min<int64_t>(mt * 16 + in, e.n_rows - 1) * x_stride;
     Sums c[NT][MT] = {};
-    int k = wave * STEP + quarter * V;
+    // A wavefront's steps are WAVES apart.  Workgroups begin at different ones: rows may lie a power of two apart, and all would ask for the
+    // same few of the memory's channels at the same time.
+    const int steps = (dim + STEP - 1) / STEP, first = each * blockIdx.y + wave, last = std::min<int>(steps, each * (blockIdx.y + 1));
+    const int own = last > first ? (last - first + WAVES - 1) / WAVES : 0;
+    int at = own ? static_cast<int>(blockIdx.x % static_cast<uint32_t>(own)) : 0;
     auto some = [&](auto COUNT) {  // steps whose loads are on their way together
         Chunk p[COUNT()][NT], q[COUNT()][MT];
 #pragma unroll
         for (int j = 0; j < COUNT(); ++j) {
-            const int at = k + j * WAVES * STEP;
+            const int k = (first + at * WAVES) * STEP + quarter * V;
+            at = at + 1 < own ? at + 1 : 0;
 #pragma unroll
-            for (int h = 0; h < NT; ++h) p[j][h] = take<T, WIDE>(w[h], at, dim);
+            for (int h = 0; h < NT; ++h) p[j][h] = take<T, WIDE>(w[h], k, dim);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) q[j][mt] = take<T, WIDE>(b[mt], at, dim);
+            for (int mt = 0; mt < MT; ++mt) q[j][mt] = take<T, WIDE>(b[mt], k, dim);
         }
 #pragma unroll
         for (int j = 0; j < COUNT(); ++j)
@@ -78,9 +85,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const T *x, int64_t x_s
             for (int h = 0; h < NT; ++h)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) multiply(p[j][h], q[j][mt], c[h][mt], T());
-        k += COUNT() * WAVES * STEP;
     };
-    const int steps = (dim + STEP - 1) / STEP, own = steps > wave ? (steps - wave + WAVES - 1) / WAVES : 0;
     int left = own;
     for (; left >= AHEAD; left -= AHEAD) some(std::integral_constant<int, AHEAD>());
     for (; left > 0; --left) some(std::integral_constant<int, 1>());
@@ -101,6 +106,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const T *x, int64_t x_s
             for (int v = 1; v < WAVES; ++v) s[h] += lds[v][h][mt][at];
         }
         if (row >= e.n_rows) continue;
+        if (parts) {
+#pragma unroll
+            for (int h = 0; h < NT; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (first + j < e.outs) parts[((blockIdx.y * e.n_rows + row) * NT + h) * e.outs + first + j] = s[h][j];
+            continue;
+        }
         with_activation(e.activation, [&](auto ACTIVATION) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -124,14 +137,16 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(const T *x, int64_t x_s
 }  // namespace
 
 template <class T, bool GATED>
-hipError_t launch_few(const head_layer &l, const End<T> &end, hipStream_t stream)
+hipError_t launch_few(const head_layer &l, const End<T> &end, int64_t splits, float *parts, hipStream_t stream)
 {
+    constexpr int WAVES = 8;
     const uint64_t strides = static_cast<uint64_t>((l.x_stride | l.weight_stride | l.dim) * static_cast<int64_t>(sizeof(T)));
     const bool wide = (address(l.x) | address(l.weight) | strides) % 16 == 0;
+    const int each = static_cast<int>(ceil_div(ceil_div(l.dim, 64 / static_cast<int64_t>(sizeof(T))), splits));
     auto run = [&](auto WIDE, auto MT) {
-        constexpr int WAVES = 8;
-        hipLaunchKernelGGL((few_kernel<T, GATED, WIDE(), MT(), WAVES>), dim3(static_cast<uint32_t>(ceil_div(l.n_outputs, COLUMNS))), dim3(64 * WAVES), 0,
-                           stream, static_cast<const T *>(l.x), l.x_stride, static_cast<const T *>(l.weight), l.weight_stride, static_cast<int>(l.dim), end);
+        hipLaunchKernelGGL((few_kernel<T, GATED, WIDE(), MT(), WAVES>), dim3(static_cast<uint32_t>(ceil_div(l.n_outputs, COLUMNS)), static_cast<uint32_t>(splits)),
+                           dim3(64 * WAVES), 0, stream, static_cast<const T *>(l.x), l.x_stride, static_cast<const T *>(l.weight), l.weight_stride,
+                           static_cast<int>(l.dim), each, end, splits > 1 ? parts : nullptr);
         return hipGetLastError();
     };
     auto rows = [&](auto WIDE) {
@@ -141,9 +156,9 @@ hipError_t launch_few(const head_layer &l, const End<T> &end, hipStream_t stream
     return wide ? rows(std::true_type()) : rows(std::false_type());
 }
 
-template hipError_t launch_few<float, false>(const head_layer &, const End<float> &, hipStream_t);
-template hipError_t launch_few<float, true>(const head_layer &, const End<float> &, hipStream_t);
-template hipError_t launch_few<bf16, false>(const head_layer &, const End<bf16> &, hipStream_t);
-template hipError_t launch_few<bf16, true>(const head_layer &, const End<bf16> &, hipStream_t);
+template hipError_t launch_few<float, false>(const head_layer &, const End<float> &, int64_t, float *, hipStream_t);
+template hipError_t launch_few<float, true>(const head_layer &, const End<float> &, int64_t, float *, hipStream_t);
+template hipError_t launch_few<bf16, false>(const head_layer &, const End<bf16> &, int64_t, float *, hipStream_t);
+template hipError_t launch_few<bf16, true>(const head_layer &, const End<bf16> &, int64_t, float *, hipStream_t);
 
 }  // namespace head_impl

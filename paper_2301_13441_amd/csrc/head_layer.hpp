@@ -76,11 +76,10 @@ struct End {
     bool wide;             // rows of residual, y and z are whole in what a lane stores of them, and short
 };
 
-// Layers of few rows, forward, have a kernel of their own (head_few.hip), without a workspace.
+// A layer of few rows, forward (head_few.hip).  splits > 1: the sum's axis is cut, and the parts are added by a kernel of the caller's.
 constexpr int64_t FEW_ROWS = 64;
-inline bool is_few(const head_layer &l) { return l.n_rows <= FEW_ROWS; }
 
 template <class T, bool GATED>
-hipError_t launch_few(const head_layer &l, const End<T> &end, hipStream_t stream);
+hipError_t launch_few(const head_layer &l, const End<T> &end, int64_t splits, float *parts, hipStream_t stream);
 
 }  // namespace head_impl

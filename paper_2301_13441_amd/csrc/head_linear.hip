@@ -331,36 +331,54 @@ struct Cut {
     int64_t tiles() const { return row_tiles * column_tiles * splits; }
 };
 
-// What a product of that cut takes, in us, from times of sum_kernel and of the kernels that add parts over 26 shapes from 100 x 64 x 4096 to
-// 8192 x 1024 x 16384.  A workgroup's step takes `more` longer for each other workgroup that its CU has, and a tile's end is its results' way to
-// memory; a launch takes 2.2; parts go to memory and back at 4.6 TB/s, in a launch of their own.  On those shapes the cut that this chooses is within
-// 15 % of the fastest one of all.
-double time_of(int32_t dtype, const Cut &c, int64_t rows, int64_t columns, int64_t depth)
+// The cut that takes the least time by a model of it, in us, made from times of sum_kernel and of the kernels that add parts over 26 shapes from
+// 100 x 64 x 4096 to 8192 x 1024 x 16384: a launch takes 2.2; a workgroup's step `step`, and `more` for each other workgroup that its CU has; a tile's
+// end, its results' way to memory, `end`; parts go to memory and back at 4.6 TB/s, in a launch of their own that takes 2.5.  On those shapes
+// what this chooses is within 12 % of the fastest cut of all.
+Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, int most_splits = 256, bool gated = false)
 {
     struct { double step, more, end; } static const TIMES[2][3] = {{{0.73, 0.5, 2.0}, {1.54, 1.26, 4.0}, {}}, {{0.39, 0.157, 1.4}, {0.62, 0.33, 3.5}, {1.4, 0, 7.4}}};
-    const auto &t = TIMES[dtype == HEAD_BF16][c.size];
-    const double step = STEP / value_bytes(dtype), steps = std::ceil(std::min(depth, c.split_depth) / step);
-    const double resident = c.size == TINY ? resident_of<Tiny>() : c.size == SMALL ? resident_of<Small>() : resident_of<Large>();
-    const double tiles = c.tiles(), others = std::ceil(std::min(tiles, resident) / 256) - 1;
-    const double us = 2.2 + std::ceil(tiles / resident) * (steps * (t.step + t.more * others) + t.end);
-    return c.splits > 1 ? us + 2.5 + static_cast<double>(c.splits) * rows * columns * 8 / 4.6e6 : us;
-}
-
-Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, bool gated = false)
-{
+    constexpr int64_t RESIDENT[] = {resident_of<Tiny>(), resident_of<Small>(), resident_of<Large>()};
     const int64_t step = STEP / value_bytes(dtype);
+    const int64_t steps = ceil_div(depth, step);
+    const double part_us = static_cast<double>(rows) * columns * 8 / 4.6e6;
     Cut best{};
     double least = INFINITY;
     for (int size = TINY; size <= (dtype == HEAD_BF16 ? LARGE : SMALL); ++size) {
-        const int64_t tile = 64 << size;
-        Cut c{size, ceil_div(rows, tile), ceil_div(columns, gated && size == TINY ? 128 : tile), 1, round_up(depth, step)};
-        for (int64_t splits = 1; splits <= 256; splits = splits & (splits - 1) ? splits / 3 * 4 : std::max(splits + 1, splits / 2 * 3)) {  // 1, 2, 3, 4, 6, 8, 12, ..
-            c.split_depth = round_up(ceil_div(depth, splits), step);
-            c.splits = std::max<int64_t>(1, ceil_div(depth, c.split_depth));
-            if (c.splits > 1 && (c.splits * rows * columns > int64_t{1} << 26 || c.tiles() > 2048)) break;
-            const double us = time_of(dtype, c, rows, columns, depth);
-            if (us < least) least = us, best = c;
+        const auto &t = TIMES[dtype == HEAD_BF16][size];
+        const int64_t tile = 64 << size, row_tiles = ceil_div(rows, tile), column_tiles = ceil_div(columns, gated && size == TINY ? 128 : tile);
+        const int64_t one = row_tiles * column_tiles;
+        for (int splits = 1; splits <= most_splits; splits = splits & (splits - 1) ? splits / 3 * 4 : std::max(splits + 1, splits / 2 * 3)) {  // 1, 2, 3, 4, 6, 8, 12, ..
+            const int64_t tiles = one * splits;
+            if (splits > 1 && (splits > steps || tiles > 2 * RESIDENT[size] || splits * rows * columns > int64_t{1} << 26)) break;
+            const int64_t each = splits == 1 ? steps : (static_cast<int32_t>(steps) + splits - 1) / splits;  // of a workgroup
+            const double others = static_cast<double>((std::min(tiles, RESIDENT[size]) + 255) / 256 - 1);
+            const double rounds = static_cast<double>((tiles + RESIDENT[size] - 1) / RESIDENT[size]);
+            const double us = 2.2 + rounds * (static_cast<double>(each) * (t.step + t.more * others) + t.end) + (splits > 1 ? 2.5 + splits * part_us : 0);
+            if (us < least) least = us, best = Cut{size, row_tiles, column_tiles, splits, each * step};
         }
+    }
+    best.splits = std::max<int64_t>(1, ceil_div(depth, best.split_depth));  // none is empty
+    return best;
+}
+
+// Parts of the sum's axis with which the kernel for few rows (head_few.hip) takes a layer whose z has that many columns; 0: tiles take it.  From
+// times of both over 10 shapes from 64 -> 256 to 8192 -> 2048 with 1 to 64 rows: up to 16 rows tiles are faster hardly anywhere; with more the
+// few-rows kernel, which reads a layer's rows again for each 16 columns, is faster up to some 128 MB of weights times rows (64 x 1024 -> 1024
+// bfloat16 7.5 us in both, 64 x 2048 -> 8192 21.5 and 13.1).  A wavefront's step, of 64 bytes of 16 weights, takes the longer the more rows there are; there are 8
+// wavefronts in a workgroup, and 512 workgroups or more need no other parts.  16 x 16384 -> 64: 30 us in one part, 6.9 in 16.
+int64_t few_of(const head_layer &l, int64_t columns)
+{
+    const int64_t row_bytes = l.dim * value_bytes(l.dtype);
+    if (l.n_rows > FEW_ROWS || (l.n_rows > 16 && l.n_rows * columns * row_bytes > int64_t{1} << 27)) return 0;
+    static const double STEP_US[] = {0.26, 0.42, 0.63, 1.06};
+    const double step = STEP_US[l.n_rows == 1 ? 0 : l.n_rows <= 16 ? 1 : l.n_rows <= 32 ? 2 : 3];
+    const int64_t steps = ceil_div(row_bytes, 64), workgroups = ceil_div(l.n_outputs, 16);
+    int64_t best = 1;
+    double least = INFINITY;
+    for (int64_t splits = 1; splits <= 16 && (splits == 1 || (splits * workgroups <= 512 && splits * 8 <= steps)); splits *= 2) {
+        const double us = static_cast<double>((steps + 8 * splits - 1) / (8 * splits)) * step + (splits > 1 ? 2.4 + 0.1 * static_cast<double>(splits) : 0);
+        if (us < least) least = us, best = splits;
     }
     return best;
 }
@@ -380,6 +398,7 @@ struct Plan : Space {
     int64_t packed;                  // values of a packed row of x and weight
     int64_t x = -1, weight = -1;     // packed operands; -1: used where they are
     Cut forward, to_x, to_weight;
+    int64_t few = 0;                 // parts of the sum's axis in the kernel for few rows; 0: not by that
     int64_t parts = -1, weight_parts = -1;
     int64_t stride;                  // values of a row of dz
     int64_t dz = -1, bias_rows, bias_chunks, bias_parts = -1;
@@ -410,9 +429,14 @@ Plan plan_forward(const head_layer &l, bool gated)
 {
     Plan p;
     const int64_t columns = gated ? 2 * l.n_outputs : l.n_outputs;
-    if (l.n_rows == 0 || is_few(l)) return p;
+    if (l.n_rows == 0) return p;
+    p.few = few_of(l, columns);
+    if (p.few) {
+        if (p.few > 1) p.parts = p.part(p.few * l.n_rows * columns * 4);
+        return p;
+    }
     plan_operands(l, columns, p);
-    p.forward = cut_of(l.dtype, l.n_rows, columns, l.dim, gated);
+    p.forward = cut_of(l.dtype, l.n_rows, columns, l.dim, 32, gated);  // finish_kernel adds a value's parts one after the other
     if (p.forward.splits > 1) p.parts = p.part(p.forward.splits * l.n_rows * columns * 4);
     return p;
 }
@@ -486,19 +510,25 @@ hipError_t forward(const head_layer &l, const void *residual, int64_t residual_s
     const int64_t columns = (GATED ? 2 : 1) * l.n_outputs;
     End<T> end{l.activation, l.bias, static_cast<const T *>(residual), residual ? residual_stride : 0, scale, static_cast<T *>(y), static_cast<T *>(z),
                l.n_rows, l.n_outputs, false};
-    if (is_few(l)) return launch_few<T, GATED>(l, end, stream);
     const Plan p = plan_forward(l, GATED);
+    float *parts = p.parts < 0 ? nullptr : reinterpret_cast<float *>(workspace + p.parts);
+    auto finish_parts = [&](int64_t splits) {
+        hipLaunchKernelGGL((finish_kernel<T, GATED>), grid_of(ceil_div(l.n_rows * l.n_outputs, 256)), dim3(256), 0, stream, parts, splits, end);
+        return hipGetLastError();
+    };
+    if (p.few) {
+        const hipError_t e = launch_few<T, GATED>(l, end, p.few, parts, stream);
+        return e || p.few == 1 ? e : finish_parts(p.few);
+    }
     const Operand<T> x = operand<T>(l.x, l.x_stride, l.n_rows, l.dim, p.packed, p.x, workspace, stream);
     const Operand<T> weight = operand<T>(l.weight, l.weight_stride, columns, l.dim, p.packed, p.weight, workspace, stream);
     if (const hipError_t e = hipGetLastError()) return e;
     const Cut &c = p.forward;
     if (c.splits > 1) {
-        float *parts = reinterpret_cast<float *>(workspace + p.parts);
         Cut sum = c;
         if (GATED && c.size == TINY) sum.column_tiles = ceil_div(columns, Tiny::TILE);
         if (const hipError_t e = launch_sum<T, true, true>(sum, x, weight, columns, 1.0f, parts, nullptr, stream)) return e;
-        hipLaunchKernelGGL((finish_kernel<T, GATED>), grid_of(ceil_div(l.n_rows * l.n_outputs, 256)), dim3(256), 0, stream, parts, c.splits, end);
-        return hipGetLastError();
+        return finish_parts(c.splits);
     }
     auto rows_whole = [&](int bytes) {  // in pieces of that many, and four of them in 32 bits of offset
         const uint64_t bits = address(y) | address(z) | address(residual) | static_cast<uint64_t>((l.n_outputs | end.residual_stride) * sizeof(T));
