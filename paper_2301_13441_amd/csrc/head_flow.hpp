@@ -218,12 +218,17 @@ struct Flow {
     static constexpr int GROUPS = STEP / 32 / GROUP, DEPTH = A::DEPTH;
     static_assert(GROUPS % 2 == 0, "a step begins in the same registers");
 
+    // Where A lies along memory B's loads go a group after A's, not all at once: bfloat16, 16,384 x 1024 x 8192 with B across 256 us and 251, 8192 x 2048 x
+    // 2048 62.4 and 60.7; both across, 8192 x 2048 x 8192, 221 and 225; pairs, 16,384 x 8192 x 1024 with their end, 309 and 314.
+    static constexpr bool LATE = sizeof(T) == 2 && A_ALONG && !PAIRS;
+
     const Operand<T> &a, &b;
     char *lds;
     A ta;
     B tb;
     int steps = 0;  // left to load of the tile that is aimed at
     int stage = 0;  // where the step is that the matrix core is at
+    int late = -1;  // where B's tile of the step goes whose loads have begun; -1: they are all on their way
     Chunk x[2][GROUP][S::MT], y[2][GROUP][S::NT];
 
     __device__ __forceinline__ Flow(const Operand<T> &a_, const Operand<T> &b_, char *lds_) : a(a_), b(b_), lds(lds_)
@@ -248,8 +253,16 @@ struct Flow {
         if (steps == 0) next();
         if (steps == 0) return;
         ta.load(a, lds + to * STAGE);
-        tb.load(b, lds + to * STAGE + A::BYTES);
+        late = to;
+        if constexpr (!LATE) load_late();
         --steps;
+    }
+
+    __device__ __forceinline__ void load_late()
+    {
+        if (late < 0) return;
+        tb.load(b, lds + late * STAGE + A::BYTES);
+        late = -1;
     }
 
     // Once the loads of stage `s`, a tile's last ones and those of ta and tb before now, are there.
@@ -361,8 +374,10 @@ struct Flow {
     __device__ __forceinline__ void begin(Next next)
     {
         load(0, next);
+        load_late();
         const int torn_a = ta.torn(), torn_b = tb.torn();
         load(1, next);
+        load_late();
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (torn_a) ta.mend(lds, torn_a);
         if (torn_b) tb.mend(lds + A::BYTES, torn_b);
@@ -385,6 +400,7 @@ struct Flow {
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 if (g + 1 < GROUPS) {
+                    if (LATE && g == 0) load_late();
                     read(g + 1);
                 } else {
                     meet();
@@ -396,6 +412,7 @@ struct Flow {
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        load_late();  // before the tile's end
     }
 };
 

@@ -22,9 +22,9 @@ namespace {
 
 // ---- forward
 
-// A lane's results of a tile, C = z before the bias, through activation and residual.  FULL: all rows and columns of the tile are there,
-// rows are whole in what a lane stores at a time, and short enough that four of them are an offset of 32 bits.
-template <class T, class S, bool GATED, bool FULL>
+// A lane's results of a tile, C = z before the bias, through activation and residual.  WIDE: rows are whole in what a lane stores at a time, and short
+// enough that four of them are an offset of 32 bits; ROWS: all rows of the tile are there.
+template <class T, class S, bool GATED, bool WIDE, bool ROWS>
 __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float (&bias)[S::NT], const End<T> &e, int64_t row0, int64_t column0)
 {
     constexpr int N = GATED ? S::NT / 2 : S::NT;  // adjacent columns of y that a lane has
@@ -35,8 +35,8 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
     const int down0 = lane / 32 * 4, across = lane % 32 * N;
     const int rows = static_cast<int>(std::min<int64_t>(S::M, e.n_rows - first)) - down0;
     const int columns = static_cast<int>(std::max<int64_t>(0, std::min<int64_t>(N, e.outs - column1 - across)));
-    if (!FULL && columns == 0) return;
-    using Offset = std::conditional_t<FULL, uint32_t, int64_t>;  // in values
+    if (columns == 0) return;
+    using Offset = std::conditional_t<WIDE, uint32_t, int64_t>;  // in values
     const int64_t z_columns = GATED ? 2 * e.outs : e.outs;
     const Offset in_y = static_cast<Offset>(down0 * e.outs + across), in_z = static_cast<Offset>(down0 * z_columns + across),
                  in_residual = static_cast<Offset>(down0 * e.residual_stride + across);
@@ -47,7 +47,7 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
         Pack<T, N> p;
 #pragma unroll
         for (int k = 0; k < N; ++k) p.v[k] = narrow<T>(v[k]);
-        if (FULL) {
+        if (WIDE) {
             *reinterpret_cast<Pack<T, N> *>(to) = p;
         } else {
 #pragma unroll
@@ -62,7 +62,7 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int down = mt * 32 + i / 4 * 8 + i % 4;
-                if (!FULL && down >= rows) continue;
+                if (!ROWS && down >= rows) continue;
                 float v[N];
                 if constexpr (GATED) {
                     float gate[N], value[N];
@@ -84,7 +84,7 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
                     for (int k = 0; k < N; ++k) v[k] = e.scale * Act(v[k]).value;
                     if (residual) {
                         const T *from = residual + down * e.residual_stride + in_residual;
-                        if (FULL) {
+                        if (WIDE) {
                             const Pack<T, N> r = *reinterpret_cast<const Pack<T, N> *>(from);
 #pragma unroll
                             for (int k = 0; k < N; ++k) v[k] += widen(r.v[k]);
@@ -130,9 +130,30 @@ __global__ __launch_bounds__(S::THREADS, 2) void layer_kernel(Operand<T> x, Oper
                 bias[nt] = k < e.outs ? e.bias[GATED ? k + nt % 2 * e.outs : k] : 0.0f;
             }
         }
-        const int64_t all_columns = GATED ? 2 * e.outs : e.outs;
-        if (e.wide && row0 + S::M <= e.n_rows && column0 + S::N <= all_columns) finish<T, S, GATED, true>(c, bias, e, row0, column0);
-        else finish<T, S, GATED, false>(c, bias, e, row0, column0);
+        if (!e.wide) finish<T, S, GATED, false, false>(c, bias, e, row0, column0);
+        else if (row0 + S::M <= e.n_rows) finish<T, S, GATED, true, true>(c, bias, e, row0, column0);
+        else finish<T, S, GATED, true, false>(c, bias, e, row0, column0);
+    }
+}
+
+// Rows of values of 2 bytes that begin at odd ones, into ones that are whole in 16 bytes: a lane makes 16 bytes of 4 or 5 words.  What is behind a
+// row's end there is not read by anybody.
+__global__ __launch_bounds__(256) void align_kernel(const uint16_t *from, int64_t stride, int64_t n_rows, int dim, uint4 *to, int chunks)
+{
+    const int64_t n = n_rows * chunks;
+    for (int64_t i = int64_t{256} * blockIdx.x + threadIdx.x; i < n; i += int64_t{256} * gridDim.x) {
+        const int64_t r = n <= INT32_MAX ? static_cast<int32_t>(i) / chunks : i / chunks;
+        const int k = static_cast<int>(i - r * chunks) * 8;
+        const uintptr_t first = reinterpret_cast<uintptr_t>(from + r * stride + k), last = reinterpret_cast<uintptr_t>(from + r * stride + dim - 1);
+        const bool odd = first & 2;
+        const uint32_t *words = reinterpret_cast<const uint32_t *>(first - (odd ? 2 : 0));
+        uint32_t w[5];  // those that hold values of the row
+#pragma unroll
+        for (int j = 0; j < 5; ++j) w[j] = reinterpret_cast<uintptr_t>(words + j) <= last && (j < 4 || odd) ? words[j] : 0;
+        uint32_t out[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] = odd ? __builtin_amdgcn_alignbit(w[j + 1], w[j], 16) : w[j];
+        to[i] = make_uint4(out[0], out[1], out[2], out[3]);
     }
 }
 
@@ -194,7 +215,7 @@ __global__ __launch_bounds__(256) void slope_kernel(Slopes<T> s)
     if (column < s.outs) {
         with_activation(s.activation, [&](auto ACTIVATION) {
             constexpr bool READS = GATED || ACTIVATION() != HEAD_IDENTITY;
-#pragma unroll 2
+#pragma unroll 4
             for (int64_t row = row0 + y; row < end; row += HIGH) {
                 const Pack<T, N> g = *reinterpret_cast<const Pack<T, N> *>(s.grad + row * s.grad_stride + column);
                 Pack<T, N> z[H], out[H];
@@ -451,7 +472,7 @@ Plan plan_backward(const head_layer &l, bool gated)
     // Rows a power of two apart would lie in few of the memory's channels: a row more than its values by 256 bytes goes through all.
     p.stride = round_up(columns, 16 / e) + 256 / e;
     p.dz = p.part(l.n_rows * p.stride * e);
-    p.bias_chunks = std::min<int64_t>(ceil_div(l.n_rows, 16), std::min<int64_t>(8192, std::max<int64_t>(1, (int64_t{1} << 20) / columns)));
+    p.bias_chunks = std::min(ceil_div(l.n_rows, 16), ceil_div(1024, ceil_div(l.n_outputs, 64 * 16 / e)));
     p.bias_rows = ceil_div(l.n_rows, p.bias_chunks);
     p.bias_chunks = ceil_div(l.n_rows, p.bias_rows);
     p.bias_parts = p.part(p.bias_chunks * columns * 4);
@@ -487,7 +508,11 @@ Operand<T> operand(const void *at, int64_t stride, int64_t rows, int64_t dim, in
     const T *from = static_cast<const T *>(at);
     if (packed_at < 0) return Operand<T>{from, stride, rows, dim};
     T *to = reinterpret_cast<T *>(workspace + packed_at);
-    hipLaunchKernelGGL((pack_kernel<T>), grid_of(ceil_div(rows * packed, 256)), dim3(256), 0, stream, from, stride, rows, dim, to, packed);
+    if constexpr (sizeof(T) == 2)
+        hipLaunchKernelGGL(align_kernel, grid_of(ceil_div(rows * packed, 8 * 256)), dim3(256), 0, stream, reinterpret_cast<const uint16_t *>(from), stride, rows,
+                           static_cast<int>(dim), reinterpret_cast<uint4 *>(to), static_cast<int>(packed / 8));
+    else  // rows too far apart
+        hipLaunchKernelGGL((pack_kernel<T>), grid_of(ceil_div(rows * packed, 256)), dim3(256), 0, stream, from, stride, rows, dim, to, packed);
     return Operand<T>{to, packed, rows, dim};
 }
 
