@@ -58,9 +58,26 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
     with_activation(e.activation, [&](auto ACTIVATION) {
         using Act = Activation<T, ACTIVATION()>;
 #pragma unroll
-        for (int mt = 0; mt < S::MT; ++mt)
+        for (int mt = 0; mt < S::MT; ++mt) {
+            // The residual's rows are read 8 at a time: loads do not go past stores, of whose memory nothing is known.
+            Pack<T, N> rest[8];
+            auto read = [&](int i0) {
+#pragma unroll
+                for (int i = i0; i < i0 + 8; ++i) {
+                    const int down = mt * 32 + i / 4 * 8 + i % 4;
+                    if (!ROWS && down >= rows) continue;
+                    const T *from = residual + down * e.residual_stride + in_residual;
+                    if (WIDE) {
+                        rest[i - i0] = *reinterpret_cast<const Pack<T, N> *>(from);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < N; ++k) rest[i - i0].v[k] = k < columns ? from[k] : T(0);
+                    }
+                }
+            };
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
+                if (!GATED && i % 8 == 0 && residual) read(i);
                 const int down = mt * 32 + i / 4 * 8 + i % 4;
                 if (!ROWS && down >= rows) continue;
                 float v[N];
@@ -83,19 +100,13 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = e.scale * Act(v[k]).value;
                     if (residual) {
-                        const T *from = residual + down * e.residual_stride + in_residual;
-                        if (WIDE) {
-                            const Pack<T, N> r = *reinterpret_cast<const Pack<T, N> *>(from);
 #pragma unroll
-                            for (int k = 0; k < N; ++k) v[k] += widen(r.v[k]);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < N; ++k) v[k] += k < columns ? widen(from[k]) : 0.0f;
-                        }
+                        for (int k = 0; k < N; ++k) v[k] += widen(rest[i % 8].v[k]);
                     }
                 }
                 put(y + down * e.outs + in_y, v);
             }
+        }
     });
 }
 
@@ -215,36 +226,46 @@ __global__ __launch_bounds__(256) void slope_kernel(Slopes<T> s)
     if (column < s.outs) {
         with_activation(s.activation, [&](auto ACTIVATION) {
             constexpr bool READS = GATED || ACTIVATION() != HEAD_IDENTITY;
-#pragma unroll 4
-            for (int64_t row = row0 + y; row < end; row += HIGH) {
-                const Pack<T, N> g = *reinterpret_cast<const Pack<T, N> *>(s.grad + row * s.grad_stride + column);
-                Pack<T, N> z[H], out[H];
-                if constexpr (READS) {
+            constexpr int ROWS = 4;  // whose loads are on their way together: they do not go past stores, of whose memory nothing is known
+            for (int64_t first = row0 + y; first < end; first += ROWS * HIGH) {
+                Pack<T, N> g[ROWS], z[ROWS][H];
 #pragma unroll
-                    for (int h = 0; h < H; ++h) z[h] = *reinterpret_cast<const Pack<T, N> *>(s.z + row * s.z_stride + h * s.outs + column);
-                }
-#pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    float d[H];
-                    d[0] = widen(g.v[k]);
+                for (int r = 0; r < ROWS; ++r) {
+                    const int64_t row = std::min(first + r * HIGH, end - 1);
+                    g[r] = *reinterpret_cast<const Pack<T, N> *>(s.grad + row * s.grad_stride + column);
                     if constexpr (READS) {
-                        const Activation<T, ACTIVATION()> a(widen(z[0].v[k]));
-                        if constexpr (GATED) {
-                            d[1] = d[0] * a.value;
-                            d[0] *= widen(z[1].v[k]);
-                        }
-                        if constexpr (ACTIVATION() == HEAD_RELU) d[0] = a.slope > 0 ? d[0] : 0;
-                        else d[0] *= a.slope;
-                    }
 #pragma unroll
-                    for (int h = 0; h < H; ++h) {
-                        sums[h][k] += d[h];
-                        out[h].v[k] = narrow<T>(d[h]);
+                        for (int h = 0; h < H; ++h) z[r][h] = *reinterpret_cast<const Pack<T, N> *>(s.z + row * s.z_stride + h * s.outs + column);
                     }
                 }
-                if (s.dz) {
 #pragma unroll
-                    for (int h = 0; h < H; ++h) *reinterpret_cast<Pack<T, N> *>(s.dz + row * s.stride + h * s.outs + column) = out[h];
+                for (int r = 0; r < ROWS; ++r) {
+                    const int64_t row = first + r * HIGH;
+                    if (row >= end) break;
+                    Pack<T, N> out[H];
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        float d[H];
+                        d[0] = widen(g[r].v[k]);
+                        if constexpr (READS) {
+                            const Activation<T, ACTIVATION()> a(widen(z[r][0].v[k]));
+                            if constexpr (GATED) {
+                                d[1] = d[0] * a.value;
+                                d[0] *= widen(z[r][1].v[k]);
+                            }
+                            if constexpr (ACTIVATION() == HEAD_RELU) d[0] = a.slope > 0 ? d[0] : 0;
+                            else d[0] *= a.slope;
+                        }
+#pragma unroll
+                        for (int h = 0; h < H; ++h) {
+                            sums[h][k] += d[h];
+                            out[h].v[k] = narrow<T>(d[h]);
+                        }
+                    }
+                    if (s.dz) {
+#pragma unroll
+                        for (int h = 0; h < H; ++h) *reinterpret_cast<Pack<T, N> *>(s.dz + row * s.stride + h * s.outs + column) = out[h];
+                    }
                 }
             }
         });
