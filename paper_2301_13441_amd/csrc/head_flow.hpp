@@ -320,13 +320,19 @@ struct Flow {
     __device__ __forceinline__ void again(Acc (&c)[S::MT][S::NT], int64_t row0, int64_t column0, int64_t from, int64_t to) const
     {
         if constexpr (sizeof(T) == 4) {
+            // Those of rows and columns that are not there, and may hold anything, do not count.
+            const int64_t columns = PAIRS ? b.rows / 2 : b.rows, column1 = PAIRS ? column0 / 2 : column0;
+            const int rows = static_cast<int>(std::min<int64_t>(S::M, a.rows - row0)) - S::row(0, 0);
             float none = 0;  // or NaN
 #pragma unroll
-            for (int mt = 0; mt < S::MT; ++mt)
+            for (int nt = 0; nt < S::NT; ++nt) {
+                const int across = PAIRS ? S::wave_n() * (S::NT * 16) + threadIdx.x % 32 * (S::NT / 2) + nt / 2 : S::column(nt);
+                const bool there = column1 + across < columns;
 #pragma unroll
-                for (int nt = 0; nt < S::NT; ++nt)
+                for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) none = fmaf(c[mt][nt][i], 0.0f, none);
+                    for (int i = 0; i < 16; ++i) none = there && mt * 32 + i / 4 * 8 + i % 4 < rows ? fmaf(c[mt][nt][i], 0.0f, none) : none;
+            }
             if (!__any(none != none)) return;
             const int lane = threadIdx.x % 32, later = threadIdx.x % 64 / 32;
             const T *pb[S::NT];

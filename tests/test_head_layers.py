@@ -368,6 +368,75 @@ def test_layers_keep_infinities_and_nan_to_their_rows(n, dim, outs, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,dim,outs", [(20, 96, 70), (130, 96, 70), (700, 200, 700)])
+def test_float32_products_over_the_range(n, dim, outs):
+    """Values far from 1, subnormal ones and the largest: float32 sums are as near as near 1."""
+    import torch
+    rng = np.random.default_rng(dim)
+    x0, w0 = rng.standard_normal((n, dim)).astype(np.float32), rng.standard_normal((2 * outs, dim)).astype(np.float32)
+    for up, down in ((-100, 100), (-100, 0), (60, 60), (120, -120), (-60, -40)):
+        x, w = x0 * np.float32(2.0 ** up), w0 * np.float32(2.0 ** down)
+        z, off = _z(x.astype(np.float64), w.astype(np.float64), None)
+        # below 2^-109 what is below 2^-133 of a value may be lost, times the other's magnitude
+        off = off + 2.0 ** -133 * (np.abs(w).astype(np.float64).sum(1)[None, :] + np.abs(x).astype(np.float64).sum(1)[:, None])
+        _close(pk.head_linear(_torch(x), _torch(w)), z, off + 2.0 ** -149, (up, down))
+    # the largest values have no bfloat16 near them
+    x, w = x0.copy(), w0 * np.float32(1e-30)
+    x[n - 1, 5], x[3, dim - 1] = 3.4e38, -3.402e38
+    z, off = _z(x.astype(np.float64), w.astype(np.float64), None)
+    got, kept = pk.head_gated(_torch(x), _torch(w), None, None, keep=True)
+    _check_z(z, off, kept, "float32", "largest")
+    g = rng.standard_normal((n, 2 * outs)).astype(np.float32)
+    gx, gw, gb = pk.head_linear_grad(_torch(g), _torch(x), _torch(w))
+    # 3.4e38 times a gradient past 1 is past the largest float32, 3.4028e38: its sum is infinite, in any order, as the other terms
+    # are below 1e31 of it.  Where it is within 1e-4 of the largest, either is right.
+    want, largest = g.astype(np.float64).T @ x.astype(np.float64), float(np.finfo(np.float32).max)
+    past, near = np.abs(want) * (1 - 1e-4) > largest, np.abs(want) * (1 + 1e-4) > largest
+    assert past.any() and (_np(gw)[past] == np.sign(want[past]) * math.inf).all()
+    gw = torch.where(torch.from_numpy(near).cuda(), torch.from_numpy(want).cuda(), gw.double())
+    _check_grads((gx, gw, gb), x.astype(np.float64), w.astype(np.float64), g.astype(np.float64), np.zeros_like(g, dtype=np.float64), 1.0, "float32", "largest")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,dim,outs", [(9, 70, 33), (70, 66, 40), (700, 200, 72)])
+def test_layers_read_nothing_between_rows(n, dim, outs, dtype):
+    """Rows that lie apart, with NaN between them and behind the last, give what rows that lie together give."""
+    import torch
+    rng = np.random.default_rng(n)
+    kept = [_rows(rng, r, c, dtype)[0] for r, c in ((n, dim), (2 * outs, dim), (n, 2 * outs), (n, outs))]
+    x, w, g, half = kept
+    nan = lambda t, to: torch.cat([t, t.new_full((len(t), to - t.shape[1]), math.nan)], 1)[:, :t.shape[1]]  # noqa: E731
+    for to in (1, 2, 64):
+        ax, aw, ag, ahalf = (nan(t, t.shape[1] + to) for t in kept)
+        y, z = pk.head_gated(x, w, keep=True)
+        for a, b in ((pk.head_linear(ax, aw), pk.head_linear(x, w)), (pk.head_gated(ax, aw), y), (pk.head_linear_grad(ag, ax, aw), pk.head_linear_grad(g, x, w)),
+                     (pk.head_gated_grad(ahalf, ax, aw, nan(z, 2 * outs + to)), pk.head_gated_grad(half, x, w, z))):
+            for p, q in zip(*((t,) if torch.is_tensor(t) else t for t in (a, b))):
+                off = (p.double() - q.double()).abs().max()  # another alignment may sum in another order
+                assert off <= (1e-4 if dtype == "float32" else 2e-2) * q.double().abs().max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,dim,outs", [(9, 70, 33), (200, 70, 33), (700, 1000, 72), (300, 64, 700)])
+def test_infinite_values_have_their_sign(n, dim, outs, dtype):
+    rng = np.random.default_rng(8)
+    x, w = _rows(rng, n, dim, dtype)[0], _rows(rng, 2 * outs, dim, dtype)[0]
+    x[2, 3], x[n - 1, dim - 1] = math.inf, -math.inf
+    w[1, 0] = -math.inf
+    with np.errstate(invalid="ignore"):
+        want = _np(x) @ _np(w).T
+    for got in (pk.head_linear(x, w), pk.head_gated(x, w, None, None, keep=True)[1]):
+        got = _np(got)
+        assert (np.isnan(got) == np.isnan(want)).all() and (got[np.isinf(want)] == want[np.isinf(want)]).all() and (np.isinf(got) == np.isinf(want)).all()
+    gx, gw, _ = pk.head_linear_grad(x[:, :1].expand(n, 2 * outs).contiguous() * 0 + 1, x, w)
+    assert (np.isinf(_np(gx)) == np.isinf(_np(w).sum(0))[None, :]).all()
+    column = _np(gw)[0]
+    assert column[3] == math.inf and column[dim - 1] == -math.inf and np.isfinite(np.delete(column, [3, dim - 1])).all()
+
+
+@pytest.mark.gpu
 def test_relu_and_its_slope_at_the_border():
     import torch
     x = torch.tensor([[0.0], [-0.0], [1e-30], [-1e-30], [math.nan]], device="cuda")
