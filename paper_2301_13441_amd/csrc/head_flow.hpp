@@ -22,7 +22,8 @@ namespace {
 
 constexpr int64_t FLOW_STRIDE = (1 << 21) + 256;  // bytes of a row's step, at most: offsets in a tile, of up to 256 rows, stay far below 2^31
 
-// Tiles of ROWS x 128 bytes of an operand: layout in LDS and meaning of the parameters as in Tile.
+// Tiles of ROWS x 128 bytes of an operand: layout in LDS and meaning of the parameters as in Tile.  PAIRS: the operand's rows are two halves, of
+// which a lane is to have the same ones: row nt * 32 + l of every NT * 32 is row NT / 2 * l + nt / 2 of the tile's ROWS / 2 of half nt % 2.
 template <class T, bool ALONG, int ROWS, int THREADS, int NT, bool PAIRS, int FRAGMENTS>
 struct FlowTile {
     static constexpr int VALUES = 16 / sizeof(T), DEPTH = STEP / sizeof(T), BYTES = ROWS * STEP, LOADS = BYTES / (THREADS * 16), WAVES = THREADS / 64;
@@ -206,7 +207,7 @@ struct Parts {
     }
 };
 
-// The products of a workgroup's tiles, one after the other.  next() aims at the next tile to load (aim), or does nothing where there is none.
+// The products of a workgroup's tiles, one after the other; PAIRS: their columns are those of two halves of B's rows (column0 counts both).  next() aims at the next tile to load (aim), or does nothing where there is none.
 template <class T, class S, bool A_ALONG, bool B_ALONG, bool PAIRS = false>
 struct Flow {
     using A = FlowTile<T, A_ALONG, S::M, S::THREADS, 1, false, S::MT>;

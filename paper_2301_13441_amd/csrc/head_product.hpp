@@ -50,12 +50,11 @@ __device__ __forceinline__ W bits_of(const uint64_t *has, int64_t word)
 // ALONG: the sum's axis lies along memory.  Row r of the tile is STEP bytes, its chunk c of 16 bytes in slot c ^ key(r): the
 // 16 lanes that are served at once read the same chunk of 16 rows, which so lie in 16 different groups of four banks.  Rows are
 // those of memory in another order where a lane of a matrix instruction is to have NT adjacent ones: row nt * 32 + l of every
-// NT * 32 is the one NT * l + nt in memory.  PAIRS: the operand's rows are two halves, of which a lane is to have the same ones: row
-// nt * 32 + l of every NT * 32 is row NT / 2 * l + nt / 2 of the tile's ROWS / 2 of half nt % 2.
+// NT * 32 is the one NT * l + nt in memory.
 // Otherwise a row of the tile holds the ROWS values of one index of the sum, its chunk c in slot c ^ key(index): bfloat16 values
 // are read by the instruction that transposes 4 x 16 of them, 16 lanes 32 bytes of each of 4 rows, and 32 lanes are served at
 // once; float32 ones one by one, 32 adjacent ones of each of two rows.
-template <class T, bool ALONG, int ROWS, int THREADS, int NT, bool PAIRS = false>
+template <class T, bool ALONG, int ROWS, int THREADS, int NT>
 struct Tile {
     static constexpr int VALUES = 16 / sizeof(T), DEPTH = STEP / sizeof(T), BYTES = ROWS * STEP;
     static constexpr int LOADS = BYTES / (THREADS * 16), WAVES = THREADS / 64;
@@ -81,13 +80,8 @@ struct Tile {
             if constexpr (ALONG) {
                 const int r = part * (64 / SLOTS) + lane / SLOTS, in = r % (NT * 32);
                 at[j] = ((lane % SLOTS) ^ key(r)) * VALUES;
-                if constexpr (PAIRS) {
-                    const int64_t row = (row0 + r - in) / 2 + in % 32 * (NT / 2) + in / 64, half = o.rows / 2;
-                    from[j] = o.at + (in / 32 % 2 * half + std::min(row, half - 1)) * o.stride + at[j];
-                } else {
-                    const int64_t row = row0 + r - in + in % 32 * NT + in / 32;
-                    from[j] = o.at + std::min(row, o.rows - 1) * o.stride + at[j];
-                }
+                const int64_t row = row0 + r - in + in % 32 * NT + in / 32;
+                from[j] = o.at + std::min(row, o.rows - 1) * o.stride + at[j];
             } else {
                 at[j] = (part * 64 + lane) / CHUNKS;
                 const int64_t row = row0 + ((part * 64 + lane) % CHUNKS ^ key(at[j])) * VALUES;
@@ -192,13 +186,11 @@ struct Shape {
 // The products of a workgroup's tiles, one after the other: tile of C = A[row0.., depth0..depth1) B[.., column0..).  While the
 // matrix core works on one step's tiles of A and B the next step's are on their way to the other half of LDS, the next
 // tile's first ones while it works on a tile's last ones and while that tile is finished.
-// PAIRS: the columns are those of two halves of B's rows (column0 counts both).
-template <class T, class S, bool A_ALONG, bool B_ALONG, bool PAIRS = false>
+template <class T, class S, bool A_ALONG, bool B_ALONG>
 struct Products {
     using A = Tile<T, A_ALONG, S::M, S::THREADS, 1>;
-    using B = Tile<T, B_ALONG, S::N, S::THREADS, S::NEXT || PAIRS ? S::NT : 1, PAIRS>;
-    static_assert(B_ALONG || !(S::NEXT || PAIRS), "rows of a tile that lies across stay in order");
-    static_assert(!PAIRS || S::NT % 2 == 0, "a wavefront's columns are as many of each half");
+    using B = Tile<T, B_ALONG, S::N, S::THREADS, S::NEXT ? S::NT : 1>;
+    static_assert(B_ALONG || !S::NEXT, "rows of a tile that lies across stay in order");
     static constexpr int BYTES = A::BYTES + B::BYTES;  // of a step; LDS holds two
 
     const Operand<T> &a, &b;
