@@ -237,8 +237,8 @@ int head_adamw_values(const head_adamw_tensor *tensors, void *const *out_m, void
  * up to 8 values are added in float32, and those sums in float64; no finite values make the norm overflow before it is rounded to float32, or
  * vanish.  A norm that is NaN makes
  * every value NaN; with an infinite one finite values become 0 and infinite ones NaN.  max_norm > 0; INFINITY: no limit (what is not
- * finite stays as it is).  grad and out, of dtype, may be the same memory, which is then not written where the factor is 1; out NULL in all
- * tensors: only the norm is wanted.  The list is HOST memory, borrowed for the call.
+ * finite stays as it is).  grad and out, of dtype, may be the same memory, which is then not written where the factor is 1; no other two of
+ * them that are written may overlap.  out NULL in all tensors: only the norm is wanted.  The list is HOST memory, borrowed for the call.
  */
 typedef struct head_clip_tensor {
     const void *grad;

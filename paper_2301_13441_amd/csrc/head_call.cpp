@@ -592,7 +592,7 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     if (rc) return PyLong_FromLong(rc);
     PyObject *list = PyList_New(n);
     for (Py_ssize_t i = 0; list && i < n; ++i) {
-        PyObject *one = in_place ? Py_NewRef(PyList_GET_ITEM(args[0], i)) : THPVariable_Wrap(out[i]);
+        PyObject *one = THPVariable_Wrap(out[i]);  // in place: the list's own object, whatever has become of the list meanwhile
         if (!one) {
             Py_DECREF(list);
             return nullptr;

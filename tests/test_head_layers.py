@@ -638,6 +638,62 @@ class _OtherDevice:
 
 
 @pytest.mark.gpu
+def test_layer_calls_of_two_threads_and_two_graphs_at_once():
+    """Two threads on streams of their own, and two graphs replayed in turn, give the bits of calls one after the other."""
+    import threading
+
+    import torch
+    rng = np.random.default_rng(3)
+    sides = []
+    for n, dim, hidden, dtype in ((2100, 600, 520, "bfloat16"), (900, 331, 200, "float32")):
+        x, g = _rows(rng, n, dim, dtype)[0], _rows(rng, n, hidden, dtype)[0]
+        w = _rows(rng, 2 * hidden, dim, dtype, scale=dim ** -0.5)[0]
+
+        def run(x=x, g=g, w=w, stream=None):
+            h, z = pk.head_gated(x, w, keep=True, stream=stream)
+            gx, gw, gb = pk.head_gated_grad(g, x, w, z, stream=stream)
+            norm, clipped = pk.head_clip([gw, gb], 0.5, stream=stream)
+            return [h, pk.head_linear(h, w[:, :h.shape[1]], stream=stream) if h.shape[1] <= w.shape[1] else h, gx, norm, *clipped]
+        sides.append((run, run()))
+    torch.cuda.synchronize()
+    failed = []
+
+    def many(run, want):
+        try:
+            stream = torch.cuda.Stream()
+            for k in range(30):
+                if k % 2:
+                    got = run(stream=stream)
+                else:
+                    with torch.cuda.stream(stream):
+                        got = run()
+                stream.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+        except BaseException as e:  # noqa: BLE001  (told by the main thread)
+            failed.append(e)
+
+    threads = [threading.Thread(target=many, args=side) for side in sides]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    graphs = []
+    for run, _ in sides:
+        graphs.append((torch.cuda.CUDAGraph(), []))
+        with torch.cuda.graph(graphs[-1][0]):
+            graphs[-1][1].extend(run())
+    for k in range(3):
+        for graph, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, got), (run, want) in zip(graphs, sides):
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+            run()
+        torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
 def test_python_refuses_layers_that_do_not_fit():
     import torch
     x, w = torch.zeros(4, 8, device="cuda"), torch.zeros(6, 8, device="cuda")
