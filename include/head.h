@@ -164,7 +164,7 @@ typedef struct head_layer {
 } head_layer;
 
 /* Bytes of workspace (16-byte aligned) of the four calls below; negative HEAD_E* on error.  Of the pointers and strides in `l` only
- * the alignment counts.  The gradients' holds the gradient of z, and grows with the rows. */
+ * the alignment counts, and whether rows begin more than 2 MB apart.  The gradients' holds the gradient of z, and grows with the rows. */
 int64_t head_linear_bytes(const head_layer *l);
 int64_t head_linear_grad_bytes(const head_layer *l);
 int64_t head_gated_bytes(const head_layer *l);
