@@ -296,6 +296,15 @@ int head_gated_grad(const head_layer *l, const void *z, int64_t z_stride, const 
     return done(launch_gated_grad(*l, z, z_stride, grad, grad_stride, grad_x, grad_weight, grad_bias, workspace, static_cast<hipStream_t>(stream)));
 }
 
+int head_layer_launch(const head_layer *l, int32_t gated, head_layer_launch_t *out)
+{
+    const int64_t bytes = gated ? head_gated_grad_bytes(l) : head_linear_grad_bytes(l);
+    if (bytes < 0) return static_cast<int>(bytes);
+    if (!out || l->n_rows < 1) return HEAD_EINVAL;
+    *out = layer_launch(*l, gated != 0);
+    return HEAD_OK;
+}
+
 int head_adamw(const head_adamw_rule *rule, const head_adamw_tensor *tensors, int32_t n_tensors, void *stream)
 {
     if (!rule || !is_dtype(rule->grad_dtype) || (rule->bits != 32 && rule->bits != 8) || rule->step < 1) return HEAD_EINVAL;

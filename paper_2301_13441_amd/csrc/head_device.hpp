@@ -8,6 +8,7 @@
 #include <cstdint>
 
 #include "../../include/head.h"
+#include "../../include/head_testing.h"
 
 namespace head_impl {
 
@@ -106,6 +107,8 @@ hipError_t launch_linear_grad(const head_layer &l, const void *z, int64_t z_stri
 hipError_t launch_gated(const head_layer &l, void *y, void *z, void *workspace, hipStream_t stream);
 hipError_t launch_gated_grad(const head_layer &l, const void *z, int64_t z_stride, const void *grad, int64_t grad_stride, void *grad_x,
                              void *grad_weight, float *grad_bias, void *workspace, hipStream_t stream);
+
+head_layer_launch_t layer_launch(const head_layer &l, bool gated);
 
 int64_t clip_bytes(const head_clip_tensor *tensors, int32_t n_tensors);
 hipError_t launch_clip(const head_clip_tensor *tensors, int32_t n_tensors, double max_norm, float *norm, void *workspace, hipStream_t stream);

@@ -669,6 +669,15 @@ hipError_t backward(const head_layer &l, const void *z, int64_t z_stride, const 
 
 }  // namespace
 
+head_layer_launch_t layer_launch(const head_layer &l, bool gated)
+{
+    const Plan f = plan_forward(l, gated), b = plan_backward(l, gated);
+    auto tile = [](const Cut &c) { return 64 << c.size; };
+    auto splits = [](const Cut &c) { return static_cast<int32_t>(c.splits); };
+    return head_layer_launch_t{static_cast<int32_t>(f.few), b.x >= 0, b.weight >= 0, f.few ? 0 : tile(f.forward), f.few ? 0 : splits(f.forward),
+                               tile(b.to_x), splits(b.to_x), tile(b.to_weight), splits(b.to_weight)};
+}
+
 int64_t linear_bytes(const head_layer &l) { return plan_forward(l, false).bytes; }
 int64_t gated_bytes(const head_layer &l) { return plan_forward(l, true).bytes; }
 int64_t linear_grad_bytes(const head_layer &l) { return plan_backward(l, false).bytes; }

@@ -28,6 +28,7 @@ HEAD_EXPORTS = ["head_embed", "head_embed_grad_bytes", "head_embed_grad", "head_
                 "head_cross_entropy_grad", "head_adamw", "head_adamw_values", "head_linear_bytes", "head_linear", "head_linear_grad_bytes",
                 "head_linear_grad", "head_gated_bytes", "head_gated", "head_gated_grad_bytes", "head_gated_grad", "head_clip_bytes",
                 "head_clip", "head_strerror"]
+HEAD_TESTING_EXPORTS = ["head_layer_launch"]
 ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}  # HEAD_IDENTITY, HEAD_RELU, HEAD_GELU, HEAD_SILU
 BLOCK = 128  # HEAD_BLOCK
 
@@ -57,6 +58,11 @@ class _Layer(ctypes.Structure):
 
 class _ClipTensor(ctypes.Structure):
     _fields_ = [("grad", _p), ("out", _p), ("n", _i64), ("dtype", _i32)]
+
+
+class _LayerLaunch(ctypes.Structure):
+    _fields_ = [(name, _i32) for name in ("few", "copies_x", "copies_weight", "tile", "splits", "to_x_tile", "to_x_splits", "to_weight_tile",
+                                          "to_weight_splits")]
 
 
 class HeadError(RuntimeError):
@@ -97,6 +103,7 @@ def _lib():
             ("head_gated_grad", _i32, layer, _p, _i64, _p, _i64, _p, _p, _p, _p, _p),
             ("head_clip_bytes", _i64, clips, _i32),
             ("head_clip", _i32, clips, _i32, _f64, _p, _p, _p),
+            ("head_layer_launch", _i32, layer, _i32, ctypes.POINTER(_LayerLaunch)),
             ("head_strerror", ctypes.c_char_p, _i32)):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = result, args
@@ -526,6 +533,17 @@ def _layer(x, weight, bias, activation: int, halves: int):
         _tensor(bias, "bias", torch.float32, (weight.shape[0],), x)
     return _Layer(dtype, activation, x.shape[0], x.shape[1], weight.shape[0] // halves, x.data_ptr(), _stride(x), weight.data_ptr(),
                   _stride(weight), _at(bias))
+
+
+def head_layer_launch(n_rows: int, dim: int, n_outputs: int, dtype: str = "float32", gated: bool = False, x: int = 0, x_stride: Optional[int] = None,
+                      weight: int = 0, weight_stride: Optional[int] = None) -> dict:
+    """What calls on a layer launch whose x and weight are at these addresses, their rows so many values apart (include/head_testing.h); no GPU
+    needed."""
+    s = _LayerLaunch()
+    layer = _Layer({"float32": 0, "bfloat16": 1}[dtype], 0, n_rows, dim, n_outputs, x, dim if x_stride is None else x_stride, weight,
+                   dim if weight_stride is None else weight_stride, None)
+    _check(_lib().head_layer_launch(layer, gated, s), "head_layer_launch")
+    return {name: int(getattr(s, name)) for name, _ in _LayerLaunch._fields_}
 
 
 def head_linear(x, weight, bias=None, activation: Optional[str] = None, residual=None, scale: float = 1.0, keep: bool = False, stream=None):

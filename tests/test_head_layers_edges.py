@@ -1,0 +1,169 @@
+"""The head's layers and head_clip where their kernels change their ways: the largest tiles with rows, columns and sums that end inside them, and
+what a call launches, which is asked for without a GPU.
+
+Tolerances are bounds on rounding as in test_head_layers.py, element by element: n float32 terms differ from their exact sum by at most n * 2^-24 *
+(sum of their magnitudes), and some more where a bias is added or parts are joined; a bfloat16 result by up to 2^-8 of itself; activations and slopes of
+bfloat16 values are right to 2^-13, and slopes are at most 1.13.  References are computed in float64, on the GPU, by the formulas of head.h.
+"""
+import math
+import os
+import re
+
+import pytest
+
+import paper_2301_13441_amd as pk
+from paper_2301_13441_amd import head_binding as hb
+
+U = 2.0 ** -24
+TINY = 1e-37
+NEAR = {"float32": U, "bfloat16": 2.0 ** -8}  # what rounding to a type may change, relative to the value
+
+
+def _within(got, want, bound, what=""):
+    import torch
+    off, bound = (got.double() - want).abs(), bound + TINY
+    assert got.shape == want.shape, what
+    assert (off <= bound).all(), (what, (off / bound).max().item(), torch.nonzero(~(off <= bound))[0].tolist())
+
+
+def _act(name, x):
+    import torch
+    if name == "silu":
+        return x * torch.sigmoid(x)
+    if name == "gelu":
+        return x * torch.special.erfc(-x / math.sqrt(2)) / 2
+    return x
+
+
+def _slope(name, x):
+    import torch
+    if name == "silu":
+        s = torch.sigmoid(x)
+        return s + x * s * (1 - s)
+    if name == "gelu":
+        return torch.special.erfc(-x / math.sqrt(2)) / 2 + x * torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+    return torch.ones_like(x)
+
+
+def _act_off(name, x, dtype):
+    if name is None:
+        return _zeros(x)
+    return _act(name, x).abs() * (2.0 ** -13 if dtype == "bfloat16" else U * (16 + 2 * x * x))
+
+
+def _slope_off(name, x, dtype):
+    return _zeros(x) if name is None else _zeros(x) + (2.0 ** -13 if dtype == "bfloat16" else 2.0 ** -19)
+
+
+def _zeros(x):
+    return x.new_zeros(x.shape)
+
+
+def _z(x, w, b):
+    """z and how far a float32 sum may be from it."""
+    z, magnitude = x.double() @ w.double().T, x.double().abs() @ w.double().abs().T
+    if b is not None:
+        z, magnitude = z + b.double(), magnitude + b.double().abs()
+    return z, (x.shape[1] + 64) * U * magnitude
+
+
+def _check_forward(got, kept, x, w, b, act, residual, scale, gated, dtype):
+    near = NEAR[dtype]
+    z, off = _z(x, w, b)
+    if kept is not None:
+        _within(kept, z, off * (1 + near) + near * z.abs(), "z")
+    if gated:
+        (gate, value), (gate_off, value_off) = z.chunk(2, 1), off.chunk(2, 1)
+        a, a_off = _act(act, gate), 1.13 * gate_off + _act_off(act, gate, dtype)
+        want = a * value
+        off = a_off * value.abs() + (a.abs() + a_off) * value_off + 4 * U * want.abs()
+    else:
+        rest = 0 if residual is None else residual.double()
+        part = scale * _act(act, z)
+        want = part + rest
+        off = abs(scale) * (1.13 * off + _act_off(act, z, dtype)) + 4 * U * (part.abs() + (0 if residual is None else rest.abs()))
+    _within(got, want, off * (1 + near) + near * want.abs(), "y")
+
+
+def _check_gradients(got, grad, x, w, z, act, scale, gated, dtype):
+    near, g, z = NEAR[dtype], grad.double(), None if z is None else z.double()
+    if gated:
+        import torch
+        gate, value = z.chunk(2, 1)
+        dz = torch.cat([g * value * _slope(act, gate), g * _act(act, gate)], 1)
+        off = torch.cat([(g * value).abs() * (_slope_off(act, gate, dtype) + 4 * U * _slope(act, gate).abs()),
+                         g.abs() * (_act_off(act, gate, dtype) + 2 * U * _act(act, gate).abs())], 1)
+    elif act is None:
+        dz, off = g, _zeros(g)
+    else:
+        dz = g * _slope(act, z)
+        off = g.abs() * (_slope_off(act, z, dtype) + 2 * U * _slope(act, z).abs())
+    if got[2] is not None:
+        _within(got[2], scale * dz.sum(0), abs(scale) * (off.sum(0) + (len(dz) + 64) * U * dz.abs().sum(0)) + 2 * U * (scale * dz.sum(0)).abs(), "bias")
+    off = off + near * (dz.abs() + off)  # dz is rounded to the type before it is multiplied
+    size = dz.abs() + off
+    for t, want, o, m, n, what in ((got[0], dz @ w.double(), off @ w.double().abs(), size @ w.double().abs(), dz.shape[1], "x"),
+                                   (got[1], dz.T @ x.double(), off.T @ x.double().abs(), size.T @ x.double().abs(), len(dz), "weight")):
+        want = scale * want
+        _within(t, want, abs(scale) * (o + (n + 64) * U * m) * (1 + near) + (near + 2 * U) * want.abs(), what)
+
+
+def _normal(seed, *shape, dtype="float32", scale=1.0):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(getattr(torch, dtype))
+
+
+# ---------------------------------------------------------------- no GPU needed
+
+def test_testing_header_declares_what_the_library_exports():
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "head_testing.h")).read()
+    code = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    assert set(re.findall(r"\b(head_[a-z_]+)\s*\(", code)) == set(hb.HEAD_TESTING_EXPORTS)
+    assert re.findall(r"\b(\w+)[,;]", code[code.index("struct"):code.index("} head_layer_launch_t")]) == [name for name, _ in hb._LayerLaunch._fields_]
+    lib = hb._lib()
+    assert all(hasattr(lib, name) for name in hb.HEAD_TESTING_EXPORTS)
+    for bad, code in (((0, 8, 8), -1), ((-1, 8, 8), -1), ((4, 0, 8), -1), ((4, 8, 0), -1), ((4, 16385, 8), -7), ((4, 8, 262_145), -7)):
+        with pytest.raises(pk.HeadError) as e:
+            hb.head_layer_launch(*bad)
+        assert e.value.code == code
+    assert lib.head_layer_launch(None, 0, hb._LayerLaunch()) == lib.head_layer_launch(hb._Layer(0, 0, 4, 8, 8, 0, 8, 0, 8, None), 0, None) == -1
+
+
+# Layers of bfloat16 values whose forward and gradients all go in tiles of 256: rows, columns and sums that end inside one and that fill it; widths
+# that are whole in 16 bytes, in what a lane stores, and not; sums in one part and in three.
+LARGE = [(False, 2049, 2049, 4101), (False, 4099, 2051, 2056), (False, 2049, 4099, 2051), (False, 4096, 4096, 4096),
+         (True, 2049, 2051, 2051), (True, 4099, 2052, 1028), (True, 4096, 4096, 2048)]
+
+
+@pytest.mark.parametrize("gated,n,dim,outs", LARGE)
+def test_these_layers_go_in_the_largest_tiles(gated, n, dim, outs):
+    """Whatever the rule that chooses tiles becomes, the shapes of the test below have to take the largest."""
+    s = hb.head_layer_launch(n, dim, outs, "bfloat16", gated)
+    assert (s["few"], s["tile"], s["to_x_tile"], s["to_weight_tile"]) == (0, 256, 256, 256), s
+
+
+# ---------------------------------------------------------------- the largest tiles
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gated,n,dim,outs", LARGE)
+def test_layers_in_the_largest_tiles(gated, n, dim, outs):
+    import torch
+    dtype, columns = "bfloat16", outs * (2 if gated else 1)
+    x, w = _normal(n, n, dim, dtype=dtype), _normal(dim, columns, dim, dtype=dtype, scale=dim ** -0.5)
+    b, residual, grad = _normal(outs, columns), _normal(1, n, outs, dtype=dtype), _normal(2, n, outs, dtype=dtype, scale=0.1)
+    for act, bias, rest, scale in (("gelu", b, None, 1.0), ("silu", None, residual, 0.5), (None, b, residual, 0.75)):
+        if gated:
+            call = lambda keep: pk.head_gated(x, w, bias, act, keep=keep)  # noqa: E731
+        else:
+            call = lambda keep: pk.head_linear(x, w, bias, act, rest, scale, keep=keep)  # noqa: E731
+        y, z = call(True)
+        _check_forward(y, z, x, w, bias, act, rest, scale, gated, dtype)
+        assert torch.equal(call(False), y)
+        if gated:
+            take = lambda: pk.head_gated_grad(grad, x, w, z, act, bias=bias is not None)  # noqa: E731
+        else:
+            take = lambda: pk.head_linear_grad(grad, x, w, z if act else None, act, scale, bias=bias is not None)  # noqa: E731
+        got = take()
+        _check_gradients(got, grad, x, w, z, act, 1.0 if gated else scale, gated, dtype)
+        assert all(p is None or torch.equal(p, q) for p, q in zip(take(), got))  # the same call gives the same bits
