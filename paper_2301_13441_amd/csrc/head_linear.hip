@@ -376,9 +376,9 @@ struct LinearOf { using Type = typename Size::template Of<true>; };
 template <>
 struct LinearOf<Large> { using Type = Shape<256, 256, 4, 2, true>; };
 
-// Workgroups of a launch: as many as the device holds at a time.
-template <class Size>
-constexpr int64_t resident_of() { return std::is_same_v<Size, Tiny> ? 1024 : Size::RESIDENT; }
+// Workgroups of a launch: as many as the device holds at a time.  A gated layer's 64 x 128 tiles have 48 KB of LDS, of which a CU holds three.
+template <class Size, bool GATED = false>
+constexpr int64_t resident_of() { return !std::is_same_v<Size, Tiny> ? Size::RESIDENT : GATED ? 768 : 1024; }
 
 enum { TINY, SMALL, LARGE };
 
@@ -393,9 +393,16 @@ struct Cut {
 // 100 x 64 x 4096 to 8192 x 1024 x 16384: a launch takes 2.2; a workgroup's step `step`, and `more` for each other workgroup that its CU has; a tile's
 // end, its results' way to memory, `end`; parts go to memory and back at 4.6 TB/s, in a launch of their own that takes 2.5.  On those shapes
 // what this chooses is within 12 % of the fastest cut of all.
+//
+// A gated layer in one part goes to layer_kernel, whose smallest tile is 64 x 128 and has a price of its own, from that kernel's times over 26 layers, with
+// and without z; in parts it goes to sum_kernel like any other product.  On those layers the choice is within 18 % of the fastest, 1.3 % on average:
+// bfloat16, z kept, 16,385 x 1024 to 4096 in tiles of 64 x 128, 128 and 256 434, 370 and 300 us, 5000 x 256 to 1024 15.9, 17.1 and 13.8, 2048 x 512 to 256
+// 8.9, 10.8 and 17.2; float32 16,384 x 512 to 2048 506 and 439, 4096 x 64 to 128 7.9 and 10.8.
 Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, int most_splits = 256, bool gated = false)
 {
-    struct { double step, more, end; } static const TIMES[2][3] = {{{0.73, 0.5, 2.0}, {1.54, 1.26, 4.0}, {}}, {{0.39, 0.157, 1.4}, {0.62, 0.33, 3.5}, {1.4, 0, 7.4}}};
+    struct Times { double step, more, end; };
+    static constexpr Times TIMES[2][3] = {{{0.73, 0.5, 2.0}, {1.54, 1.26, 4.0}, {}}, {{0.39, 0.157, 1.4}, {0.62, 0.33, 3.5}, {1.4, 0, 7.4}}};
+    static constexpr Times GATED_TINY[2] = {{1.08, 0.61, 2.75}, {0.56, 0.25, 2.0}};
     constexpr int64_t RESIDENT[] = {resident_of<Tiny>(), resident_of<Small>(), resident_of<Large>()};
     const int64_t step = STEP / value_bytes(dtype);
     const int64_t steps = ceil_div(depth, step);
@@ -403,15 +410,16 @@ Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, int most
     Cut best{};
     double least = INFINITY;
     for (int size = TINY; size <= (dtype == HEAD_BF16 ? LARGE : SMALL); ++size) {
-        const auto &t = TIMES[dtype == HEAD_BF16][size];
-        const int64_t tile = 64 << size, row_tiles = ceil_div(rows, tile), column_tiles = ceil_div(columns, gated && size == TINY ? 128 : tile);
-        const int64_t one = row_tiles * column_tiles;
+        const int64_t tile = 64 << size, row_tiles = ceil_div(rows, tile);
         for (int splits = 1; splits <= most_splits; splits = splits & (splits - 1) ? splits / 3 * 4 : std::max(splits + 1, splits / 2 * 3)) {  // 1, 2, 3, 4, 6, 8, 12, ..
-            const int64_t tiles = one * splits;
-            if (splits > 1 && (splits > steps || tiles > 2 * RESIDENT[size] || splits * rows * columns > int64_t{1} << 26)) break;
+            const bool wide = gated && size == TINY && splits == 1;
+            const auto &t = wide ? GATED_TINY[dtype == HEAD_BF16] : TIMES[dtype == HEAD_BF16][size];
+            const int64_t column_tiles = ceil_div(columns, wide ? 128 : tile), tiles = row_tiles * column_tiles * splits;
+            const int64_t resident = wide ? resident_of<Tiny, true>() : RESIDENT[size];
+            if (splits > 1 && (splits > steps || tiles > 2 * resident || splits * rows * columns > int64_t{1} << 26)) break;
             const int64_t each = splits == 1 ? steps : (static_cast<int32_t>(steps) + splits - 1) / splits;  // of a workgroup
-            const double others = static_cast<double>((std::min(tiles, RESIDENT[size]) + 255) / 256 - 1);
-            const double rounds = static_cast<double>((tiles + RESIDENT[size] - 1) / RESIDENT[size]);
+            const double others = static_cast<double>((std::min(tiles, resident) + 255) / 256 - 1);
+            const double rounds = static_cast<double>((tiles + resident - 1) / resident);
             const double us = 2.2 + rounds * (static_cast<double>(each) * (t.step + t.more * others) + t.end) + (splits > 1 ? 2.5 + splits * part_us : 0);
             if (us < least) least = us, best = Cut{size, row_tiles, column_tiles, splits, each * step};
         }
@@ -587,9 +595,7 @@ hipError_t forward(const head_layer &l, const void *residual, int64_t residual_s
     if (const hipError_t e = hipGetLastError()) return e;
     const Cut &c = p.forward;
     if (c.splits > 1) {
-        Cut sum = c;
-        if (GATED && c.size == TINY) sum.column_tiles = ceil_div(columns, Tiny::TILE);
-        if (const hipError_t e = launch_sum<T, true, true>(sum, x, weight, columns, 1.0f, parts, nullptr, stream)) return e;
+        if (const hipError_t e = launch_sum<T, true, true>(c, x, weight, columns, 1.0f, parts, nullptr, stream)) return e;
         return finish_parts(c.splits);
     }
     auto rows_whole = [&](int bytes) {  // in pieces of that many, and four of them in 32 bits of offset
@@ -600,7 +606,7 @@ hipError_t forward(const head_layer &l, const void *residual, int64_t residual_s
         using Size = decltype(size);
         using S = typename std::conditional_t<GATED, GatedOf<Size>, LinearOf<Size>>::Type;
         end.wide = rows_whole((GATED ? S::NT / 2 : S::NT) * static_cast<int>(sizeof(T)));
-        return launch_tiles<S, layer_kernel<T, S, GATED>>(c.tiles(), resident_of<Size>(), stream, x, weight, end, static_cast<uint32_t>(c.row_tiles),
+        return launch_tiles<S, layer_kernel<T, S, GATED>>(c.tiles(), resident_of<Size, GATED>(), stream, x, weight, end, static_cast<uint32_t>(c.row_tiles),
                                                           static_cast<uint32_t>(c.column_tiles));
     });
 }

@@ -143,7 +143,42 @@ def test_these_layers_go_in_the_largest_tiles(gated, n, dim, outs):
     assert (s["few"], s["tile"], s["to_x_tile"], s["to_weight_tile"]) == (0, 256, 256, 256), s
 
 
-# ---------------------------------------------------------------- the largest tiles
+# Gated layers and the tile that was fastest by 8 % or more, z kept, of 64 x 128, 128 and 256 results.
+FASTEST = [("bfloat16", 15_000, 1024, 4096, 256), ("bfloat16", 16_384, 1024, 4096, 256), ("bfloat16", 16_385, 1024, 4096, 256), ("bfloat16", 33_000, 512, 2048, 256),
+           ("bfloat16", 8192, 2048, 1024, 256), ("bfloat16", 4096, 512, 2048, 256), ("bfloat16", 1000, 1024, 4096, 128), ("bfloat16", 2048, 512, 256, 64),
+           ("bfloat16", 4096, 64, 128, 64), ("float32", 8192, 2048, 1024, 128), ("float32", 4096, 512, 2048, 128), ("float32", 16_384, 512, 2048, 128),
+           ("float32", 1000, 1024, 4096, 128), ("float32", 4096, 64, 128, 64), ("float32", 1000, 128, 500, 64)]
+
+
+@pytest.mark.parametrize("dtype,n,dim,outs,tile", FASTEST)
+def test_a_gated_layer_goes_in_the_fastest_tiles(dtype, n, dim, outs, tile):
+    s = hb.head_layer_launch(n, dim, outs, dtype, gated=True)
+    assert (s["few"], s["tile"], s["splits"]) == (0, tile, 1), s
+
+
+# Gated layers in tiles of 64 x 128 and 128 x 128.
+GATED = [("bfloat16", 1003, 1027, 4093, 128), ("bfloat16", 9001, 336, 332, 128), ("float32", 4090, 515, 1021, 128), ("float32", 4090, 512, 1016, 128),
+         ("bfloat16", 2050, 515, 257, 64), ("bfloat16", 2050, 512, 256, 64), ("float32", 4099, 67, 131, 64), ("float32", 4099, 64, 136, 64)]
+
+
+@pytest.mark.parametrize("dtype,n,dim,outs,tile", GATED)
+def test_these_gated_layers_go_in_these_tiles(dtype, n, dim, outs, tile):
+    s = hb.head_layer_launch(n, dim, outs, dtype, gated=True)
+    assert (s["few"], s["tile"], s["splits"]) == (0, tile, 1), s
+
+
+# ---------------------------------------------------------------- tiles
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n,dim,outs,tile", GATED)
+def test_gated_layers_in_each_tile(dtype, n, dim, outs, tile):
+    import torch
+    x, w, b = _normal(n, n, dim, dtype=dtype), _normal(dim, 2 * outs, dim, dtype=dtype, scale=dim ** -0.5), _normal(outs, 2 * outs)
+    for act, bias in (("silu", b), ("gelu", None), (None, b)):
+        y, z = pk.head_gated(x, w, bias, act, keep=True)
+        _check_forward(y, z, x, w, bias, act, None, 1.0, True, dtype)
+        assert torch.equal(pk.head_gated(x, w, bias, act), y)
+
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("gated,n,dim,outs", LARGE)
