@@ -298,8 +298,7 @@ int head_gated_grad(const head_layer *l, const void *z, int64_t z_stride, const 
 
 int head_layer_launch(const head_layer *l, int32_t gated, head_layer_launch_t *out)
 {
-    const int64_t bytes = gated ? head_gated_grad_bytes(l) : head_linear_grad_bytes(l);
-    if (bytes < 0) return static_cast<int>(bytes);
+    if (int rc = check_layer(l, gated ? 2 : 1)) return rc;
     if (!out || l->n_rows < 1) return HEAD_EINVAL;
     *out = layer_launch(*l, gated != 0);
     return HEAD_OK;

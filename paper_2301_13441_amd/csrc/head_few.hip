@@ -18,7 +18,7 @@ using Sums = float __attribute__((ext_vector_type(4)));
 using Bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using Chunk = float __attribute__((ext_vector_type(4)));  // 16 bytes of either type
 
-constexpr int COLUMNS = 16;  // of a workgroup
+constexpr int COLUMNS = FEW_COLUMNS;
 
 __device__ __forceinline__ void multiply(Chunk a, Chunk b, Sums &c, bf16)
 {

@@ -98,6 +98,8 @@ struct End {
 
 // A layer of few rows, forward (head_few.hip).  splits > 1: the sum's axis is cut, and the parts are added by a kernel of the caller's.
 constexpr int64_t FEW_ROWS = 64;
+constexpr int FEW_COLUMNS = 16;               // of y, of a workgroup of 512 lanes
+constexpr int64_t FEW_WORKGROUPS = 1 << 22;   // of a launch: 2^31 lanes, a grid's axis has room for 2^32.  Layers of more columns go by tiles
 
 template <class T, bool GATED>
 hipError_t launch_few(const head_layer &l, const End<T> &end, int64_t splits, float *parts, hipStream_t stream);

@@ -436,10 +436,11 @@ Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, int most
 int64_t few_of(const head_layer &l, int64_t columns)
 {
     const int64_t row_bytes = l.dim * value_bytes(l.dtype);
-    if (l.n_rows > FEW_ROWS || (l.n_rows > 16 && l.n_rows * columns * row_bytes > int64_t{1} << 27)) return 0;
+    if (l.n_rows > FEW_ROWS || ceil_div(l.n_outputs, FEW_COLUMNS) > FEW_WORKGROUPS) return 0;
+    if (l.n_rows > 16 && l.n_rows * columns * row_bytes > int64_t{1} << 27) return 0;
     static const double STEP_US[] = {0.26, 0.42, 0.63, 1.06};
     const double step = STEP_US[l.n_rows == 1 ? 0 : l.n_rows <= 16 ? 1 : l.n_rows <= 32 ? 2 : 3];
-    const int64_t steps = ceil_div(row_bytes, 64), workgroups = ceil_div(l.n_outputs, 16);
+    const int64_t steps = ceil_div(row_bytes, 64), workgroups = ceil_div(l.n_outputs, FEW_COLUMNS);
     int64_t best = 1;
     double least = INFINITY;
     for (int64_t splits = 1; splits <= 16 && (splits == 1 || (splits * workgroups <= 512 && splits * 8 <= steps)); splits *= 2) {
@@ -463,7 +464,7 @@ struct Space {
 struct Plan : Space {
     int64_t packed;                  // values of a packed row of x and weight
     int64_t x = -1, weight = -1;     // packed operands; -1: used where they are
-    Cut forward, to_x, to_weight;
+    Cut forward{}, to_x{}, to_weight{};
     int64_t few = 0;                 // parts of the sum's axis in the kernel for few rows; 0: not by that
     int64_t parts = -1, weight_parts = -1;
     int64_t stride;                  // values of a row of dz
@@ -677,10 +678,10 @@ hipError_t backward(const head_layer &l, const void *z, int64_t z_stride, const 
 
 head_layer_launch_t layer_launch(const head_layer &l, bool gated)
 {
-    const Plan f = plan_forward(l, gated), b = plan_backward(l, gated);
-    auto tile = [](const Cut &c) { return 64 << c.size; };
+    const Plan f = plan_forward(l, gated), b = l.n_outputs <= HEAD_MAX_OUTPUTS ? plan_backward(l, gated) : Plan{};
+    auto tile = [](const Cut &c) { return c.splits ? 64 << c.size : 0; };
     auto splits = [](const Cut &c) { return static_cast<int32_t>(c.splits); };
-    return head_layer_launch_t{static_cast<int32_t>(f.few), b.x >= 0, b.weight >= 0, f.few ? 0 : tile(f.forward), f.few ? 0 : splits(f.forward),
+    return head_layer_launch_t{static_cast<int32_t>(f.few), f.x >= 0 || b.x >= 0, f.weight >= 0 || b.weight >= 0, tile(f.forward), splits(f.forward),
                                tile(b.to_x), splits(b.to_x), tile(b.to_weight), splits(b.to_weight)};
 }
 

@@ -123,7 +123,7 @@ def test_testing_header_declares_what_the_library_exports():
     assert re.findall(r"\b(\w+)[,;]", code[code.index("struct"):code.index("} head_layer_launch_t")]) == [name for name, _ in hb._LayerLaunch._fields_]
     lib = hb._lib()
     assert all(hasattr(lib, name) for name in hb.HEAD_TESTING_EXPORTS)
-    for bad, code in (((0, 8, 8), -1), ((-1, 8, 8), -1), ((4, 0, 8), -1), ((4, 8, 0), -1), ((4, 16385, 8), -7), ((4, 8, 262_145), -7)):
+    for bad, code in (((0, 8, 8), -1), ((-1, 8, 8), -1), ((4, 0, 8), -1), ((4, 8, 0), -1), ((4, 16385, 8), -7), ((4, 8, 10 ** 9 + 1), -7)):
         with pytest.raises(pk.HeadError) as e:
             hb.head_layer_launch(*bad)
         assert e.value.code == code
@@ -165,6 +165,35 @@ GATED = [("bfloat16", 1003, 1027, 4093, 128), ("bfloat16", 9001, 336, 332, 128),
 def test_these_gated_layers_go_in_these_tiles(dtype, n, dim, outs, tile):
     s = hb.head_layer_launch(n, dim, outs, dtype, gated=True)
     assert (s["few"], s["tile"], s["splits"]) == (0, tile, 1), s
+
+
+# The kernel for few rows has a workgroup of 512 lanes for each 16 columns, and a grid's axis fewer than 2^32 lanes.
+MANY = [("bfloat16", False, 140_000_003, 8), ("float32", False, 140_000_000, 3), ("bfloat16", True, 134_217_729, 7)]
+
+
+@pytest.mark.parametrize("dtype,gated,outs,dim", MANY)
+def test_few_rows_of_very_many_columns_fit_a_grid(dtype, gated, outs, dim):
+    for n in (1, 16, 64):
+        for columns in (outs, 10 ** 9 // (1 + gated)):
+            s = hb.head_layer_launch(n, dim, columns, dtype, gated)
+            assert s["few"] == 0 and s["tile"] and s["splits"] == 1 and s["to_x_tile"] == 0, s
+        assert hb.head_layer_launch(n, dim, 1 << 15, dtype, gated)["few"] == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,gated,outs,dim", MANY)
+def test_few_rows_of_very_many_columns(dtype, gated, outs, dim):
+    import torch
+    halves = 1 + gated
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    w = torch.randn(halves * outs, dim, generator=g, device="cuda", dtype=getattr(torch, dtype))
+    x = _normal(1, 1, dim, dtype=dtype)
+    y = pk.head_gated(x, w, None, "gelu") if gated else pk.head_linear(x, w, None, "gelu")
+    assert y.shape == (1, outs)
+    at = torch.randint(0, outs, (200_000,), generator=g, device="cuda")
+    at = torch.cat([at, torch.arange(5, device="cuda"), outs - 1 - torch.arange(5, device="cuda"), torch.arange(134_217_700, 134_217_729, device="cuda")])
+    picked = torch.cat([w[at], w[at + outs]]) if gated else w[at]
+    _check_forward(y[:, at], None, x, picked, None, "gelu", None, 1.0, gated, dtype)
 
 
 # ---------------------------------------------------------------- tiles
