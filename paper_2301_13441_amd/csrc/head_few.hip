@@ -141,8 +141,6 @@ template <class T, bool GATED>
 hipError_t launch_few(const head_layer &l, const End<T> &end, int64_t splits, float *parts, hipStream_t stream)
 {
     constexpr int WAVES = 8;
-    const uint64_t strides = static_cast<uint64_t>((l.x_stride | l.weight_stride | l.dim) * static_cast<int64_t>(sizeof(T)));
-    const bool wide = (address(l.x) | address(l.weight) | strides) % 16 == 0;
     const int each = static_cast<int>(ceil_div(ceil_div(l.dim, 64 / static_cast<int64_t>(sizeof(T))), splits));
     auto run = [&](auto WIDE, auto MT) {
         hipLaunchKernelGGL((few_kernel<T, GATED, WIDE(), MT(), WAVES>), dim3(static_cast<uint32_t>(ceil_div(l.n_outputs, COLUMNS)), static_cast<uint32_t>(splits)),
@@ -154,7 +152,7 @@ hipError_t launch_few(const head_layer &l, const End<T> &end, int64_t splits, fl
         using std::integral_constant;
         return l.n_rows <= 16 ? run(WIDE, integral_constant<int, 1>()) : l.n_rows <= 32 ? run(WIDE, integral_constant<int, 2>()) : run(WIDE, integral_constant<int, 4>());
     };
-    return wide ? rows(std::true_type()) : rows(std::false_type());
+    return few_wide(l) ? rows(std::true_type()) : rows(std::false_type());
 }
 
 template hipError_t launch_few<float, false>(const head_layer &, const End<float> &, int64_t, float *, hipStream_t);

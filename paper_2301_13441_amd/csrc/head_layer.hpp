@@ -101,6 +101,13 @@ constexpr int64_t FEW_ROWS = 64;
 constexpr int FEW_COLUMNS = 16;               // of y, of a workgroup of 512 lanes
 constexpr int64_t FEW_WORKGROUPS = 1 << 22;   // of a launch: 2^31 lanes, a grid's axis has room for 2^32.  Layers of more columns go by tiles
 
+// Whether it reads rows in whole pieces of 16 bytes; value by value otherwise.
+inline bool few_wide(const head_layer &l)
+{
+    const uint64_t strides = static_cast<uint64_t>((l.x_stride | l.weight_stride | l.dim) * value_bytes(l.dtype));
+    return (address(l.x) | address(l.weight) | strides) % 16 == 0;
+}
+
 template <class T, bool GATED>
 hipError_t launch_few(const head_layer &l, const End<T> &end, int64_t splits, float *parts, hipStream_t stream);
 

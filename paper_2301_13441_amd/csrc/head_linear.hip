@@ -386,6 +386,7 @@ enum { TINY, SMALL, LARGE };
 struct Cut {
     int size;
     int64_t row_tiles, column_tiles, splits, split_depth;
+    double us;  // by cut_of's model
     int64_t tiles() const { return row_tiles * column_tiles * splits; }
 };
 
@@ -421,32 +422,10 @@ Cut cut_of(int32_t dtype, int64_t rows, int64_t columns, int64_t depth, int most
             const double others = static_cast<double>((std::min(tiles, resident) + 255) / 256 - 1);
             const double rounds = static_cast<double>((tiles + resident - 1) / resident);
             const double us = 2.2 + rounds * (static_cast<double>(each) * (t.step + t.more * others) + t.end) + (splits > 1 ? 2.5 + splits * part_us : 0);
-            if (us < least) least = us, best = Cut{size, row_tiles, column_tiles, splits, each * step};
+            if (us < least) least = us, best = Cut{size, row_tiles, column_tiles, splits, each * step, us};
         }
     }
     best.splits = std::max<int64_t>(1, ceil_div(depth, best.split_depth));  // none is empty
-    return best;
-}
-
-// Parts of the sum's axis with which the kernel for few rows (head_few.hip) takes a layer whose z has that many columns; 0: tiles take it.  From
-// times of both over 10 shapes from 64 -> 256 to 8192 -> 2048 with 1 to 64 rows: up to 16 rows tiles are faster hardly anywhere; with more the
-// few-rows kernel, which reads a layer's rows again for each 16 columns, is faster up to some 128 MB of weights times rows (64 x 1024 -> 1024
-// bfloat16 7.5 us in both, 64 x 2048 -> 8192 21.5 and 13.1).  A wavefront's step, of 64 bytes of 16 weights, takes the longer the more rows there are; there are 8
-// wavefronts in a workgroup, and 512 workgroups or more need no other parts.  16 x 16384 -> 64: 30 us in one part, 6.9 in 16.
-int64_t few_of(const head_layer &l, int64_t columns)
-{
-    const int64_t row_bytes = l.dim * value_bytes(l.dtype);
-    if (l.n_rows > FEW_ROWS || ceil_div(l.n_outputs, FEW_COLUMNS) > FEW_WORKGROUPS) return 0;
-    if (l.n_rows > 16 && l.n_rows * columns * row_bytes > int64_t{1} << 27) return 0;
-    static const double STEP_US[] = {0.26, 0.42, 0.63, 1.06};
-    const double step = STEP_US[l.n_rows == 1 ? 0 : l.n_rows <= 16 ? 1 : l.n_rows <= 32 ? 2 : 3];
-    const int64_t steps = ceil_div(row_bytes, 64), workgroups = ceil_div(l.n_outputs, FEW_COLUMNS);
-    int64_t best = 1;
-    double least = INFINITY;
-    for (int64_t splits = 1; splits <= 16 && (splits == 1 || (splits * workgroups <= 512 && splits * 8 <= steps)); splits *= 2) {
-        const double us = static_cast<double>((steps + 8 * splits - 1) / (8 * splits)) * step + (splits > 1 ? 2.4 + 0.1 * static_cast<double>(splits) : 0);
-        if (us < least) least = us, best = splits;
-    }
     return best;
 }
 
@@ -484,6 +463,46 @@ bool readable(int32_t dtype, const void *at, int64_t stride)
     return bytes <= FLOW_STRIDE && (address(at) | static_cast<uint64_t>(bytes)) % 4 == 0;
 }
 
+constexpr int FORWARD_SPLITS = 32;  // of a layer's product, at most: finish_kernel adds a value's parts one after the other
+
+// Parts of the sum's axis with which the kernel for few rows (head_few.hip) takes a layer whose z has that many columns; 0: tiles take it.
+//
+// Rows that are whole in 16 bytes, from times of both over 10 shapes from 64 -> 256 to 8192 -> 2048 with 1 to 64 rows: up to 16 rows tiles are faster
+// hardly anywhere, but for large bfloat16 weights that the caches hold (1 x 4096 -> 16384 33 us, by tiles 24); with more the few-rows kernel, which
+// reads a layer's rows again for each 16 columns, is faster up to some 128 MB of weights times rows (64 x 1024 -> 1024 bfloat16 7.5 us in both, 64 x 2048 ->
+// 8192 21.5 and 13.1).  A wavefront's step, of 64 bytes of 16 weights, takes the longer the more rows there are; there are 8 wavefronts in a workgroup, and
+// 512 workgroups or more need no other parts.  16 x 16384 -> 64: 30 us in one part, 6.9 in 16.
+//
+// Others are read value by value, and each of 256 CUs takes its workgroups one after the other: a workgroup by its rows, a step by its loads, fewer than
+// 8 steps by their share of 8.  Tiles read such rows in pieces of 16 bytes from any word of 4, bfloat16 rows that begin at odd values after a copy.  From times of
+// both over 103 layers, linear and gated, from 3 -> 1000 to 8186 -> 4096 and 31 -> 262144, with 1 to 64 rows: the choice is 1 % behind the faster on
+// average, 37 % at most.  us in the few-rows kernel and by tiles, bfloat16: 1 x 58 -> 256 4.0 and 5.7, 1 x 2042 -> 8192 24 and 13, 16 x 4090 -> 16384 156 and 27; odd
+// 1 x 249 -> 16384 8.1 and 19, 16 x 4089 -> 16384 154 and 81; float32 16 x 2041 -> 8192 42 and 25.  16 x 1018 -> 1000 bfloat16: 13 in one part, 7.8 in 4.
+int64_t few_of(const head_layer &l, int64_t columns, bool gated)
+{
+    const bool wide = few_wide(l);
+    const int64_t row_bytes = l.dim * value_bytes(l.dtype);
+    if (l.n_rows > FEW_ROWS || ceil_div(l.n_outputs, FEW_COLUMNS) > FEW_WORKGROUPS) return 0;
+    if (l.n_rows > 16 && l.n_rows * columns * row_bytes > int64_t{1} << 27) return 0;
+    static const double STEP_US[] = {0.26, 0.42, 0.63, 1.06};
+    const double rows = static_cast<double>(l.n_rows);
+    const double step = wide ? STEP_US[l.n_rows == 1 ? 0 : l.n_rows <= 16 ? 1 : l.n_rows <= 32 ? 2 : 3] : ((gated ? 2.3 : 1.3) + 0.07 * rows) * 2 / value_bytes(l.dtype);
+    const int64_t steps = ceil_div(row_bytes, 64), workgroups = ceil_div(l.n_outputs, FEW_COLUMNS);
+    int64_t best = 1;
+    double least = INFINITY;
+    for (int64_t splits = 1; splits <= 16 && (splits == 1 || (splits * workgroups <= 512 && splits * 8 <= steps)); splits *= 2) {
+        double us = static_cast<double>((steps + 8 * splits - 1) / (8 * splits)) * step;
+        if (!wide) us = static_cast<double>(ceil_div(splits * workgroups, 256)) * (0.3 + 0.01 * rows + (steps < 8 ? static_cast<double>(steps) / 8 * step : us));
+        if (splits > 1) us += 2.4 + 0.1 * static_cast<double>(splits);
+        if (us < least) least = us, best = splits;
+    }
+    if (wide || least < 2.2) return best;  // tiles take that and more
+    double tiles = cut_of(l.dtype, l.n_rows, columns, l.dim, FORWARD_SPLITS, gated).us;
+    const int64_t copied = (readable(l.dtype, l.x, l.x_stride) ? 0 : l.n_rows) + (readable(l.dtype, l.weight, l.weight_stride) ? 0 : columns);
+    if (copied) tiles += 5 + static_cast<double>(copied * row_bytes) * 2 / 5e6;  // launches, and a copy's reads and writes at 5 TB/s
+    return tiles < least ? 0 : best;
+}
+
 void plan_operands(const head_layer &l, int64_t columns, Plan &p)
 {
     const int e = value_bytes(l.dtype);
@@ -497,13 +516,13 @@ Plan plan_forward(const head_layer &l, bool gated)
     Plan p;
     const int64_t columns = gated ? 2 * l.n_outputs : l.n_outputs;
     if (l.n_rows == 0) return p;
-    p.few = few_of(l, columns);
+    p.few = few_of(l, columns, gated);
     if (p.few) {
         if (p.few > 1) p.parts = p.part(p.few * l.n_rows * columns * 4);
         return p;
     }
     plan_operands(l, columns, p);
-    p.forward = cut_of(l.dtype, l.n_rows, columns, l.dim, 32, gated);  // finish_kernel adds a value's parts one after the other
+    p.forward = cut_of(l.dtype, l.n_rows, columns, l.dim, FORWARD_SPLITS, gated);
     if (p.forward.splits > 1) p.parts = p.part(p.forward.splits * l.n_rows * columns * 4);
     return p;
 }
