@@ -134,12 +134,16 @@ __device__ __forceinline__ double squares_of(const Batch &b)
 template <int TEAM>
 __device__ __forceinline__ void scale_all(const Batch &b, double norm, double max_norm)
 {
-    const float factor = max_norm >= norm || max_norm == INFINITY ? 1.0f : static_cast<float>(max_norm / norm);
-    if (factor == 1.0f && b.in_place) return;
+    const double share = max_norm >= norm || max_norm == INFINITY ? 1.0 : max_norm / norm;
+    const bool same = static_cast<float>(share) == 1.0f;
+    // A share that float32 holds with few bits or none, as of values near its end and a small limit, goes in two factors, the second a power of two.
+    int down = 0;
+    const float factor = static_cast<float>(share < 0x1p-100 ? frexp(share, &down) : share);
+    if (same && b.in_place) return;
     over_blocks<TEAM>(b, [&](const Tensor &t, auto type, int64_t block) {
         using T = decltype(type);
         constexpr int V = 16 / sizeof(T);
-        if (t.grad == t.out && factor == 1.0f) return;
+        if (t.grad == t.out && same) return;
         Pack<T, V> p[PIECES];
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) p[j] = take(static_cast<const T *>(t.grad), place<T, TEAM>(block, j), t.n, t.wide);
@@ -147,7 +151,7 @@ __device__ __forceinline__ void scale_all(const Batch &b, double norm, double ma
         for (int j = 0; j < PIECES; ++j) {
             const int64_t at = place<T, TEAM>(block, j);
 #pragma unroll
-            for (int i = 0; i < V; ++i) p[j].v[i] = factor == 1.0f ? p[j].v[i] : narrow<T>(widen(p[j].v[i]) * factor);
+            for (int i = 0; i < V; ++i) p[j].v[i] = same ? p[j].v[i] : narrow<T>(ldexpf(widen(p[j].v[i]) * factor, down));
             T *to = static_cast<T *>(t.out);
             if (t.wide && at + V <= t.n) {
                 store_past(to + at, p[j]);

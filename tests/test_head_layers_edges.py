@@ -256,3 +256,23 @@ def test_layers_in_the_largest_tiles(gated, n, dim, outs):
         got = take()
         _check_gradients(got, grad, x, w, z, act, 1.0 if gated else scale, gated, dtype)
         assert all(p is None or torch.equal(p, q) for p, q in zip(take(), got))  # the same call gives the same bits
+
+
+# ---------------------------------------------------------------- clipping
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [100, 300_001])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_clip_by_a_share_that_float32_does_not_hold(dtype, n):
+    """Values near the end of float32 and limits far below them: the share is subnormal in float32, or below that, and the results are ordinary."""
+    import torch
+    for limit in (1e-6, 1e-20, 1e-33, 2.0 ** -100 * 3e38):
+        g = _normal(n, n).clamp_(-4, 4).mul_(5e37).to(getattr(torch, dtype))
+        norm64 = g.double().square().sum().sqrt()
+        want = g.double() * (limit / norm64)
+        for in_place in (False, True):
+            norm, (got,) = pk.head_clip([g], limit, in_place=in_place)
+            assert norm.item() == math.inf or abs(norm.item() / norm64.item() - 1) <= 5 * U
+            # the norm's and the factor's rounding, the product's and that to the type; results below the smallest normal ones in steps of the type's last
+            off = (got.double() - want).abs()
+            assert (off <= (NEAR[dtype] + 8 * U) * want.abs() + 2.0 ** -125 * NEAR[dtype]).all(), (limit, in_place, (off / want.abs()).max().item())
