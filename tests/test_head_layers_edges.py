@@ -221,6 +221,61 @@ def test_few_odd_rows(dtype, gated, n, dim, outs, apart, few):
     _check_forward(y, z, x, w, b, "silu", rest, 0.5, gated, dtype)
 
 
+# Rows that begin further apart than products read them where they are, 2 MB and 256 bytes, just as far, and in bfloat16 at odd values.
+FAR = [(dtype, apart) for dtype, apart in (("float32", 1), ("float32", 0), ("bfloat16", 1), ("bfloat16", 2), ("bfloat16", 0))]
+
+
+def _far_stride(dtype, apart):
+    return ((1 << 21) + 256) // (4 if dtype == "float32" else 2) + apart
+
+
+@pytest.mark.parametrize("dtype,apart", FAR)
+def test_rows_too_far_apart_are_copied_first(dtype, apart):
+    stride = _far_stride(dtype, apart)
+    for gated in (False, True):
+        s = hb.head_layer_launch(70, 41, 33, dtype, gated, x_stride=stride, weight_stride=stride)
+        assert s["few"] == 0 and s["copies_x"] == s["copies_weight"] == (apart > 0), s
+        s = hb.head_layer_launch(70, 40, 33, dtype, gated, x_stride=stride, weight_stride=40)
+        assert s["copies_x"] == (apart > 0) and not s["copies_weight"], s
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,apart", FAR)
+def test_rows_that_lie_megabytes_apart(dtype, apart):
+    """All operands so, with NaN between their rows and behind the last."""
+    import torch
+    stride = _far_stride(dtype, apart)
+
+    def far(t):
+        whole = torch.full((len(t), stride), math.nan, device="cuda", dtype=t.dtype)
+        whole[:, 2:2 + t.shape[1]] = t
+        return whole[:, 2:2 + t.shape[1]]
+
+    for n, dim, outs in ((70, 41, 34), (5, 40, 33)):
+        x, b, rest, grad = far(_normal(1, n, dim, dtype=dtype)), _normal(2, 2 * outs), far(_normal(3, n, outs, dtype=dtype)), far(_normal(4, n, outs, dtype=dtype, scale=0.1))
+        w = far(_normal(5, 2 * outs, dim, dtype=dtype, scale=dim ** -0.5))
+        for act in ("silu", None):
+            y, z = pk.head_linear(x, w[:outs], b[:outs], act, rest, 0.5, keep=True)
+            _check_forward(y, z, x, w[:outs], b[:outs], act, rest, 0.5, False, dtype)
+            got = pk.head_linear_grad(grad, x, w[:outs], far(z), act, 0.5)
+            _check_gradients(got, grad, x, w[:outs], z, act, 0.5, False, dtype)
+            y, z = pk.head_gated(x, w, b, act, keep=True)
+            _check_forward(y, z, x, w, b, act, None, 1.0, True, dtype)
+            _check_gradients(pk.head_gated_grad(grad, x, w, far(z), act), grad, x, w, z, act, 1.0, True, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gated", [False, True])
+def test_float32_gradients_of_the_most_outputs(gated):
+    """Gated, rows of the gradient of z begin just as far apart as products read them."""
+    n, dim, outs, dtype = 70, 9, 262_144, "float32"
+    columns = outs * (1 + gated)
+    x, w = _normal(1, n, dim), _normal(2, columns, dim, scale=dim ** -0.5)
+    z, grad = _normal(3, n, columns), _normal(4, n, outs, scale=0.1)
+    got = pk.head_gated_grad(grad, x, w, z, "silu") if gated else pk.head_linear_grad(grad, x, w, z, "silu")
+    _check_gradients(got, grad, x, w, z, "silu", 1.0, gated, dtype)
+
+
 # ---------------------------------------------------------------- tiles
 
 @pytest.mark.gpu
@@ -276,3 +331,24 @@ def test_clip_by_a_share_that_float32_does_not_hold(dtype, n):
             # the norm's and the factor's rounding, the product's and that to the type; results below the smallest normal ones in steps of the type's last
             off = (got.double() - want).abs()
             assert (off <= (NEAR[dtype] + 8 * U) * want.abs() + 2.0 ** -125 * NEAR[dtype]).all(), (limit, in_place, (off / want.abs()).max().item())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [100, 300_001])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_the_norm_alone(dtype, n):
+    """The C call whose tensors have no results: nothing but the norm is written, whatever the limit is."""
+    import torch
+    lib, tensors = hb._lib(), [_normal(1, n, dtype=dtype), _normal(2, 33), _normal(3, 0)]
+    before = [t.clone() for t in tensors]
+    want = math.sqrt(sum(t.double().square().sum().item() for t in tensors))
+    rows = (hb._ClipTensor * 3)(*(hb._ClipTensor(t.data_ptr() or None, None, t.numel(), int(t.dtype == torch.bfloat16)) for t in tensors))
+    size = lib.head_clip_bytes(rows, 3)
+    assert (size > 0) == (n > 100)
+    work, norm = torch.empty(max(16, size), dtype=torch.uint8, device="cuda"), torch.full((3,), -1.0, device="cuda")
+    for limit in (0.5, 1e9, math.inf):
+        norm.fill_(-1)
+        assert lib.head_clip(rows, 3, limit, norm.data_ptr() + 4, work.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+        got = norm.tolist()
+        assert abs(got[1] - want) <= 5 * U * want and got[0] == got[2] == -1
+        assert all(torch.equal(a, b) for a, b in zip(tensors, before))
