@@ -144,6 +144,11 @@ int head_cross_entropy_grad(const head_classes *c, const float *lse, const float
  * and bias [2 * n_outputs]; the first n_outputs columns of z are gates, the others values, and each value is multiplied by the
  * activation of its gate.
  *
+ * Products of float32 values are float32 sums.  Those of gradients, of many rows, and of few rows with large weights that are not whole in 16 bytes are
+ * made of three bfloat16 parts of each value, which together are the value and round as float32 products do; of a value below 2^-109 they are the
+ * value to 2^-133, which counts where the other operand is large (some 2^-13 of a product of 2^-120 and 2^120).  So a row's last bits may depend on
+ * how many rows its call has.
+ *
  * HEAD_GELU is x times the normal distribution's integral up to x, HEAD_SILU x / (1 + exp(-x)); the slope of HEAD_RELU at 0 is 0.
  * For bfloat16 values activations and slopes are right to 2^-13, relative to the activation and to 1, which is small next to their results'
  * rounding.

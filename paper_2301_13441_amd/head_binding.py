@@ -553,6 +553,9 @@ def head_linear(x, weight, bias=None, activation: Optional[str] = None, residual
     None, "relu", "gelu" (x times the normal distribution's integral up to x) or "silu".  residual: [n_rows, n_outputs] of the same type, or
     None.  Returns y, [n_rows, n_outputs] of the same type, and with keep (y, z): z, which the gradients of a layer with an
     activation need.
+
+    float32 products of many rows, and those of the gradients, take a value below 2^-109 to 2^-133 (include/head.h); a row's last bits may depend on how
+    many rows its call has.
     """
     act = _activation(activation)
     if stream is None:
@@ -614,7 +617,7 @@ def head_gated(x, weight, bias=None, activation: Optional[str] = "silu", keep: b
 
     x: [n_rows, dim] float32 or bfloat16, weight: [2 * n_outputs, dim] of the same type, bias: float32 [2 * n_outputs] or None, activation: as
     in head_linear.  Returns y, [n_rows, n_outputs] of the same type, and with keep (y, z): z, [n_rows, 2 * n_outputs], which
-    the gradients need.
+    the gradients need.  Products are as in head_linear.
     """
     act = _activation(activation)
     if stream is None:
