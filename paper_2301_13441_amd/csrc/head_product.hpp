@@ -1,6 +1,7 @@
-// Matrix products C = A B of the trainable head, on gfx950: the body that the kernels of head_loss.hip and head_linear.hip run on.  A
-// workgroup makes tiles of C one after the other; A and B come to LDS in tiles of 128 bytes of the sum's axis, by the loads that bypass
-// registers, while the matrix core works on the tiles before.  An operand lies in memory with the sum's axis along its rows or across
+// Matrix products C = A B of the trainable head, on gfx950.  What head_loss.hip and head_linear.hip share: operands, the shapes of a workgroup's tile,
+// their order over the XCDs, and the kernels that add parts; and the body that head_loss.hip's kernels run on (Tile, Products; that of head_linear.hip is in
+// head_flow.hpp).  There a workgroup makes tiles of C one after the other; A and B come to LDS in tiles of 128 bytes of the sum's axis, by the loads that
+// bypass registers, while the matrix core works on the tiles before.  An operand lies in memory with the sum's axis along its rows or across
 // them.  bfloat16 products run on the 32x32x16 matrix instruction, float32 ones on the 32x32x2 float32 one, whose rate, a sixteenth, then
 // bounds them; both accumulate in float32.
 #pragma once
