@@ -2,8 +2,8 @@
 
 Thin binding over the C ABI declared in include/forest.h, include/linear.h and include/head.h: ctypes, and a CPython extension on
 torch's C++ interface for the calls whose time is the host's (csrc/short_call.cpp), without which they go the ctypes way.
-PyTorch is used only for device memory and streams, and by LeafHead for its first values, the number of a batch's targets and the mean
-loss.  There is no CPU fallback: without the built HIP library, or without a GPU at load time, the calls raise.
+PyTorch is used only for device memory and streams, and by LeafHead for its first values, the number of a batch's targets, the mean
+loss and the sum of a residual block's two gradients.  There is no CPU fallback: without the built HIP library, or without a GPU at load time, the calls raise.
 """
 from .binding import (Forest, ForestError, forest_load, forest_pack, lib_path, load_library,
                       AGG_SUM, AGG_MEAN, TRANSFORM_NONE, TRANSFORM_SIGMOID, TRANSFORM_SOFTMAX,

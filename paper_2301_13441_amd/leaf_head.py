@@ -105,7 +105,8 @@ class LeafHead:
             g_h, g_out_weight, g_out_bias = head_linear_grad(g, h, out_weight, scale=self.block_scale)
             g_u, g_wide_weight, g_wide_bias = head_gated_grad(g_h, u, wide_weight, z, self.activation)
             g_x, g_norm_weight, g_norm_bias = head_layer_norm_grad(g_u, x, b.norm_weight, mean, rstd)
-            g = g_x.add_(g)  # the block's and what goes past it
+            # The block's and what goes past it, by torch, in a pass of its own: in bfloat16 the sum is rounded once more, for each block.
+            g = g_x.add_(g)
             grads = [g_norm_weight, g_norm_bias, g_wide_weight, g_wide_bias, g_out_weight, g_out_bias] + grads
         return g, grads
 
