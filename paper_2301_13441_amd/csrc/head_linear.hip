@@ -494,9 +494,10 @@ int64_t few_of(const head_layer &l, int64_t columns, bool gated)
         double us = static_cast<double>((steps + 8 * splits - 1) / (8 * splits)) * step;
         if (!wide) us = static_cast<double>(ceil_div(splits * workgroups, 256)) * (0.3 + 0.01 * rows + (steps < 8 ? static_cast<double>(steps) / 8 * step : us));
         if (splits > 1) us += 2.4 + 0.1 * static_cast<double>(splits);
+        if (splits > 1 && !wide) us = std::max(us, 6.5 + 0.01 * static_cast<double>(splits));  // the host's two launches
         if (us < least) least = us, best = splits;
     }
-    if (wide || least < 2.2) return best;  // tiles take that and more
+    if (wide || least < 3.9) return best;  // tiles take more than that by any cut, and looking for the best one takes the host half a microsecond
     double tiles = cut_of(l.dtype, l.n_rows, columns, l.dim, FORWARD_SPLITS, gated).us;
     const int64_t copied = (readable(l.dtype, l.x, l.x_stride) ? 0 : l.n_rows) + (readable(l.dtype, l.weight, l.weight_stride) ? 0 : columns);
     if (copied) tiles += 5 + static_cast<double>(copied * row_bytes) * 2 / 5e6;  // launches, and a copy's reads and writes at 5 TB/s
