@@ -37,7 +37,8 @@ __device__ __forceinline__ float reciprocal32(float y)
     return y < INFINITY ? fmaf(fmaf(-y, r, 1.0f), r, r) : r;
 }
 
-// Value and slope of an activation at x, for results of type T.
+// Value and slope of an activation at x, for results of type T.  Those of bfloat16 results, whose own rounding is 2^-9 of them, are right to 2^-13: a shorter
+// polynomial, and the exponential and the reciprocal as the instructions give them.
 template <class T, int ACTIVATION>
 struct Activation {
     float value, slope;

@@ -227,6 +227,10 @@ struct Slopes {
     float *parts;
 };
 
+// dz of bfloat16 values is rounded to bfloat16, one plane of 8 bits: that is what the matrix core takes at once, and a second plane would double the products
+// (522 of the 652 us of 16,384 x 1024 to 4096 gated ones), for gradients that are 0.0017 from 64 bits, by their own rounding alone, in place of 0.0023.
+// The sums of its columns take it before that.
+//
 // LANES lanes side by side, of N columns each, 256 / LANES rows at a time.  Bound by memory: 16,384 rows of 4096 gated bfloat16 columns, 671 MB, 118 us
 // (5.7 TB/s); one value a lane where rows are odd, 4,099 of 331 gated float32 ones 8.4 us (3.2 TB/s).
 template <class T, bool GATED, int N, int LANES>
